@@ -1,0 +1,383 @@
+// Appending to the 8-bit paged cache (wz_cache_append): rotation, scales,
+// rounding and layout in one launch.
+//
+// A workgroup of the first part owns one page that receives tokens and one
+// key/value head, so the page's scales need no other workgroup: it reads the
+// new keys and values once into registers, takes their largest magnitudes,
+// fixes both scales, moves what the page held to them if they grew, and
+// writes codes.  Values are turned to [head_dim][page_size] through LDS.
+// Workgroups behind those rotate the queries.
+#include "wz_serve.h"
+
+namespace wz {
+namespace {
+
+constexpr int kThreads = 256;
+
+// Eight consecutive elements as fp32.
+template <typename In>
+__device__ __forceinline__ void load8(const In* p, float (&x)[8]) {
+  if constexpr (sizeof(In) == 2) {
+    const u32x4 u = *reinterpret_cast<const u32x4*>(p);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x[2 * i] = bf16_lo(u[i]), x[2 * i + 1] = bf16_hi(u[i]);
+  } else {
+    const f32x4 a = reinterpret_cast<const f32x4*>(p)[0], b = reinterpret_cast<const f32x4*>(p)[1];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x[i] = a[i], x[4 + i] = b[i];
+  }
+}
+template <typename In>
+__device__ __forceinline__ void load4(const In* p, float (&x)[4]) {
+  if constexpr (sizeof(In) == 2) {
+    const u32x2 u = *reinterpret_cast<const u32x2*>(p);
+    x[0] = bf16_lo(u[0]), x[1] = bf16_hi(u[0]), x[2] = bf16_lo(u[1]), x[3] = bf16_hi(u[1]);
+  } else {
+    const f32x4 a = *reinterpret_cast<const f32x4*>(p);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x[i] = a[i];
+  }
+}
+
+// Cosines and sines of COUNT frequencies from j on, for token t.
+template <int COUNT>
+__device__ __forceinline__ void angles(const wz_rotation& r, int tokens, int t, int j, float (&c)[COUNT],
+                                       float (&s)[COUNT]) {
+  auto row = [&](int f) {
+    int a = 0;
+    if (r.axes > 1) a = f < r.sections[0] ? 0 : f < r.sections[0] + r.sections[1] ? 1 : 2;
+    const int p = r.positions[int64_t(a) * tokens + t];
+    return min(max(p, 0), r.max_pos - 1);
+  };
+  const int half = r.rot_dim / 2;
+  auto section = [&](int f) {
+    return r.axes == 1 ? 0 : f < r.sections[0] ? 0 : f < r.sections[0] + r.sections[1] ? 1 : 2;
+  };
+  if (section(j) == section(j + COUNT - 1)) {
+    const float* p = r.table + int64_t(row(j)) * r.rot_dim + j;
+#pragma unroll
+    for (int i = 0; i < COUNT; i += 4) {
+      const f32x4 u = *reinterpret_cast<const f32x4*>(p + i), w = *reinterpret_cast<const f32x4*>(p + half + i);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) c[i + e] = u[e], s[i + e] = w[e];
+    }
+  } else {
+    for (int i = 0; i < COUNT; ++i) {
+      const float* p = r.table + int64_t(row(j + i)) * r.rot_dim + j + i;
+      c[i] = p[0], s[i] = p[half];
+    }
+  }
+}
+
+// The angles that the eight elements from 8 * chunk on turn by, and how.
+struct Turn {
+  int partner;  // offset in elements of the other halves of the pairs (0: inside the chunk, or none)
+  bool turned, second;
+  float c[8], s[8];  // interleaved: the first four
+};
+__device__ __forceinline__ Turn turn_of(const wz_rotation& r, int tokens, int t, int chunk) {
+  Turn u;
+  u.partner = 0, u.turned = chunk * 8 < r.rot_dim, u.second = false;
+  if (!u.turned) return u;
+  if (r.interleaved) {
+    float c[4], s[4];
+    angles<4>(r, tokens, t, chunk * 4, c, s);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) u.c[i] = c[i], u.s[i] = s[i];
+  } else {
+    const int half = r.rot_dim / 2;
+    u.second = chunk * 8 >= half;
+    u.partner = u.second ? -half : half;
+    angles<8>(r, tokens, t, chunk * 8 - (u.second ? half : 0), u.c, u.s);
+  }
+  return u;
+}
+// The rotated elements.  No fused multiply-add: a key rounds to the same code
+// wherever it is computed in plain fp32 products and sums.
+template <typename In>
+__device__ __forceinline__ void load_turned(const In* p, const Turn& u, bool interleaved, float (&x)[8]) {
+#pragma clang fp contract(off)
+  load8(p, x);
+  if (!u.turned) return;
+  if (interleaved) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float a = x[2 * i], b = x[2 * i + 1];
+      x[2 * i] = a * u.c[i] - b * u.s[i];
+      x[2 * i + 1] = b * u.c[i] + a * u.s[i];
+    }
+  } else {
+    float y[8];
+    load8(p + u.partner, y);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const float ac = x[i] * u.c[i], bs = y[i] * u.s[i];
+      x[i] = u.second ? ac + bs : ac - bs;
+    }
+  }
+}
+
+__device__ __forceinline__ bool finite(float x) { return (__float_as_uint(x) & 0x7fffffffu) < 0x7f800000u; }
+
+// The least 2^e, e in [kScaleMinExp, kScaleMaxExp], with amax <= 448 * 2^e.
+__device__ __forceinline__ int scale_exp(float amax) {
+  const uint32_t u = __float_as_uint(amax);
+  // 448 = 1.75 * 2^8 (a subnormal amax has exponent field 0: the least scale)
+  const int e = int(u >> 23) - 127 - 8 + ((u & 0x7fffffu) > 0x600000u ? 1 : 0);
+  return min(max(e, kScaleMinExp), kScaleMaxExp);
+}
+
+// Four numbers to e4m3 codes, ties to even, beyond the range the largest.
+__device__ __forceinline__ uint32_t e4m3x4(float a, float b, float c, float d) {
+  auto cut = [](float x) { return __builtin_amdgcn_fmed3f(x, -kE4m3Max, kE4m3Max); };
+  int r = __builtin_amdgcn_cvt_pk_fp8_f32(cut(a), cut(b), 0, false);
+  return uint32_t(__builtin_amdgcn_cvt_pk_fp8_f32(cut(c), cut(d), r, true));
+}
+// Four codes moved to another scale; NaN codes stay (0x7f and 0xff hold no
+// number that a factor below one could make finite, and the cut would).
+__device__ __forceinline__ uint32_t rescaled4(uint32_t codes, float factor) {
+  auto f = [&](auto hi) { return __builtin_amdgcn_cvt_pk_f32_fp8(int(codes), decltype(hi)::value); };
+  const auto lo = f(std::false_type{}), hi = f(std::true_type{});
+  uint32_t y = e4m3x4(lo[0] * factor, lo[1] * factor, hi[0] * factor, hi[1] * factor);
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    if (((codes >> (8 * i)) & 0x7fu) == 0x7fu) y |= 0x7fu << (8 * i);
+  return y;
+}
+
+// The largest of a and of b over the workgroup's 256 threads (kept in smem[8]).
+__device__ __forceinline__ void block_max2(float& a, float& b, float* smem) {
+  a = wave_max_f32(a), b = wave_max_f32(b);
+  const int w = threadIdx.x / kWave;
+  if (__lane_id() == 0) smem[w] = a, smem[4 + w] = b;
+  __syncthreads();
+  a = fmaxf(fmaxf(smem[0], smem[1]), fmaxf(smem[2], smem[3]));
+  b = fmaxf(fmaxf(smem[4], smem[5]), fmaxf(smem[6], smem[7]));
+}
+
+// Stores go through byte merges where a 16-byte piece of the page also holds
+// tokens that are not new: bytes of `fresh` where `mask` is set.
+__device__ __forceinline__ uint32_t merge4(uint32_t old, uint32_t fresh, uint32_t mask) {
+  return (old & ~mask) | (fresh & mask);
+}
+// Byte mask of the slots s0 .. s0 + 3 that lie in [lo, hi).
+__device__ __forceinline__ uint32_t slots_mask(int s0, int lo, int hi) {
+  uint32_t m = 0;
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    if (s0 + i >= lo && s0 + i < hi) m |= 0xffu << (8 * i);
+  return m;
+}
+
+template <typename In, int D, int P>
+__device__ void append_page(const AppendArgs& a, int b, const Seq& q, int nth, int h, char* smem) {
+  constexpr int kChunks = D / 8;               // chunks of 8 elements in a row
+  constexpr int kRows = kThreads / kChunks;    // rows the workgroup covers at once (keys)
+  constexpr int kPasses = (P + kRows - 1) / kRows;
+  constexpr int kQuads = (P / 4) * (D / 4);    // 4 x 4 squares of values
+  constexpr int kSquares = (kQuads + kThreads - 1) / kThreads;
+  constexpr int kLd = P + 4;                   // bytes between channels of the turned values in LDS
+  uint8_t* turned = reinterpret_cast<uint8_t*>(smem);            // [D][kLd]
+  float* red = reinterpret_cast<float*>(smem + D * kLd);         // [8]
+  uint32_t* bad = reinterpret_cast<uint32_t*>(smem + D * kLd + 32);  // [P]
+
+  const int tid = threadIdx.x, Hkv = a.cache.kv_heads;
+  const int place_lo = max(q.place0, 0), end = min(q.place0 + q.n, q.kv);
+  const int entry = place_lo / P + nth;
+  const int page = page_of(a.batch, a.cache.pages, b, entry);
+  if (page < 0) return;
+  const int s0 = max(place_lo - entry * P, 0);   // slots [s0, s1) are new, [0, s0) held before
+  const int s1 = min(end - entry * P, P);
+  const int row0 = q.start + entry * P - q.place0;  // the call's row of slot 0
+
+  for (int i = tid; i < P; i += kThreads) bad[i] = 0;
+  __syncthreads();
+
+  // keys: thread (chunk, row)
+  const int chunk = tid % kChunks, krow = tid / kChunks;
+  float kx[kPasses][8];
+  float kmax = 0.f, vmax = 0.f;
+#pragma unroll
+  for (int i = 0; i < kPasses; ++i) {
+    const int slot = krow + i * kRows;
+    if (slot >= s0 && slot < s1) {
+      const int t = row0 + slot;
+      const Turn u = turn_of(a.turn, a.batch.tokens, t, chunk);
+      load_turned(static_cast<const In*>(a.k) + t * a.k_stride + h * D + chunk * 8, u, a.turn.interleaved, kx[i]);
+      bool nan = false;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        if (finite(kx[i][e])) kmax = fmaxf(kmax, fabsf(kx[i][e]));
+        else nan = true;
+      }
+      if (nan) bad[slot] = 1;
+    }
+  }
+  // values: squares of 4 tokens x 4 channels, so that a token's four channels
+  // are one load and a channel's four tokens one store
+  float vx[kSquares][4][4];
+#pragma unroll
+  for (int i = 0; i < kSquares; ++i) {
+    const int sq = tid + i * kThreads, d = (sq % (D / 4)) * 4, t4 = (sq / (D / 4)) * 4;
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      const int slot = t4 + r;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) vx[i][r][e] = 0.f;
+      if (sq < kQuads && slot >= s0 && slot < s1) {
+        load4(static_cast<const In*>(a.v) + (row0 + slot) * a.v_stride + h * D + d, vx[i][r]);
+        bool nan = false;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          if (!finite(vx[i][r][e])) vx[i][r][e] = 0.f, nan = true;
+          vmax = fmaxf(vmax, fabsf(vx[i][r][e]));
+        }
+        if (nan) bad[slot] = 1;
+      }
+    }
+  }
+  block_max2(kmax, vmax, red);  // its barrier also covers `bad`
+
+  float* const kscale = a.cache.k_scale + int64_t(page) * Hkv + h;
+  float* const vscale = a.cache.v_scale + int64_t(page) * Hkv + h;
+  float ks = pow2(scale_exp(kmax)), vs = pow2(scale_exp(vmax)), kmove = 1.f, vmove = 1.f;
+  if (s0 > 0) {
+    const float ok = *kscale, ov = *vscale;
+    if (ok < ks) kmove = ok / ks; else ks = ok;
+    if (ov < vs) vmove = ov / vs; else vs = ov;
+  }
+  __syncthreads();  // the old scales are read by every thread
+  if (tid == 0) *kscale = ks, *vscale = vs;
+  const float kinv = 1.f / ks, vinv = 1.f / vs;
+
+  uint8_t* const kpage = static_cast<uint8_t*>(a.cache.k) + (int64_t(page) * Hkv + h) * P * D;
+  uint8_t* const vpage = static_cast<uint8_t*>(a.cache.v) + (int64_t(page) * Hkv + h) * P * D;
+  if (kmove != 1.f)
+    for (int i = tid; i < s0 * kChunks; i += kThreads) {
+      u32x2* p = reinterpret_cast<u32x2*>(kpage) + i;
+      const u32x2 u = *p;
+      *p = u32x2{rescaled4(u[0], kmove), rescaled4(u[1], kmove)};
+    }
+#pragma unroll
+  for (int i = 0; i < kPasses; ++i) {
+    const int slot = krow + i * kRows;
+    if (slot >= s0 && slot < s1) {
+      const float(&x)[8] = kx[i];
+      u32x2 u{e4m3x4(x[0] * kinv, x[1] * kinv, x[2] * kinv, x[3] * kinv),
+              e4m3x4(x[4] * kinv, x[5] * kinv, x[6] * kinv, x[7] * kinv)};
+      if (bad[slot]) u = u32x2{0x7f7f7f7fu, 0x7f7f7f7fu};
+      *reinterpret_cast<u32x2*>(kpage + slot * D + chunk * 8) = u;
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < kSquares; ++i) {
+    const int sq = tid + i * kThreads, d = (sq % (D / 4)) * 4, t4 = (sq / (D / 4)) * 4;
+    if (sq < kQuads) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        *reinterpret_cast<uint32_t*>(turned + (d + e) * kLd + t4) =
+            e4m3x4(vx[i][0][e] * vinv, vx[i][1][e] * vinv, vx[i][2][e] * vinv, vx[i][3][e] * vinv);
+    }
+  }
+  __syncthreads();
+  constexpr int kPieces = D * (P / 16);
+  for (int i = tid; i < kPieces; i += kThreads) {
+    const int d = i / (P / 16), t16 = (i % (P / 16)) * 16;
+    const bool fresh = t16 < s1 && t16 + 16 > s0;
+    if (!fresh && !(vmove != 1.f && t16 < s0)) continue;
+    u32x4 y;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) y[e] = *reinterpret_cast<const uint32_t*>(turned + d * kLd + t16 + 4 * e);
+    u32x4* const p = reinterpret_cast<u32x4*>(vpage + d * P + t16);
+    if (t16 < s0 || t16 + 16 > s1) {
+      const u32x4 old = *p;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const int s = t16 + 4 * e;
+        uint32_t was = old[e];
+        if (vmove != 1.f) was = merge4(was, rescaled4(was, vmove), slots_mask(s, 0, s0));
+        y[e] = merge4(was, y[e], slots_mask(s, s0, s1));
+      }
+    }
+    *p = y;
+  }
+}
+
+// Query rows: thread (chunk, head group, token); it keeps its angles over the
+// heads it goes through.
+template <typename In, int D>
+__device__ void rotate_queries(const AppendArgs& a, int unit, int heads_at_once) {
+  constexpr int kChunks = D / 8;
+  const int chunk = threadIdx.x % kChunks, r = threadIdx.x / kChunks;
+  const int per = kThreads / kChunks / heads_at_once;
+  const int t = unit * per + r / heads_at_once;
+  if (t >= a.batch.tokens) return;
+  const Turn u = turn_of(a.turn, a.batch.tokens, t, chunk);
+  const In* src = static_cast<const In*>(a.q) + t * a.q_stride + chunk * 8;
+  uint16_t* dst = static_cast<uint16_t*>(a.q_out) + t * a.q_out_stride + chunk * 8;
+  for (int h = r % heads_at_once; h < a.q_heads; h += heads_at_once) {
+    float x[8];
+    load_turned(src + h * D, u, a.turn.interleaved, x);
+    u32x4 y;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) y[i] = f32_to_bf16_rne(x[2 * i]) | (f32_to_bf16_rne(x[2 * i + 1]) << 16);
+    *reinterpret_cast<u32x4*>(dst + h * D) = y;
+  }
+}
+
+template <typename In, int D, int P>
+__global__ __launch_bounds__(kThreads) void k_append(AppendArgs a, int page_groups, int heads_at_once) {
+  __shared__ __align__(16) char smem[D * (P + 4) + 32 + 4 * P];
+  const int id = blockIdx.x;
+  if (id >= page_groups) {
+    rotate_queries<In, D>(a, id - page_groups, heads_at_once);
+    return;
+  }
+  auto touched = [&](int b) {
+    const Seq q = sequence(a.batch, b);
+    const int lo = max(q.place0, 0), hi = min(q.place0 + q.n, q.kv);
+    return hi > lo ? (hi - 1) / P - lo / P + 1 : 0;
+  };
+  int b, nth;
+  if (!find_item(a.batch.batch, id / a.cache.kv_heads, touched, &b, &nth)) return;
+  append_page<In, D, P>(a, b, sequence(a.batch, b), nth, id % a.cache.kv_heads, smem);
+}
+
+template <typename In, int D>
+hipError_t launch(const AppendArgs& a, int groups, int units, int heads_at_once, hipStream_t s) {
+  const dim3 grid(groups + units), block(kThreads);
+  switch (a.cache.page_size) {
+    case 16: hipLaunchKernelGGL((k_append<In, D, 16>), grid, block, 0, s, a, groups, heads_at_once); break;
+    case 32: hipLaunchKernelGGL((k_append<In, D, 32>), grid, block, 0, s, a, groups, heads_at_once); break;
+    case 64: hipLaunchKernelGGL((k_append<In, D, 64>), grid, block, 0, s, a, groups, heads_at_once); break;
+    default: hipLaunchKernelGGL((k_append<In, D, 128>), grid, block, 0, s, a, groups, heads_at_once); break;
+  }
+  return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_append(const AppendArgs& a, int in_dtype, hipStream_t s) {
+  const wz_ragged& r = a.batch;
+  const int P = a.cache.page_size, D = a.cache.head_dim;
+  if (r.tokens == 0 || r.max_tokens == 0) return hipSuccess;
+  // pages that receive tokens: at most one a token, (n + P - 2) / P + 1 a
+  // sequence, and tokens / P and two more a sequence together
+  const int64_t pages = std::min({int64_t(r.tokens), int64_t(r.batch) * ((r.max_tokens + P - 2) / P + 1),
+                                  int64_t(r.tokens / P) + 2 * int64_t(r.batch)});
+  const int64_t groups = pages * a.cache.kv_heads;
+  int heads_at_once = 1;
+  const int most = 4;
+  while (heads_at_once < most && heads_at_once < a.q_heads) heads_at_once *= 2;
+  const int per = kThreads / (D / 8) / heads_at_once;
+  const int64_t units = a.q ? (int64_t(r.tokens) + per - 1) / per : 0;
+  if (groups + units > 0x7fffffff) return hipErrorInvalidValue;
+  const bool bf = in_dtype == WZ_BF16;
+  if (D == 128)
+    return bf ? launch<uint16_t, 128>(a, int(groups), int(units), heads_at_once, s)
+              : launch<float, 128>(a, int(groups), int(units), heads_at_once, s);
+  return bf ? launch<uint16_t, 64>(a, int(groups), int(units), heads_at_once, s)
+            : launch<float, 64>(a, int(groups), int(units), heads_at_once, s);
+}
+
+}  // namespace wz
