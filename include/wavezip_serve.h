@@ -168,8 +168,8 @@ wz_status wz_quantize_rows(const void* x, int64_t x_stride, int32_t rows,
  * multiplies first), rounded to out_dtype.  a [M][K] and w [N][K] int8, rows
  * a_stride and w_stride bytes apart; out [M][N], rows out_stride elements
  * apart; bias [N] fp32 or NULL.  Supported: 0 <= M < 2^24; 1 <= N < 2^24;
- * 16 <= K <= 65536 (K * 128^2 < 2^31 holds up to 131071), a multiple of 16;
- * a_stride, w_stride multiples of 16, >= K; out_stride >= N; a and w 16-byte
+ * 16 <= K <= 65536 (a sum is then at most 2^30), a multiple of 16; a_stride,
+ * w_stride multiples of 16, K to 2^22; out_stride >= N; a and w 16-byte
  * aligned, out aligned to its element.  One kernel launch.                   */
 wz_status wz_matmul_int(const int8_t* a, int64_t a_stride,
                         const float* a_scale, const int8_t* w,

@@ -1,5 +1,7 @@
 // Rows to 8-bit integers and their product with weights held the same way
 // (wz_quantize_rows, wz_matmul_int).
+#include <cmath>
+
 #include "wz_serve.h"
 
 namespace wz {
@@ -7,6 +9,8 @@ namespace {
 
 typedef int i32x4 __attribute__((ext_vector_type(4)));
 typedef int i32x16 __attribute__((ext_vector_type(16)));
+typedef u32x4 u32x4_of_2 __attribute__((aligned(2)));
+typedef u32x4 u32x4_of_4 __attribute__((aligned(4)));
 
 // ---------------------------------------------------------------------------
 // Rows to integers
@@ -104,87 +108,55 @@ hipError_t quantize(const In* x, int64_t x_stride, int rows, int cols, int8_t* q
 template <typename Out>
 __device__ __forceinline__ Out finish(int acc, float sa, float sw, float bias) {
   const float v = float(acc) * sa * sw + bias;
-  if constexpr (sizeof(Out) == 2) return f32_to_bf16_rne(v);
+  if constexpr (sizeof(Out) == 2) return __builtin_bit_cast(uint16_t, __bf16(v));
   else return v;
 }
 
-__device__ __align__(16) int g_zeros[4];  // what a lane behind the end of a row reads
-
-// Few rows: the weights are read once and the sum over k is what there is to
-// share.  Eight waves of a workgroup take the 64-byte steps of k in turn, for
-// 16 MT rows by 16 NT columns, straight from memory into the fragments, and
-// add up their integers through LDS.
-constexpr int kSkinnyWaves = 8;
-template <typename Out, int MT, int NT>
-__global__ __launch_bounds__(kSkinnyWaves* kWave) void k_matmul_skinny(MatmulArgs p) {
-  constexpr int BM = 16 * MT, BN = 16 * NT, kDepth = 4;
-  __shared__ int red[kSkinnyWaves][BM * BN];
-  const int lane = __lane_id(), w = threadIdx.x / kWave, c = lane & 15, g = lane >> 4;
-  const int n0 = blockIdx.x * BN, m0 = blockIdx.y * BM;
-  const int8_t *ap[MT], *wp[NT];
-#pragma unroll
-  for (int i = 0; i < MT; ++i) ap[i] = p.a + int64_t(min(m0 + 16 * i + c, p.M - 1)) * p.a_stride + 16 * g;
-#pragma unroll
-  for (int i = 0; i < NT; ++i) wp[i] = p.w + int64_t(min(n0 + 16 * i + c, p.N - 1)) * p.w_stride + 16 * g;
-  const int8_t* const zeros = reinterpret_cast<const int8_t*>(g_zeros);
-  i32x4 acc[MT][NT] = {};
-  const int steps = (p.K + 63) / 64;
-  for (int s0 = w; s0 < steps; s0 += kSkinnyWaves * kDepth) {
-    i32x4 x[kDepth][MT], y[kDepth][NT];
-#pragma unroll
-    for (int d = 0; d < kDepth; ++d) {
-      const int at = (s0 + d * kSkinnyWaves) * 64;
-      const bool in = at + 16 * g < p.K;
-#pragma unroll
-      for (int i = 0; i < NT; ++i) y[d][i] = *reinterpret_cast<const i32x4*>(in ? wp[i] + at : zeros);
-#pragma unroll
-      for (int i = 0; i < MT; ++i) x[d][i] = *reinterpret_cast<const i32x4*>(in ? ap[i] + at : zeros);
-    }
-#pragma unroll
-    for (int d = 0; d < kDepth; ++d)
-#pragma unroll
-      for (int i = 0; i < MT; ++i)
-#pragma unroll
-        for (int j = 0; j < NT; ++j)
-          acc[i][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(x[d][i], y[d][j], acc[i][j], 0, 0, 0);
-  }
-#pragma unroll
-  for (int i = 0; i < MT; ++i)
-#pragma unroll
-    for (int j = 0; j < NT; ++j)
-#pragma unroll
-      for (int e = 0; e < 4; ++e) red[w][(16 * i + 4 * g + e) * BN + 16 * j + c] = acc[i][j][e];
-  __syncthreads();
-  Out* const out = static_cast<Out*>(p.out);
-  for (int i = threadIdx.x; i < BM * BN; i += kSkinnyWaves * kWave) {
-    const int m = m0 + i / BN, n = n0 + i % BN;
-    if (m >= p.M || n >= p.N) continue;
-    int sum = 0;
-#pragma unroll
-    for (int k = 0; k < kSkinnyWaves; ++k) sum += red[k][i];
-    out[m * p.out_stride + n] = finish<Out>(sum, p.a_scale[m], p.w_scale[n], p.bias ? p.bias[n] : 0.f);
-  }
-}
-
 // 16 bytes a lane from a buffer to LDS, lane after lane from `to` on (the
-// same in every lane); zeros for an offset behind the buffer's end.
-__device__ __forceinline__ void load_to_lds(__amdgpu_buffer_rsrc_t r, int8_t* to, int offset, int uniform) {
-  typedef __attribute__((address_space(3))) void* lds_ptr;
-  __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_ptr)to, 16, offset, uniform, 0, 0);
+// same in every lane); zeros for an offset behind the buffer's end.  It has no
+// register for a result.  As assembly because the compiler, which cannot tell
+// stages apart once more than a few loads are under way, would otherwise wait
+// for all of them before every read of LDS; wait_loads() is the only wait.
+__device__ __forceinline__ void load_to_lds(i32x4 buffer, uint32_t to, int offset, int uniform) {
+  // (m0 holds nothing else in this kernel: no other instruction here reads it)
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds" ::"s"(to), "v"(offset),
+               "s"(buffer), "s"(uniform)
+               : "memory");
+}
+__device__ __forceinline__ uint32_t lds_address(const void* p) {
+  return uint32_t(reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) const void*)p));
+}
+// A buffer's descriptor in scalar registers.
+__device__ __forceinline__ i32x4 descriptor(const void* base, uint32_t bytes) {
+  const uint64_t a = reinterpret_cast<uint64_t>(base);
+  return i32x4{__builtin_amdgcn_readfirstlane(int(uint32_t(a))),
+               __builtin_amdgcn_readfirstlane(int(uint32_t(a >> 32) & 0xffffu)),
+               __builtin_amdgcn_readfirstlane(int(bytes)), kBufWord3};
 }
 
-// Many rows: tiles of BM x BN, WM x WN waves, 128 bytes of k at a time through
-// two buffers of LDS that the loads write directly while the other one is
-// worked on.  Chunk c of 16 bytes of row r lies at chunk c ^ (r & 7), so that
-// eight lanes that read eight rows hit all banks; the loads' lanes fetch in
-// that order.
-constexpr int kStep = 128;
-template <typename Out, int BM, int BN, int WM, int WN>
-__global__ __launch_bounds__(WM* WN* kWave) void k_matmul_tile(MatmulArgs p, int tiles_m, int tiles_n) {
+// All but the wave's last N loads from memory, and all its reads of LDS, are done.
+template <int N>
+__device__ __forceinline__ void wait_loads() {
+  asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(N) : "memory");
+}
+
+// Tiles of BM x BN, WM x WN waves, KB bytes of k at a time through ST stages of
+// LDS that the loads write directly, ST - 1 stages ahead of the work.  KS such
+// groups of waves take the steps in turn and add up their integers at the end.  Chunks of 16 bytes are exchanged within a row by the row's number, so
+// that eight lanes that read eight rows hit all banks; the loads' lanes fetch
+// in that order.
+template <typename Out, int BM, int BN, int WM, int WN, int KB, int ST, int KS>
+__global__ __launch_bounds__(WM* WN* KS* kWave) void k_matmul_tile(MatmulArgs p, int tiles_m, int tiles_n) {
   constexpr int kWaves = WM * WN, MT = BM / WM / 32, NT = BN / WN / 32;
-  constexpr int kLoadsA = BM / 8 / kWaves, kLoadsB = BN / 8 / kWaves;  // of 8 rows each, a wave
-  __shared__ __align__(16) int8_t a0[BM * kStep], b0[BN * kStep], a1[BM * kStep], b1[BN * kStep];
-  const int lane = __lane_id(), w = threadIdx.x / kWave, c = lane & 31, g = lane >> 5;
+  constexpr int kChunks = KB / 16, kLoadRows = kWave / kChunks;  // chunks of a row, rows of one load
+  constexpr int kLoadsA = BM / kLoadRows / kWaves, kLoadsB = BN / kLoadRows / kWaves;
+  static_assert((KB == 64 || KB == 128) && BM % (WM * 32) == 0 && BN % (WN * 32) == 0 &&
+                    BM % (kLoadRows * kWaves) == 0 && BN % (kLoadRows * kWaves) == 0, "");
+  constexpr int kStage = (BM + BN) * KB;
+  __shared__ __align__(16) int8_t lds[ST * KS * kStage];  // [ST][KS][rows of a, then of w][KB]
+  const int lane = __lane_id(), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+  const int w = wave % kWaves, group = wave / kWaves, c = lane & 31, g = lane >> 5;
+  auto exchange = [](int row) { return KB == 128 ? row & 7 : (row >> 1) & 3; };
 
   // Workgroups go to the XCDs in turn: each XCD gets a run of tiles that lie
   // together (columns of 8 row tiles), whose rows and weights its L2 holds.
@@ -199,106 +171,199 @@ __global__ __launch_bounds__(WM* WN* kWave) void k_matmul_tile(MatmulArgs p, int
 
   // a row behind the last one is behind its buffer's end and reads as zeros;
   // so is, by its offset, what lies behind the end of a row
-  const int lr = lane / 8, lc = 16 * ((lane % 8) ^ lr);  // row of the eight and byte that this lane fetches
-  const __amdgpu_buffer_rsrc_t abuf = make_rsrc(p.a + int64_t(m0) * p.a_stride, min(BM, p.M - m0) * int(p.a_stride));
-  const __amdgpu_buffer_rsrc_t bbuf = make_rsrc(p.w + int64_t(n0) * p.w_stride, min(BN, p.N - n0) * int(p.w_stride));
+  const int lr = lane / kChunks, lc = 16 * ((lane % kChunks) ^ exchange(lr));  // this lane's row and byte of a load
+  i32x4 abuf = descriptor(p.a + int64_t(m0) * p.a_stride, min(BM, p.M - m0) * int(p.a_stride));
+  i32x4 bbuf = descriptor(p.w + int64_t(n0) * p.w_stride, min(BN, p.N - n0) * int(p.w_stride));
+  // a scalar register that the vector unit wrote may be a load's descriptor
+  // five instructions later; the compiler does not look into the assembly
+  asm volatile("s_nop 4" : "+s"(abuf), "+s"(bbuf));
   int ao[kLoadsA], bo[kLoadsB];
 #pragma unroll
-  for (int i = 0; i < kLoadsA; ++i) ao[i] = ((w * kLoadsA + i) * 8 + lr) * int(p.a_stride) + lc;
+  for (int i = 0; i < kLoadsA; ++i) ao[i] = ((w * kLoadsA + i) * kLoadRows + lr) * int(p.a_stride) + lc;
 #pragma unroll
-  for (int i = 0; i < kLoadsB; ++i) bo[i] = ((w * kLoadsB + i) * 8 + lr) * int(p.w_stride) + lc;
-  auto fetch = [&](int8_t* a, int8_t* b, int k) {
+  for (int i = 0; i < kLoadsB; ++i) bo[i] = ((w * kLoadsB + i) * kLoadRows + lr) * int(p.w_stride) + lc;
+  const uint32_t base = lds_address(lds) + group * kStage;
+  auto fetch = [&](int i, int s) {  // step s to stage i
+    const int k = (s * KS + group) * KB;
     const bool in = k + lc < p.K;
+    const uint32_t to = base + i * KS * kStage;
 #pragma unroll
-    for (int i = 0; i < kLoadsA; ++i)
-      load_to_lds(abuf, a + (w * kLoadsA + i) * 8 * kStep, in ? ao[i] : kOOB, k);
+    for (int x = 0; x < kLoadsA; ++x) load_to_lds(abuf, to + (w * kLoadsA + x) * 1024, in ? ao[x] : kOOB, k);
 #pragma unroll
-    for (int i = 0; i < kLoadsB; ++i)
-      load_to_lds(bbuf, b + (w * kLoadsB + i) * 8 * kStep, in ? bo[i] : kOOB, k);
-    // the loads go out before the work that hides them
-    __builtin_amdgcn_sched_barrier(0);
+    for (int x = 0; x < kLoadsB; ++x) load_to_lds(bbuf, to + BM * KB + (w * kLoadsB + x) * 1024, in ? bo[x] : kOOB, k);
   };
 
   i32x16 acc[MT][NT] = {};
-  const int ra = (w / WN) * (BM / WM) + c, rb = (w % WN) * (BN / WN) + c;
-  auto work = [&](const int8_t* a, const int8_t* b) {
+  const int ra = (w / WN) * (BM / WM) + c, rb = (w % WN) * (BN / WN) + c, ex = exchange(c);
+  // Two sets of fragments: one is read while the products of the other run.
+  struct Set {
+    i32x4 x[MT], y[NT];
+  } even, odd;
+  auto read = [&](const int8_t* a, int k, Set& f) {
 #pragma unroll
-    for (int k = 0; k < kStep / 32; ++k) {
-      i32x4 x[MT], y[NT];
+    for (int i = 0; i < MT; ++i)
+      f.x[i] = *reinterpret_cast<const i32x4*>(a + (ra + 32 * i) * KB + 16 * ((2 * k + g) ^ ex));
 #pragma unroll
-      for (int i = 0; i < MT; ++i)
-        x[i] = *reinterpret_cast<const i32x4*>(a + (ra + 32 * i) * kStep + 16 * ((2 * k + g) ^ (c & 7)));
-#pragma unroll
-      for (int j = 0; j < NT; ++j)
-        y[j] = *reinterpret_cast<const i32x4*>(b + (rb + 32 * j) * kStep + 16 * ((2 * k + g) ^ (c & 7)));
-#pragma unroll
-      for (int i = 0; i < MT; ++i)
-#pragma unroll
-        for (int j = 0; j < NT; ++j) acc[i][j] = __builtin_amdgcn_mfma_i32_32x32x32_i8(x[i], y[j], acc[i][j], 0, 0, 0);
-    }
+    for (int j = 0; j < NT; ++j)
+      f.y[j] = *reinterpret_cast<const i32x4*>(a + BM * KB + (rb + 32 * j) * KB + 16 * ((2 * k + g) ^ ex));
+    __builtin_amdgcn_sched_barrier(0);
   };
-  // the buffer that is waited for is complete in every wave, and the other one
-  // is no longer read, behind this
-  auto ready = [] {
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    __syncthreads();
-  };
-
-  const int steps = (p.K + kStep - 1) / kStep;
-  fetch(a0, b0, 0);
-  for (int s = 0; s + 1 < steps; s += 2) {
-    ready();
-    fetch(a1, b1, (s + 1) * kStep);
-    work(a0, b0);
-    ready();
-    fetch(a0, b0, (s + 2) * kStep);  // behind the last step: zeros, from no memory
-    work(a1, b1);
-  }
-  if (steps % 2) {
-    ready();
-    work(a0, b0);
-  }
-
-  Out* const out = static_cast<Out*>(p.out);
-#pragma unroll
-  for (int j = 0; j < NT; ++j) {
-    const int n = n0 + rb + 32 * j;
-    const bool in = n < p.N;
-    const float sw = in ? p.w_scale[n] : 0.f, bias = in && p.bias ? p.bias[n] : 0.f;
+  auto multiply = [&](const Set& f) {
 #pragma unroll
     for (int i = 0; i < MT; ++i)
 #pragma unroll
-      for (int e = 0; e < 16; ++e) {
-        const int m = m0 + ra - c + 32 * i + 8 * (e / 4) + 4 * g + e % 4;
-        if (in && m < p.M) out[m * p.out_stride + n] = finish<Out>(acc[i][j][e], p.a_scale[m], sw, bias);
+      for (int j = 0; j < NT; ++j)
+        acc[i][j] = __builtin_amdgcn_mfma_i32_32x32x32_i8(f.y[j], f.x[i], acc[i][j], 0, 0, 0);
+    __builtin_amdgcn_sched_barrier(0);
+  };
+  // Step s, in stage `now`: behind the barrier its loads, which every wave waits
+  // for, are complete, and the stage that the next loads go to (step s - 1's) is
+  // no longer read: its last fragments are in registers, and their products
+  // hide this step's first reads.  Behind the last step the loads are of
+  // zeros, from no memory.
+  const int steps = (p.K + KB * KS - 1) / (KB * KS);
+#pragma unroll
+  for (int i = 0; i < MT; ++i) odd.x[i] = i32x4{};  // the first products of all are of zeros
+#pragma unroll
+  for (int j = 0; j < NT; ++j) odd.y[j] = i32x4{};
+#pragma unroll
+  for (int i = 0; i < ST - 1; ++i) fetch(i, i);
+  auto step = [&](int s, int now, int next) {
+    wait_loads<(ST - 2) * (kLoadsA + kLoadsB)>();
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+    fetch(next, s + ST - 1);
+    const int8_t* const at = lds + (now * KS + group) * kStage;
+#pragma unroll
+    for (int k = 0; k < KB / 32; k += 2) {
+      read(at, k, even);
+      multiply(odd);
+      read(at, k + 1, odd);
+      multiply(even);
+    }
+  };
+  int s = 0;
+  for (; s + ST <= steps; s += ST) {  // (with its stages known, a step's addresses need no arithmetic)
+#pragma unroll
+    for (int i = 0; i < ST; ++i) step(s + i, i, (i + ST - 1) % ST);
+  }
+  for (int i = 0; s + i < steps; ++i) step(s + i, i, i == 0 ? ST - 1 : i - 1);
+  multiply(odd);
+  wait_loads<0>();  // no load may write LDS behind the workgroup's end
+
+  // The weights are the left operand, so a lane has four columns of one row
+  // together.  A wave turns units of 32 rows by 128 bytes in LDS and stores
+  // them 16 bytes a lane, whole lines of the result (or half lines).
+  constexpr int kUnitBytes = kWaves * 32 * 128 <= (BM + BN) * KB && BN / WN * sizeof(Out) >= 128 ? 128 : 64;
+  constexpr int kUnit = kUnitBytes / sizeof(Out);  // columns of a unit
+  constexpr int kUnitChunks = kUnit * sizeof(Out) / 16, kPer = 16 / sizeof(Out);    // 16-byte chunks of its row, elements of one
+  static_assert(kWaves * 32 * kUnit * sizeof(Out) <= (BM + BN) * KB, "");
+  Out* const out = static_cast<Out*>(p.out);
+  Out* const unit = reinterpret_cast<Out*>(lds) + w * 32 * kUnit;
+  auto place = [&](int row, int chunk) {
+    return unit + row * kUnit + kPer * (chunk ^ (kUnitChunks == 8 ? row & 7 : (row >> 1) & (kUnitChunks - 1)));
+  };
+  float* const wsc = reinterpret_cast<float*>(lds + KS * kStage);  // [BN] scales, [BN] biases
+  const int mw = m0 + (w / WN) * (BM / WM), nt = (w % WN) * (BN / WN);
+  __syncthreads();  // no wave reads its stages any more
+  if constexpr (KS > 1) {
+    static_assert((KS - 1) * kWaves * MT * NT * 4096 <= KS * kStage, "");
+    i32x4* const sums = reinterpret_cast<i32x4*>(lds + KS * kStage) + w * (MT * NT * 4 * kWave) + lane;
+    auto each = [&](auto f) {
+#pragma unroll
+      for (int i = 0; i < MT; ++i)
+#pragma unroll
+        for (int j = 0; j < NT; ++j)
+#pragma unroll
+          for (int q = 0; q < 4; ++q) f(acc[i][j], q, ((i * NT + j) * 4 + q) * kWave);
+    };
+    if (group > 0)
+      each([&](i32x16& x, int q, int at) {
+        sums[(group - 1) * kWaves * MT * NT * 4 * kWave + at] = i32x4{x[4 * q], x[4 * q + 1], x[4 * q + 2], x[4 * q + 3]};
+      });
+    __syncthreads();
+    if (group == 0)
+      for (int k = 0; k < KS - 1; ++k)
+        each([&](i32x16& x, int q, int at) {
+          const i32x4 y = sums[k * kWaves * MT * NT * 4 * kWave + at];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) x[4 * q + e] += y[e];
+        });
+    __syncthreads();
+  }
+  for (int i = threadIdx.x; i < BN; i += KS * kWaves * kWave) {
+    const int n = min(n0 + i, p.N - 1);
+    wsc[i] = p.w_scale[n], wsc[BN + i] = p.bias ? p.bias[n] : 0.f;
+  }
+  __syncthreads();
+  if (group > 0) return;
+#pragma unroll
+  for (int i = 0; i < MT; ++i) {
+    const float sa = mw + 32 * i + c < p.M ? p.a_scale[mw + 32 * i + c] : 0.f;
+#pragma unroll
+    for (int u = 0; u < BN / WN; u += kUnit) {
+#pragma unroll
+      for (int col = 0; col < kUnit; col += 8) {
+        const int j = (u + col) / 32, q = (u + col) % 32 / 8;
+        const f32x4 sw = *reinterpret_cast<const f32x4*>(wsc + nt + u + col + 4 * g);
+        const f32x4 bias = *reinterpret_cast<const f32x4*>(wsc + BN + nt + u + col + 4 * g);
+        Out y[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) y[e] = finish<Out>(acc[i][j][4 * q + e], sa, sw[e], bias[e]);
+        Out* to = place(c, (col + 4 * g) / kPer) + (col + 4 * g) % kPer;
+        if constexpr (sizeof(Out) == 2) *reinterpret_cast<u32x2*>(to) = u32x2{y[0] | uint32_t(y[1]) << 16, y[2] | uint32_t(y[3]) << 16};
+        else *reinterpret_cast<f32x4*>(to) = f32x4{y[0], y[1], y[2], y[3]};
       }
+      // rows of the result may start at any element: stores of 16 bytes that
+      // need no more than its alignment
+      typedef std::conditional_t<sizeof(Out) == 2, u32x4_of_2, u32x4_of_4> loose;
+      const int rows = min(32, p.M - (mw + 32 * i)), cols = min(kUnit, p.N - (n0 + nt + u));
+      Out* const to = out + int64_t(mw + 32 * i) * p.out_stride + n0 + nt + u;
+#pragma unroll
+      for (int x = 0; x < 32 * kUnitChunks; x += kWave) {
+        const int row = (x + lane) / kUnitChunks, chunk = (x + lane) % kUnitChunks;
+        const u32x4 v = *reinterpret_cast<const u32x4*>(place(row, chunk));
+        Out* const at = to + row * p.out_stride + kPer * chunk;
+        if (row < rows && kPer * chunk + kPer <= cols) {
+          *reinterpret_cast<loose*>(at) = v;
+        } else if (row < rows) {
+          for (int e = 0; e < cols - kPer * chunk; ++e) at[e] = place(row, chunk)[e];
+        }
+      }
+    }
   }
 }
 
-template <typename Out, int BM, int BN, int WM, int WN>
+template <typename Out, int BM, int BN, int WM, int WN, int KB, int ST, int KS>
 hipError_t tiles(const MatmulArgs& p, hipStream_t s) {
   const int64_t tm = (p.M + BM - 1) / BM, tn = (int64_t(p.N) + BN - 1) / BN;
   const int64_t groups = (tm * tn + kXcds - 1) / kXcds * kXcds;
   if (groups > 0x7fffffff) return hipErrorInvalidValue;
-  hipLaunchKernelGGL((k_matmul_tile<Out, BM, BN, WM, WN>), dim3(uint32_t(groups)), dim3(WM * WN * kWave), 0, s, p,
-                     int(tm), int(tn));
+  hipLaunchKernelGGL((k_matmul_tile<Out, BM, BN, WM, WN, KB, ST, KS>), dim3(uint32_t(groups)), dim3(WM * WN * KS * kWave),
+                     0, s, p, int(tm), int(tn));
   return hipGetLastError();
 }
-template <typename Out, int MT, int NT>
-hipError_t skinny(const MatmulArgs& p, hipStream_t s) {
-  hipLaunchKernelGGL((k_matmul_skinny<Out, MT, NT>), dim3((p.N + 16 * NT - 1) / (16 * NT), (p.M + 16 * MT - 1) / (16 * MT)),
-                     dim3(kSkinnyWaves * kWave), 0, s, p);
-  return hipGetLastError();
-}
+// The tile by the time of a product with K = 3584, measured (us; other K scale
+// all alike): a CU works on one 256 x 256 tile in 46, one of 192 x 128 in 26, two
+// of 128 x 128 together in 29 and one alone in 18, one of 64 x 64 in 6.4.  Large
+// tiles read LDS less for the same products, small ones fill the chip.  Where
+// even these are too few for the CUs, four groups of waves share the steps of
+// a 32 x 32 tile (M <= 32: 6.3 us for 4608 columns, a 64 x 64 tile 8.8), or two
+// those of a 64 x 32 tile (M <= 64: 7.5 against 9.2).
 template <typename Out>
 hipError_t matmul(const MatmulArgs& p, hipStream_t s) {
-  if (p.M <= 16) return skinny<Out, 1, 1>(p, s);
-  if (p.M <= 32) return skinny<Out, 2, 1>(p, s);
-  if (p.M <= 64) return skinny<Out, 4, 1>(p, s);
-  if (p.M <= 256) return skinny<Out, 4, 2>(p, s);
-  const int64_t big = int64_t((p.M + 255) / 256) * ((p.N + 255) / 256);
-  if (big >= 2 * kCUs) return tiles<Out, 256, 256, 2, 4>(p, s);
-  return tiles<Out, 128, 128, 2, 2>(p, s);
+  auto count = [&](int bm, int bn) { return (int64_t(p.M) + bm - 1) / bm * ((int64_t(p.N) + bn - 1) / bn); };
+  auto turns = [&](int bm, int bn) { return double((count(bm, bn) + kCUs - 1) / kCUs); };
+  if (p.M <= 32 && count(32, 32) <= kCUs) return tiles<Out, 32, 32, 1, 1, 128, 4, 4>(p, s);
+  if (p.M <= 64 && count(64, 32) <= kCUs) return tiles<Out, 64, 32, 2, 1, 128, 3, 2>(p, s);
+  const double n128 = turns(128, 128);
+  const double t256 = 46 * turns(256, 256), t192 = 26 * turns(192, 128);
+  const double t128 = 29 * std::floor(n128 / 2) + 18 * std::fmod(n128, 2), t64 = 6.4 * turns(64, 64);
+  const double best = std::min({t256, t192, t128, t64});
+  if (best == t64) return tiles<Out, 64, 64, 2, 2, 128, 4, 1>(p, s);
+  if (best == t128) return tiles<Out, 128, 128, 2, 2, 128, 2, 1>(p, s);
+  if (best == t192) return tiles<Out, 192, 128, 2, 4, 128, 2, 1>(p, s);
+  return tiles<Out, 256, 256, 2, 4, 128, 2, 1>(p, s);
 }
 
 }  // namespace

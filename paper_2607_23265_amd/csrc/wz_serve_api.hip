@@ -170,7 +170,7 @@ wz_status wz_matmul_int(const int8_t* a, int64_t a_stride, const float* a_scale,
   if (M == 0) return WZ_OK;
   WZ_TRY(check_rows(a, a_stride, K));
   WZ_TRY(check_rows(w, w_stride, K));
-  if (a_stride % 16 != 0 || w_stride % 16 != 0 || out_stride < N || out_stride > (int64_t(1) << 40))
+  if (a_stride % 16 != 0 || w_stride % 16 != 0 || a_stride > (1 << 22) || w_stride > (1 << 22) || out_stride < N || out_stride > (int64_t(1) << 40))
     return WZ_ERR_SHAPE;
   WZ_TRY(check_ptr(a_scale, 4));
   WZ_TRY(check_ptr(w_scale, 4));

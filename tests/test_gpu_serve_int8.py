@@ -48,7 +48,9 @@ def test_quantize(rows, cols, dtype):
 
 SHAPES = [(1, 1, 16), (1, 100, 48), (2, 17, 3584), (16, 64, 64), (31, 33, 80), (64, 4608, 3584), (65, 130, 1040),
           (17, 1000, 8192), (128, 128, 128), (130, 257, 3600), (200, 515, 272), (300, 640, 16), (1286, 384, 1152),
-          (513, 769, 2064), (256, 256, 65536), (1, 16384, 256), (90, 2048, 4096), (700, 3584, 560)]
+          (513, 769, 2064), (256, 256, 65536), (1, 16384, 256), (90, 2048, 4096), (700, 3584, 560),
+          # one for each tile the product is done in, with ragged edges
+          (31, 4600, 1104), (63, 4601, 1168), (33, 9000, 144), (391, 2040, 528), (1286, 4600, 48), (2499, 4601, 144)]
 
 
 @pytest.mark.parametrize("M,N,K", SHAPES)

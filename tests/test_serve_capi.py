@@ -184,6 +184,7 @@ def test_int8_arguments(L):
         return L.wz_matmul_int(a, as_, sa, w, ws, sw, b, M, N, K, o, os_, dtype, None)
     assert mul(dtype=5) == DTYPE and mul(M=-1) == SHAPE and mul(N=0) == SHAPE and mul(K=20) == SHAPE
     assert mul(as_=48) == SHAPE and mul(ws=72) == SHAPE and mul(os_=4) == SHAPE and mul(K=65552, as_=70000) == SHAPE
+    assert mul(as_=(1 << 22) + 16) == SHAPE and mul(ws=(1 << 22) + 16) == SHAPE
     assert mul(a=None) == NULL and mul(w=AT + 8) == ALIGN and mul(sa=None) == NULL and mul(sw=AT + 2) == ALIGN
     assert mul(b=AT + 2) == ALIGN and mul(o=None) == NULL and mul(o=AT + 1) == ALIGN
 
