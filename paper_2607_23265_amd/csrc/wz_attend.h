@@ -1,12 +1,15 @@
-// How the attention kernels share out a ragged batch: row blocks and, where
-// there are few of them, runs of tokens of each block.
+// How the attention kernels share out a ragged batch.
 //
 // The rows of sequence b under one key/value head are its new tokens times
 // the head's group of query heads, token by token: row i * G + g.  They fall
-// into blocks of BR rows.  A block's tokens are worked on in tiles of 64; in a
-// shared plan a block's tiles are split into runs of `chunk` tiles, an item
-// each, where chunk follows from the whole batch's tiles, so that a long
-// sequence gets more workgroups than a short one and all finish together.
+// into blocks of BR rows; a block's tokens are worked on in tiles of 64.
+//
+// Where blocks are few or long they are shared: all blocks' tiles, one block
+// behind the other, are cut into equal runs, one for each workgroup (for
+// each key/value head), so that a long sequence gets more workgroups than a
+// short one and all finish together.  A workgroup leaves a part of every
+// block that it does not have to itself in slot (its number + the block's),
+// and a second kernel adds a block's parts up in order.
 #pragma once
 
 #include "wz_serve.h"
@@ -14,7 +17,7 @@
 namespace wz {
 
 constexpr int kTile = 64;       // tokens of a tile
-constexpr int kMinChunk = 4;    // tiles: an item is at least this long where blocks are shared
+constexpr int kMinRun = 4;      // tiles of a workgroup's run at least
 
 struct Block {
   int rows, r0;            // rows of the sequence, first row of the block
@@ -22,48 +25,22 @@ struct Block {
   int full_lo, full_hi;    // places that every one of its rows sees
 };
 
+// A place in the shared plan: tile `off` of the `tiles` that block k of
+// sequence seq has; `block` blocks and `before` tiles lie in front of that one.
+struct Spot {
+  int seq, k, off, tiles, block, before;
+};
+
 template <int BR>
 struct Partition {
   const AttendArgs& a;
-  int G, chunk;
+  int G;
+  int total, run;  // shared: tiles of all blocks, and of a workgroup's run
 
-  __device__ __forceinline__ int rows(const Seq& s) const { return s.n * G; }
-  __device__ __forceinline__ int blocks(const Seq& s) const { return (rows(s) + BR - 1) / BR; }
-  // tiles that a block of the sequence spans at most
-  __device__ __forceinline__ int tiles(const Seq& s) const {
-    const int all = (s.kv + kTile - 1) / kTile;
-    if (!(a.causal && a.window > 0)) return all;
-    const int64_t span = int64_t(a.window) + (BR - 1) / G + 1;
-    return int(min(int64_t(all), (span + kTile - 1) / kTile + 1));
-  }
-  __device__ __forceinline__ int splits(const Seq& s) const {
-    return a.shared ? max(1, (tiles(s) + chunk - 1) / chunk) : 1;
-  }
-  __device__ __forceinline__ int items(int b) const {
-    const Seq s = sequence(a.batch, b);
-    return blocks(s) * splits(s);
-  }
-  // The same in every workgroup: the tiles of all blocks over the items that
-  // are meant for them; the host's bound on slots leaves one more a block.
-  __device__ __forceinline__ Partition(const AttendArgs& args, int blocks_bound)
-      : a(args), G(args.q_heads / args.cache.kv_heads), chunk(1 << 30) {
-    if (!a.shared) return;
-    double total = 0;
-    for (int b0 = 0; b0 < a.batch.batch; b0 += kWave) {
-      const int b = b0 + __lane_id();
-      if (b < a.batch.batch) {
-        const Seq s = sequence(a.batch, b);
-        total += double(blocks(s)) * tiles(s);
-      }
-    }
-    total = wave_reduce_f64(total, [](double x, double y) { return x + y; });
-    const int meant = max(a.slots - blocks_bound, 1);
-    const double c = ceil(total / meant);
-    chunk = c < (1 << 24) ? max(int(c), kMinChunk) : (1 << 24);
-  }
+  __device__ __forceinline__ int blocks(const Seq& s) const { return (s.n * G + BR - 1) / BR; }
   __device__ __forceinline__ Block block(const Seq& s, int k) const {
     Block x;
-    x.rows = rows(s);
+    x.rows = s.n * G;
     x.r0 = k * BR;
     const int first = s.place0 + x.r0 / G, last = s.place0 + (min(x.r0 + BR, x.rows) - 1) / G;
     x.hi = a.causal ? min(last + 1, s.kv) : s.kv;
@@ -71,6 +48,100 @@ struct Partition {
     x.lo = a.causal && a.window > 0 ? max(0, first - a.window + 1) : 0;
     x.full_lo = a.causal && a.window > 0 ? max(0, last - a.window + 1) : 0;
     return x;
+  }
+  // The tiles of a block: one if it sees nothing, since its rows have to be
+  // written.  With few rows to a block (the token kernel) all blocks of a
+  // sequence count as many as the widest may span, so that the sequence's sum
+  // is a product.
+  static constexpr bool kUniform = BR <= 64;
+  __device__ __forceinline__ int tiles(const Seq& s, int k) const {
+    if constexpr (kUniform) {
+      const int all = max(1, (s.kv + kTile - 1) / kTile);
+      if (!(a.causal && a.window > 0)) return all;
+      const int64_t span = int64_t(a.window) + (BR - 1) / G + 1;
+      return int(min(int64_t(all), (span + kTile - 1) / kTile + 1));
+    } else {
+      const Block x = block(s, k);
+      return max(1, (x.hi + kTile - 1) / kTile - x.lo / kTile);
+    }
+  }
+  // The first block whose running count of blocks (TILES: of tiles) passes
+  // `at`; false if none does, with the counts of all blocks.
+  template <bool TILES>
+  __device__ __forceinline__ bool find(int at, Spot* spot) const {
+    const int lane = __lane_id();
+    int nb = 0, nt = 0;
+    for (int b0 = 0; b0 < a.batch.batch; b0 += kWave) {
+      const bool in = b0 + lane < a.batch.batch;
+      const Seq s = in ? sequence(a.batch, b0 + lane) : Seq{0, 0, 0, 0};
+      const int mine = blocks(s);
+      if constexpr (kUniform) {
+        const int each = tiles(s, 0), work = mine * each;
+        const int ib = wave_incl_scan_i32(mine), it = wave_incl_scan_i32(work);
+        const unsigned long long pass = __ballot(TILES ? nt + it > at : nb + ib > at);
+        if (pass) {
+          const int l = __builtin_ctzll(pass);
+          const int b1 = nb + __builtin_amdgcn_readlane(ib - mine, l), t1 = nt + __builtin_amdgcn_readlane(it - work, l);
+          const int n = __builtin_amdgcn_readlane(each, l);
+          const int k = TILES ? (at - t1) / n : at - b1;
+          *spot = Spot{b0 + l, k, TILES ? (at - t1) % n : 0, n, b1 + k, t1 + k * n};
+          return true;
+        }
+        nb += __builtin_amdgcn_readlane(ib, kWave - 1), nt += __builtin_amdgcn_readlane(it, kWave - 1);
+      } else {
+        for (unsigned long long left = __ballot(mine > 0); left; left &= left - 1) {
+          const int l = __builtin_ctzll(left);
+          const Seq one{__builtin_amdgcn_readlane(s.start, l), __builtin_amdgcn_readlane(s.n, l),
+                        __builtin_amdgcn_readlane(s.kv, l), __builtin_amdgcn_readlane(s.place0, l)};
+          const int count = blocks(one);
+          if (!TILES && at >= nb + count && !a.shared) {  // (tiles are not needed)
+            nb += count;
+            continue;
+          }
+          for (int k0 = 0; k0 < count; k0 += kWave) {
+            const int n = k0 + lane < count ? tiles(one, k0 + lane) : 0;
+            const int it = wave_incl_scan_i32(n);
+            const unsigned long long pass = __ballot(n > 0 && (TILES ? nt + it > at : nb + k0 + lane + 1 > at));
+            if (pass) {
+              const int i = __builtin_ctzll(pass), t1 = nt + __builtin_amdgcn_readlane(it - n, i);
+              *spot = Spot{b0 + l, k0 + i, TILES ? at - t1 : 0, __builtin_amdgcn_readlane(n, i), nb + k0 + i, t1};
+              return true;
+            }
+            nt += __builtin_amdgcn_readlane(it, kWave - 1);
+          }
+          nb += count;
+        }
+      }
+    }
+    spot->block = nb, spot->before = nt;
+    return false;
+  }
+  // (the host shares only where the tiles of all blocks fit in an int)
+  __device__ __forceinline__ Partition(const AttendArgs& args)
+      : a(args), G(args.q_heads / args.cache.kv_heads), total(0), run(0) {
+    if (!a.shared) return;
+    Spot all;
+    find<true>(0x7fffffff, &all);
+    total = all.before;
+    run = max((total + a.workers - 1) / a.workers, kMinRun);
+  }
+  // Calls f(seq, k, off, count, slot) for every piece of a block that workgroup
+  // `me` has; slot is where its part goes, -1 if the block is all its own.
+  template <typename F>
+  __device__ __forceinline__ void each_piece(int me, F f) const {
+    Spot x;
+    if (!a.shared) {
+      if (find<false>(me, &x)) f(x.seq, x.k, 0, x.tiles, -1);
+      return;
+    }
+    int at = me * run;
+    const int end = min(at + run, total);
+    while (at < end && find<true>(at, &x)) {
+      const int count = min(end - at, x.tiles - x.off);
+      f(x.seq, x.k, x.off, count, count == x.tiles ? -1 : me + x.block);
+      at += count;
+      if (at < end) __syncthreads();  // LDS is used again
+    }
   }
 };
 

@@ -28,22 +28,25 @@ constexpr int kThreads = kWaves * kWave;
 constexpr int kRows = 32 * kWaves;
 
 template <int D>
-__global__ __launch_bounds__(kThreads, 2) void k_attend_prompt(AttendArgs a, int blocks_bound) {
+struct Stages {
+  __bf16 k[2][kTile * D];  // [row of a product][D]
+  __bf16 v[2][D * kTile];  // [channel][token]
+};
+
+// Tiles [off, off + count) of block kb of sequence b, key/value head h; slot:
+// where its part goes, -1 if the block is this workgroup's alone.
+template <int D>
+__device__ __forceinline__ void attend_block(const AttendArgs& a, const Partition<kRows>& part, int h, int b, int kb,
+                                             int off, int count, int slot, Stages<D>& lds) {
   constexpr int KK = D / 16, DT = D / 32;
   constexpr int kKeyPieces = kTile * (D / 16) / kThreads, kValPieces = D * (kTile / 16) / kThreads;
-  __shared__ __align__(16) __bf16 kt[2][kTile * D];  // [row of a product][D]
-  __shared__ __align__(16) __bf16 vt[2][D * kTile];  // [channel][token]
-
-  const int Hkv = a.cache.kv_heads, h = blockIdx.x % Hkv, item = blockIdx.x / Hkv;
-  const Partition<kRows> part(a, blocks_bound);
-  int b, local;
-  if (!find_item(a.batch.batch, item, [&](int i) { return part.items(i); }, &b, &local)) return;
+  auto& kt = lds.k;
+  auto& vt = lds.v;
+  const int Hkv = a.cache.kv_heads, G = part.G;
   const Seq s = sequence(a.batch, b);
-  const int splits = part.splits(s), G = part.G;
-  const int nblocks = part.blocks(s);
-  const Block blk = part.block(s, nblocks - 1 - local / splits);  // the longest first
-  const int T0 = blk.lo / kTile + local % splits * part.chunk;
-  const int T1 = min((max(blk.hi, blk.lo) + kTile - 1) / kTile, splits > 1 ? T0 + part.chunk : 1 << 24);
+  const Block blk = part.block(s, kb);
+  const int T0 = blk.lo / kTile + off;
+  const int T1 = min((max(blk.hi, blk.lo) + kTile - 1) / kTile, T0 + count);
 
   const int tid = threadIdx.x, lane = __lane_id(), w = tid / kWave, c = lane & 31, g = lane >> 5;
   const int P = a.cache.page_size, logP = __builtin_ctz(P);
@@ -67,44 +70,54 @@ __global__ __launch_bounds__(kThreads, 2) void k_attend_prompt(AttendArgs a, int
   for (int d = 0; d < DT; ++d) o[d] = f32x16{};
   float m = -INFINITY, l = 0.f;
 
-  // staging: this thread's pieces of a tile, 16 codes each
-  auto page = [&](int tile, int blk16) {
-    const int tok = tile * kTile + 16 * blk16;
-    return tile < T1 && tok < s.kv ? page_of(a.batch, a.cache.pages, b, tok >> logP) : -1;
-  };
+  // Staging: this thread's pieces of a tile, 16 codes each.  Nothing branches
+  // around a load: what lies behind the last tile is the last tile again, and a
+  // block of 16 tokens that has no page reads page 0 and is masked.
   u32x4 kx[kKeyPieces], vx[kValPieces];
   float ks[kKeyPieces], vs;
-  int kp[kKeyPieces], vp;
-  auto pages = [&](int tile) {
-#pragma unroll
-    for (int i = 0; i < kKeyPieces; ++i) kp[i] = page(tile, (tid + i * kThreads) / (D / 16) / 16);
-    vp = page(tile, tid % 4);
-  };
   uint32_t in_next = 0;  // bit k: tokens 16 k .. of the tile loaded last lie in pages of the cache
-  auto load = [&](int tile) {
-    in_next = uint32_t(__ballot(vp >= 0)) & 0xfu;
+  struct Pages {
+    int k[kKeyPieces], v;
+  } ids;
+  const int* const row_of = a.batch.table + int64_t(b) * a.batch.table_stride;
+  const int entries = max((s.kv + P - 1) >> logP, 1);
+  auto pages = [&](int tile) {
+    const int tok = min(tile, T1 - 1) * kTile;
+    Pages x;
+#pragma unroll
+    for (int i = 0; i < kKeyPieces; ++i)
+      x.k[i] = row_of[min((tok + (tid + i * kThreads) / (D / 16) / 16 * 16) >> logP, entries - 1)];
+    x.v = row_of[min((tok + 16 * (tid % 4)) >> logP, entries - 1)];
+    return x;
+  };
+  auto load = [&](int tile, const Pages& id) {
+    const int first = tile * kTile;
+    const bool vin = uint32_t(id.v) < uint32_t(a.cache.pages);
+    in_next = uint32_t(__ballot(vin)) & 0xfu;
 #pragma unroll
     for (int i = 0; i < kKeyPieces; ++i) {
       const int p = tid + i * kThreads, tok = p / (D / 16), part16 = p % (D / 16);
-      const int64_t at = int64_t(max(kp[i], 0)) * Hkv + h;
-      kx[i] = *reinterpret_cast<const u32x4*>(kc + at * (P * D) + ((tile * kTile + tok) & (P - 1)) * D + 16 * part16);
+      const int64_t at = int64_t(uint32_t(id.k[i]) < uint32_t(a.cache.pages) ? id.k[i] : 0) * Hkv + h;
+      kx[i] = *reinterpret_cast<const u32x4*>(kc + at * (P * D) + ((first + tok) & (P - 1)) * D + 16 * part16);
       ks[i] = a.cache.k_scale[at];
     }
-    const int64_t at = int64_t(max(vp, 0)) * Hkv + h;
-    vs = vp < 0 ? 1.f : a.cache.v_scale[at];
+    const int64_t at = int64_t(vin ? id.v : 0) * Hkv + h;
+    const float scale = a.cache.v_scale[at];
+    vs = vin ? scale : 1.f;
 #pragma unroll
     for (int i = 0; i < kValPieces; ++i) {
       const int p = tid + i * kThreads, d = p / 4;
-      vx[i] = *reinterpret_cast<const u32x4*>(vc + at * (P * D) + d * P + ((tile * kTile + 16 * (p % 4)) & (P - 1)));
+      vx[i] = *reinterpret_cast<const u32x4*>(vc + at * (P * D) + d * P + ((first + 16 * (p % 4)) & (P - 1)));
     }
+    __builtin_amdgcn_sched_barrier(0);
+  };
+  auto store = [&](int buf, int tile) {
     // values behind the sequence's end may be any bytes and must be zeros
-    const int count = vp < 0 ? 0 : min(max(s.kv - (tile * kTile + 16 * (tid % 4)), 0), 16);
-    if (count < 16) {
+    if (tile * kTile + kTile > s.kv || in_next != 0xfu) {
+      const int count = in_next >> (tid % 4) & 1u ? min(max(s.kv - (tile * kTile + 16 * (tid % 4)), 0), 16) : 0;
 #pragma unroll
       for (int i = 0; i < kValPieces; ++i) vx[i] = first_codes(vx[i], count);
     }
-  };
-  auto store = [&](int buf) {
 #pragma unroll
     for (int i = 0; i < kKeyPieces; ++i) {
       const int p = tid + i * kThreads, tok = p / (D / 16), part16 = p % (D / 16);
@@ -122,20 +135,22 @@ __global__ __launch_bounds__(kThreads, 2) void k_attend_prompt(AttendArgs a, int
     }
   };
 
+  uint32_t in = 0;
   if (T0 < T1) {
-    pages(T0);
-    load(T0);
-    pages(T0 + 1);
-    store(0);
+    const Pages now = pages(T0);
+    ids = pages(T0 + 1);
+    load(T0, now);
+    in = in_next;
+    store(0, T0);
   }
   for (int tile = T0; tile < T1; ++tile) {
     const int buf = (tile - T0) & 1;
     __syncthreads();
     const bool more = tile + 1 < T1;
-    const uint32_t in = in_next;
     if (more) {
-      load(tile + 1);
-      pages(tile + 2);
+      const Pages now = ids;
+      ids = pages(tile + 2);
+      load(tile + 1, now);
     }
     f32x16 sc[2];
 #pragma unroll
@@ -148,19 +163,22 @@ __global__ __launch_bounds__(kThreads, 2) void k_attend_prompt(AttendArgs a, int
             *reinterpret_cast<const bf16x8*>(at + 8 * ((2 * k + g) ^ (c & 7))), qf[k], sc[t], 0, 0, 0);
     }
     const bool masked = tile * kTile < blk.full_lo || tile * kTile + kTile > blk.full_hi || in != 0xfu;
+#pragma unroll
+    for (int t = 0; t < 2; ++t) sc[t] *= a.scale2;
+    if (masked) {
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          const int j = tile * kTile + 32 * t + 16 * (i / 8) + 8 * g + i % 8;
+          sc[t][i] = j >= lo && j < hi && (in >> (2 * t + i / 8) & 1u) ? sc[t][i] : -INFINITY;
+        }
+    }
     float top = -INFINITY;
 #pragma unroll
     for (int t = 0; t < 2; ++t)
 #pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        float x = sc[t][i] * a.scale2;
-        if (masked) {
-          const int j = tile * kTile + 32 * t + 16 * (i / 8) + 8 * g + i % 8;
-          x = j >= lo && j < hi && (in >> (2 * t + i / 8) & 1u) ? x : -INFINITY;
-        }
-        sc[t][i] = x;
-        top = fmaxf(top, x);
-      }
+      for (int i = 0; i < 16; ++i) top = fmaxf(top, sc[t][i]);
     {
       const auto u = __builtin_amdgcn_permlane32_swap(__float_as_uint(top), __float_as_uint(top), false, false);
       top = fmaxf(__uint_as_float(u[0]), __uint_as_float(u[1]));
@@ -190,23 +208,23 @@ __global__ __launch_bounds__(kThreads, 2) void k_attend_prompt(AttendArgs a, int
             *reinterpret_cast<const bf16x8*>(vt[buf] + (32 * d + c) * kTile + 8 * ((2 * u + g) ^ (c & 7))), p, o[d], 0,
             0, 0);
     }
-    if (more) store(buf ^ 1);
+    if (more) store(buf ^ 1, tile + 1);
+    in = in_next;
   }
   {
     const auto u = __builtin_amdgcn_permlane32_swap(__float_as_uint(l), __float_as_uint(l), false, false);
     l = __uint_as_float(u[0]) + __uint_as_float(u[1]);
   }
   if (!valid) return;
-  if (splits > 1) {
-    // items count blocks from the first, as the join does
-    const int64_t slot = (int64_t(item - local + (nblocks - 1 - local / splits) * splits + local % splits) * Hkv + h) * kRows + 32 * w + c;
+  if (slot >= 0) {
+    const int64_t at = (int64_t(slot) * Hkv + h) * kRows + 32 * w + c;
 #pragma unroll
     for (int d = 0; d < DT; ++d)
 #pragma unroll
       for (int i = 0; i < 4; ++i)
-        *reinterpret_cast<f32x4*>(a.part + slot * D + 32 * d + 8 * i + 4 * g) =
+        *reinterpret_cast<f32x4*>(a.part + at * D + 32 * d + 8 * i + 4 * g) =
             f32x4{o[d][4 * i], o[d][4 * i + 1], o[d][4 * i + 2], o[d][4 * i + 3]};
-    if (g == 0) a.part_ml[2 * slot] = m, a.part_ml[2 * slot + 1] = l;
+    if (g == 0) a.part_ml[2 * at] = m, a.part_ml[2 * at + 1] = l;
     return;
   }
   const int t = s.start + row / G, head = h * G + row % G;
@@ -222,12 +240,23 @@ __global__ __launch_bounds__(kThreads, 2) void k_attend_prompt(AttendArgs a, int
   if (a.lse && g == 0) a.lse[int64_t(t) * a.q_heads + head] = l == 0.f ? -INFINITY : m * kLn2 + logf(l);
 }
 
+template <int D>
+__global__ __launch_bounds__(kThreads, 2) void k_attend_prompt(AttendArgs a) {
+  __shared__ __align__(16) Stages<D> lds;
+  const int Hkv = a.cache.kv_heads, h = blockIdx.x % Hkv, all = gridDim.x / Hkv;
+  const Partition<kRows> part(a);
+  // the last blocks first: in a causal batch they are the longest
+  part.each_piece(all - 1 - int(blockIdx.x) / Hkv, [&](int b, int k, int off, int count, int slot) {
+    attend_block<D>(a, part, h, b, k, off, count, slot, lds);
+  });
+}
+
 }  // namespace
 
 hipError_t launch_attend_prompt(const AttendArgs& a, const AttendPlan& p, hipStream_t s) {
-  const dim3 grid(p.slots * a.cache.kv_heads), block(kThreads);
-  if (a.cache.head_dim == 128) hipLaunchKernelGGL((k_attend_prompt<128>), grid, block, 0, s, a, p.blocks);
-  else hipLaunchKernelGGL((k_attend_prompt<64>), grid, block, 0, s, a, p.blocks);
+  const dim3 grid(uint32_t((p.shared ? p.workers : p.blocks) * a.cache.kv_heads)), block(kThreads);
+  if (a.cache.head_dim == 128) hipLaunchKernelGGL((k_attend_prompt<128>), grid, block, 0, s, a);
+  else hipLaunchKernelGGL((k_attend_prompt<64>), grid, block, 0, s, a);
   return hipGetLastError();
 }
 

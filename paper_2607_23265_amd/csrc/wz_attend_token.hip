@@ -14,32 +14,26 @@
 //                 product m's right operand as they stand; its left operand is
 //                 8 bytes of a channel's tokens, which lie together in a page.
 //
-// Four waves take a block's tiles in turn, each with a running maximum and sum,
+// The waves take a block's tiles in turn, each with a running maximum and sum,
 // and join through LDS at the end in a fixed order.
 #include "wz_attend.h"
 
 namespace wz {
 namespace {
 
-constexpr int kWaves = 4;
-constexpr int kThreads = kWaves * kWave;
-
-template <int D, int NT>
-__global__ __launch_bounds__(kThreads) void k_attend_token(AttendArgs a, int blocks_bound) {
-  constexpr int BR = 16 * NT, KK = D / 32, DT = D / 16, kPieces = D / 64;
+// Tiles [off, off + count) of block k of sequence b, key/value head h; slot:
+// where its part goes, -1 if the block is this workgroup's alone.
+template <int D, int NT, int kWaves>
+__device__ __forceinline__ void attend_block(const AttendArgs& a, const Partition<16 * NT>& part, int h, int b, int k,
+                                             int off, int count, int slot, float* so, float (*sm)[16 * NT],
+                                             float (*sl)[16 * NT]) {
+  constexpr int BR = 16 * NT, KK = D / 32, DT = D / 16, kPieces = D / 64, kThreads = kWaves * kWave;
   constexpr int kLd = D + 4;
-  __shared__ float so[BR * kLd];
-  __shared__ float sm[kWaves][BR], sl[kWaves][BR];
-
-  const int Hkv = a.cache.kv_heads, h = blockIdx.x % Hkv, item = blockIdx.x / Hkv;
-  const Partition<BR> part(a, blocks_bound);
-  int b, local;
-  if (!find_item(a.batch.batch, item, [&](int i) { return part.items(i); }, &b, &local)) return;
+  const int Hkv = a.cache.kv_heads, G = part.G;
   const Seq s = sequence(a.batch, b);
-  const int splits = part.splits(s), G = part.G;
-  const Block blk = part.block(s, local / splits);
-  const int T0 = blk.lo / kTile + local % splits * part.chunk;
-  const int T1 = min((max(blk.hi, blk.lo) + kTile - 1) / kTile, splits > 1 ? T0 + part.chunk : 1 << 24);
+  const Block blk = part.block(s, k);
+  const int T0 = blk.lo / kTile + off;
+  const int T1 = min((max(blk.hi, blk.lo) + kTile - 1) / kTile, T0 + count);
 
   const int lane = __lane_id(), w = threadIdx.x / kWave, c = lane & 15, q = lane >> 4;
   const int P = a.cache.page_size, logP = __builtin_ctz(P);
@@ -71,27 +65,48 @@ __global__ __launch_bounds__(kThreads) void k_attend_token(AttendArgs a, int blo
     for (int d = 0; d < DT; ++d) o[n][d] = f32x4{};
   }
 
-  // pages of the lane's key block (c / 4) and value block (q) in a tile
-  auto page = [&](int tile, int blk16) {
-    const int tok = tile * kTile + 16 * blk16;
-    return tile < T1 && tok < s.kv ? page_of(a.batch, a.cache.pages, b, tok >> logP) : -1;
-  };
-  int kp = page(T0 + w, c >> 2), vp = page(T0 + w, q);
-  for (int tile = T0 + w; tile < T1; tile += kWaves) {
-    const bool kin = kp >= 0, vin = vp >= 0;
-    const int64_t kh = int64_t(kin ? kp : 0) * Hkv + h, vh = int64_t(vin ? vp : 0) * Hkv + h;
-    const uint8_t* kb = kc + kh * (P * D) + ((tile * kTile + 16 * (c >> 2)) & (P - 1)) * D + (c & 3) * D + 16 * q;
-    const uint8_t* vb = vc + vh * (P * D) + c * P + ((tile * kTile + 16 * q) & (P - 1));
+  // Codes of a tile as they come, two tiles to a wave: the loads of the next
+  // one are under way while this one is worked on.  Nothing branches around a
+  // load: what lies behind the last tile is the last tile again, and a block
+  // that has no page reads page 0 and is masked.
+  struct Tile {
     u32x4 kx[4][kPieces], vx[DT];
+    float ks, vs;
+    bool vin;
+  } bufs[2];
+  const int last = T0 + w + (max(T1 - T0 - w, 1) - 1) / kWaves * kWaves;  // this wave's last tile
+  const int* const row = a.batch.table + int64_t(b) * a.batch.table_stride;
+  const int entries = max((s.kv + P - 1) >> logP, 1);
+  // Pages of the lane's key block (c / 4) and value block (q) in a tile: asked
+  // for before the loads of the tile in front, so that waiting for them does
+  // not wait for those.
+  struct Pages {
+    int k, v;
+  } ids[2];
+  auto pages = [&](int tile) {
+    const int tok = min(tile, last) * kTile;
+    return Pages{row[min((tok + 16 * (c >> 2)) >> logP, entries - 1)], row[min((tok + 16 * q) >> logP, entries - 1)]};
+  };
+  auto load = [&](Tile& x, int tile, Pages id) {
+    const int tok = min(tile, last) * kTile, kp = id.k, vp = id.v;
+    const bool kin = uint32_t(kp) < uint32_t(a.cache.pages);
+    x.vin = uint32_t(vp) < uint32_t(a.cache.pages);
+    const int64_t kh = int64_t(kin ? kp : 0) * Hkv + h, vh = int64_t(x.vin ? vp : 0) * Hkv + h;
+    const uint8_t* kb = kc + kh * (P * D) + ((tok + 16 * (c >> 2)) & (P - 1)) * D + (c & 3) * D + 16 * q;
+    const uint8_t* vb = vc + vh * (P * D) + c * P + ((tok + 16 * q) & (P - 1));
 #pragma unroll
     for (int t = 0; t < 4; ++t)
 #pragma unroll
-      for (int i = 0; i < kPieces; ++i) kx[t][i] = *reinterpret_cast<const u32x4*>(kb + 4 * t * D + 64 * i);
-    const float ks = a.cache.k_scale[kh], vs = vin ? a.cache.v_scale[vh] : 1.f;
+      for (int i = 0; i < kPieces; ++i) x.kx[t][i] = *reinterpret_cast<const u32x4*>(kb + 4 * t * D + 64 * i);
+    x.ks = a.cache.k_scale[kh], x.vs = a.cache.v_scale[vh];
 #pragma unroll
-    for (int d = 0; d < DT; ++d) vx[d] = *reinterpret_cast<const u32x4*>(vb + 16 * d * P);
-    kp = page(tile + kWaves, c >> 2), vp = page(tile + kWaves, q);
-
+    for (int d = 0; d < DT; ++d) x.vx[d] = *reinterpret_cast<const u32x4*>(vb + 16 * d * P);
+    __builtin_amdgcn_sched_barrier(0);
+  };
+  auto work = [&](Tile& x, int tile) {
+    const bool vin = x.vin;
+    const float ks = x.ks, vs = vin ? x.vs : 1.f;
+    u32x4 (&kx)[4][kPieces] = x.kx, (&vx)[DT] = x.vx;
     f32x4 sc[NT][4];
 #pragma unroll
     for (int t = 0; t < 4; ++t) {
@@ -117,19 +132,22 @@ __global__ __launch_bounds__(kThreads) void k_attend_token(AttendArgs a, int blo
     bf16x8 p[NT][2];
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
+#pragma unroll
+      for (int t = 0; t < 4; ++t) sc[n][t] *= a.scale2;
+      if (masked) {
+#pragma unroll
+        for (int t = 0; t < 4; ++t)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const int j = first + 4 * t + i;
+            sc[n][t][i] = vin && j >= lo[n] && j < hi[n] ? sc[n][t][i] : -INFINITY;
+          }
+      }
       float top = -INFINITY;
 #pragma unroll
       for (int t = 0; t < 4; ++t)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          float x = sc[n][t][i] * a.scale2;
-          if (masked) {
-            const int j = first + 4 * t + i;
-            x = vin && j >= lo[n] && j < hi[n] ? x : -INFINITY;
-          }
-          sc[n][t][i] = x;
-          top = fmaxf(top, x);
-        }
+        for (int i = 0; i < 4; ++i) top = fmaxf(top, sc[n][t][i]);
       {
         const auto u = __builtin_amdgcn_permlane16_swap(__float_as_uint(top), __float_as_uint(top), false, false);
         top = fmaxf(__uint_as_float(u[0]), __uint_as_float(u[1]));
@@ -166,6 +184,20 @@ __global__ __launch_bounds__(kThreads) void k_attend_token(AttendArgs a, int blo
         o[n][d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v1, p[n][1], o[n][d], 0, 0, 0);
       }
     }
+  };
+  if (T0 + w < T1) {
+    ids[0] = pages(T0 + w);
+    ids[1] = pages(T0 + w + kWaves);
+    load(bufs[0], T0 + w, ids[0]);
+    for (int tile = T0 + w; tile < T1; tile += 2 * kWaves) {
+      ids[0] = pages(tile + 2 * kWaves);
+      load(bufs[1], tile + kWaves, ids[1]);
+      work(bufs[0], tile);
+      if (tile + kWaves >= T1) break;
+      ids[1] = pages(tile + 3 * kWaves);
+      load(bufs[0], tile + 2 * kWaves, ids[0]);
+      work(bufs[1], tile + kWaves);
+    }
   }
 
   // join the waves
@@ -175,41 +207,39 @@ __global__ __launch_bounds__(kThreads) void k_attend_token(AttendArgs a, int blo
     if (q == 0) sm[w][16 * n + c] = m[n], sl[w][16 * n + c] = l[n];
   }
   __syncthreads();
-  float top[NT], f[NT];
+  float f[NT];
 #pragma unroll
   for (int n = 0; n < NT; ++n) {
-    const int r = 16 * n + c;
-    top[n] = fmaxf(fmaxf(sm[0][r], sm[1][r]), fmaxf(sm[2][r], sm[3][r]));
-    f[n] = m[n] == -INFINITY ? (l[n] == 0.f ? 0.f : l[n]) : __builtin_amdgcn_exp2f(m[n] - top[n]);
-  }
-  for (int turn = 0; turn < kWaves; ++turn) {
-    if (turn == w) {
+    float top = -INFINITY;
 #pragma unroll
-      for (int n = 0; n < NT; ++n)
+    for (int i = 0; i < kWaves; ++i) top = fmaxf(top, sm[i][16 * n + c]);
+    // a wave without a score has a sum of 0, or of NaN if every score was
+    f[n] = m[n] == -INFINITY ? l[n] : __builtin_amdgcn_exp2f(m[n] - top);
 #pragma unroll
-        for (int d = 0; d < DT; ++d) {
-          f32x4* at = reinterpret_cast<f32x4*>(so + (16 * n + c) * kLd + 16 * d + 4 * q);
-          f32x4 x = turn ? *at : f32x4{};
+    for (int d = 0; d < DT; ++d) {
+      f32x4 x;
 #pragma unroll
-          for (int i = 0; i < 4; ++i) x[i] += o[n][d][i] * f[n];
-          *at = x;
-        }
+      for (int i = 0; i < 4; ++i) x[i] = o[n][d][i] * f[n];
+      *reinterpret_cast<f32x4*>(so + (w * BR + 16 * n + c) * kLd + 16 * d + 4 * q) = x;
     }
-    __syncthreads();
   }
+  __syncthreads();
   const int rows = min(BR, blk.rows - blk.r0);
   for (int i = threadIdx.x; i < rows * (D / 4); i += kThreads) {
     const int r = i / (D / 4), d = (i % (D / 4)) * 4;
     float mx = -INFINITY, sum = 0.f;
+    f32x4 x{};
 #pragma unroll
-    for (int k = 0; k < kWaves; ++k) mx = fmaxf(mx, sm[k][r]);
+    for (int u = 0; u < kWaves; ++u) mx = fmaxf(mx, sm[u][r]);
 #pragma unroll
-    for (int k = 0; k < kWaves; ++k) sum += sm[k][r] == -INFINITY ? sl[k][r] : sl[k][r] * __builtin_amdgcn_exp2f(sm[k][r] - mx);
-    const f32x4 x = *reinterpret_cast<const f32x4*>(so + r * kLd + d);
-    if (splits > 1) {
-      const int64_t slot = (int64_t(item) * Hkv + h) * BR + r;
-      *reinterpret_cast<f32x4*>(a.part + slot * D + d) = x;
-      if (d == 0) a.part_ml[2 * slot] = mx, a.part_ml[2 * slot + 1] = sum;
+    for (int u = 0; u < kWaves; ++u) {
+      sum += sm[u][r] == -INFINITY ? sl[u][r] : sl[u][r] * __builtin_amdgcn_exp2f(sm[u][r] - mx);
+      x += *reinterpret_cast<const f32x4*>(so + (u * BR + r) * kLd + d);
+    }
+    if (slot >= 0) {
+      const int64_t at = (int64_t(slot) * Hkv + h) * BR + r;
+      *reinterpret_cast<f32x4*>(a.part + at * D + d) = x;
+      if (d == 0) a.part_ml[2 * at] = mx, a.part_ml[2 * at + 1] = sum;
     } else {
       const int row = blk.r0 + r, t = s.start + row / G, head = h * G + row % G;
       const float inv = sum == 0.f ? 0.f : 1.f / sum;
@@ -221,53 +251,113 @@ __global__ __launch_bounds__(kThreads) void k_attend_token(AttendArgs a, int blo
   }
 }
 
-// The parts of a shared block added up in order: eight rows a workgroup.
-template <int D, int BR>
-__global__ __launch_bounds__(256) void k_attend_join(AttendArgs a, int blocks_bound) {
-  constexpr int kLanes = D / 4, kRows = 256 / kLanes, kGroups = (BR + kRows - 1) / kRows;
-  const int Hkv = a.cache.kv_heads, h = blockIdx.x % Hkv, at = blockIdx.x / Hkv, group = at % kGroups;
-  const Partition<BR> part(a, blocks_bound);
-  int b, k;
-  if (!find_item(a.batch.batch, at / kGroups, [&](int i) { return part.blocks(sequence(a.batch, i)); }, &b, &k)) return;
-  const Seq s = sequence(a.batch, b);
-  const int splits = part.splits(s), G = part.G;
-  if (splits == 1) return;  // written by its only item
-  const int r = group * kRows + threadIdx.x / kLanes, d = (threadIdx.x % kLanes) * 4, row = k * BR + r;
-  int base = 0;  // items of the sequences before b
-  for (int b0 = 0; b0 < b; b0 += kWave) {
-    const int i = b0 + __lane_id();
-    base += wave_reduce_sum_i32(i < b ? part.items(i) : 0);
-  }
-  if (r >= BR || row >= part.rows(s)) return;
-  const int64_t step = int64_t(Hkv) * BR, slot0 = (int64_t(base + k * splits) * Hkv + h) * BR + r;
-  float mx = -INFINITY;
-  for (int i = 0; i < splits; ++i) mx = fmaxf(mx, a.part_ml[2 * (slot0 + i * step)]);
-  float sum = 0.f;
-  f32x4 x{};
-#pragma unroll 8
-  for (int i = 0; i < splits; ++i) {
-    const int64_t slot = slot0 + i * step;
-    const float m = a.part_ml[2 * slot], l = a.part_ml[2 * slot + 1];
-    const f32x4 y = *reinterpret_cast<const f32x4*>(a.part + slot * D + d);
-    // a part without a score has a sum of 0, or of NaN if every score was
-    const float f = m == -INFINITY ? l : __builtin_amdgcn_exp2f(m - mx);
-    sum += m == -INFINITY ? l : l * f;
+template <int D, int NT, int kWaves>
+__global__ __launch_bounds__(kWaves* kWave, NT == 1 ? 2 : 1) void k_attend_token(AttendArgs a) {
+  constexpr int BR = 16 * NT;
+  __shared__ __align__(16) float so[kWaves * BR * (D + 4)];
+  __shared__ float sm[kWaves][BR], sl[kWaves][BR];
+  const int Hkv = a.cache.kv_heads, h = blockIdx.x % Hkv, me = blockIdx.x / Hkv;
+  const Partition<BR> part(a);
+  part.each_piece(me, [&](int b, int k, int off, int count, int slot) {
+    attend_block<D, NT, kWaves>(a, part, h, b, k, off, count, slot, so, sm, sl);
+  });
+}
+
+// The parts of a shared block added up.  A workgroup has 256 / (D / 4) groups
+// of lanes; PG of them share a row, taking its parts in turn, so that a row of
+// many parts costs a few loads' latency, and add up through LDS in order.
+template <int D, int BR, int PG>
+__global__ __launch_bounds__(256) void k_attend_join(AttendArgs a) {
+  constexpr int kLanes = D / 4, kRows = 256 / kLanes / PG;  // rows of a workgroup
+  __shared__ __align__(16) float sums[256 / kLanes][D];
+  __shared__ float red[2][256 / kLanes];
+  const int Hkv = a.cache.kv_heads, h = blockIdx.x % Hkv, at = blockIdx.x / Hkv;
+  const Partition<BR> part(a);
+  Spot x;
+  if (!part.template find<false>(at / (BR / kRows), &x)) return;
+  const Seq s = sequence(a.batch, x.seq);
+  const int first = x.before / part.run, last = (x.before + x.tiles - 1) / part.run;
+  if (first == last) return;  // written by the only workgroup that had it
+  const int lane = threadIdx.x % kLanes, all_groups = threadIdx.x / kLanes, d = 4 * lane;
+  const int group = all_groups % PG, mine = all_groups / PG;
+  const int G = part.G, r = at % (BR / kRows) * kRows + mine, row = x.k * BR + r;
+  const bool in = row < s.n * G;  // (its slots exist in any case)
+  const int64_t step = int64_t(Hkv) * BR, slot0 = (int64_t(first + x.block) * Hkv + h) * BR + r;
+  // a running maximum as in the kernels that left the parts; a part without a
+  // score has a maximum of -inf and a sum of 0, or of NaN if every score was
+  float top = -INFINITY, sum = 0.f;
+  f32x4 o{};
+  for (int i = first + group; i <= last; i += 4 * PG) {
+    float m[4], l[4];
+    f32x4 y[4];
 #pragma unroll
-    for (int e = 0; e < 4; ++e) x[e] += f == 0.f ? 0.f : y[e] * f;
+    for (int u = 0; u < 4; ++u) {  // four parts at once; behind the last one the first again, without weight
+      const int j = i + u * PG;
+      const int64_t slot = slot0 + (j <= last ? j - first : 0) * step;
+      m[u] = a.part_ml[2 * slot], l[u] = a.part_ml[2 * slot + 1];
+      y[u] = *reinterpret_cast<const f32x4*>(a.part + slot * D + d);
+      if (j > last) m[u] = -INFINITY, l[u] = 0.f;
+    }
+    float next = top;
+#pragma unroll
+    for (int u = 0; u < 4; ++u) next = fmaxf(next, m[u]);
+    const float use = next == -INFINITY ? 0.f : next, keep = __builtin_amdgcn_exp2f(top - use);
+    sum *= keep;
+    o *= keep;
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const float f = m[u] == -INFINITY ? l[u] : __builtin_amdgcn_exp2f(m[u] - use);
+      sum += m[u] == -INFINITY ? l[u] : l[u] * f;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) o[e] += f == 0.f ? 0.f : y[u][e] * f;
+    }
+    top = next;
   }
+  float mx = top, total = sum;
+  if constexpr (PG > 1) {
+    if (lane == 0) red[0][all_groups] = top, red[1][all_groups] = sum;
+    __syncthreads();
+    const float *const tops = red[0] + mine * PG, *const sum_of = red[1] + mine * PG;
+    total = 0.f;
+#pragma unroll
+    for (int i = 0; i < PG; ++i) mx = fmaxf(mx, tops[i]);
+#pragma unroll
+    for (int i = 0; i < PG; ++i)
+      total += tops[i] == -INFINITY ? sum_of[i] : sum_of[i] * __builtin_amdgcn_exp2f(tops[i] - mx);
+    *reinterpret_cast<f32x4*>(sums[all_groups] + d) = o * (top == -INFINITY ? sum : __builtin_amdgcn_exp2f(top - mx));
+    __syncthreads();
+    if (group > 0) return;
+    o = f32x4{};
+#pragma unroll
+    for (int i = 0; i < PG; ++i) o += *reinterpret_cast<const f32x4*>(sums[mine * PG + i] + d);
+  }
+  if (!in) return;
   const int t = s.start + row / G, head = h * G + row % G;
-  const float inv = sum == 0.f ? 0.f : 1.f / sum;
+  const float inv = total == 0.f ? 0.f : 1.f / total;
   uint16_t* dst = static_cast<uint16_t*>(a.out) + t * a.out_stride + head * D + d;
-  *reinterpret_cast<u32x2*>(dst) = u32x2{to_bf16(x[0] * inv) | uint32_t(to_bf16(x[1] * inv)) << 16,
-                                         to_bf16(x[2] * inv) | uint32_t(to_bf16(x[3] * inv)) << 16};
-  if (a.lse && d == 0) a.lse[int64_t(t) * a.q_heads + head] = sum == 0.f ? -INFINITY : mx * kLn2 + logf(sum);
+  *reinterpret_cast<u32x2*>(dst) = u32x2{to_bf16(o[0] * inv) | uint32_t(to_bf16(o[1] * inv)) << 16,
+                                         to_bf16(o[2] * inv) | uint32_t(to_bf16(o[3] * inv)) << 16};
+  if (a.lse && d == 0) a.lse[int64_t(t) * a.q_heads + head] = total == 0.f ? -INFINITY : mx * kLn2 + logf(total);
 }
 
 template <int D, int BR>
-hipError_t join(const AttendArgs& a, int blocks, hipStream_t s) {
-  constexpr int kRows = 256 / (D / 4), kGroups = (BR + kRows - 1) / kRows;
-  hipLaunchKernelGGL((k_attend_join<D, BR>), dim3(blocks * kGroups * a.cache.kv_heads), dim3(256), 0, s, a, blocks);
+hipError_t join(const AttendArgs& a, const AttendPlan& p, hipStream_t s) {
+  // groups share rows where blocks have eight parts or more on average
+  constexpr int kGroups = 1024 / D;
+  const bool many = p.workers >= 8 * p.blocks;
+  const dim3 grid(uint32_t(p.blocks * (many ? BR : BR / kGroups) * a.cache.kv_heads)), block(256);
+  if (many) hipLaunchKernelGGL((k_attend_join<D, BR, kGroups>), grid, block, 0, s, a);
+  else hipLaunchKernelGGL((k_attend_join<D, BR, 1>), grid, block, 0, s, a);
   return hipGetLastError();
+}
+
+template <int D>
+void launch_token(const AttendArgs& a, const AttendPlan& p, int64_t groups, hipStream_t s) {
+  const dim3 grid{uint32_t(groups)}, four{4 * kWave}, eight{8 * kWave};
+  if (p.block_rows == 64) hipLaunchKernelGGL((k_attend_token<D, 4, 4>), grid, four, 0, s, a);
+  else if (p.block_rows == 32) hipLaunchKernelGGL((k_attend_token<D, 2, 4>), grid, four, 0, s, a);
+  else if (!p.shared && groups <= kCUs) hipLaunchKernelGGL((k_attend_token<D, 1, 8>), grid, eight, 0, s, a);
+  else hipLaunchKernelGGL((k_attend_token<D, 1, 4>), grid, four, 0, s, a);
 }
 
 }  // namespace
@@ -281,11 +371,11 @@ AttendPlan attend_plan(const wz_cache& c, const wz_ragged& r, int q_heads) {
   const int64_t blocks = std::min({int64_t(r.batch) * each, int64_t(r.tokens) * G / p.block_rows + r.batch,
                                    int64_t(r.tokens) * G});
   p.blocks = int(std::min(blocks, int64_t(1) << 28));
-  const int64_t tiles = (int64_t(r.max_kv) + 63) / 64;
-  // items meant for the whole call: a few workgroups to a CU
-  const int64_t meant = std::max<int64_t>(1, (p.block_rows > 64 ? 2 : 4) * kCUs / c.kv_heads);
-  p.shared = tiles > 8 && p.blocks < meant;
-  p.slots = p.blocks + (p.shared ? int(meant) : 0);
+  const int64_t tiles = (int64_t(r.max_kv) + kTile - 1) / kTile;
+  p.workers = int(std::max<int64_t>(1, 2 * kCUs / c.kv_heads));  // two workgroups of four waves to a CU
+  p.shared = tiles > 24 && p.blocks * tiles < (int64_t(1) << 30) &&
+             (p.block_rows > 64 ? p.blocks < p.workers : int64_t(p.blocks) * c.kv_heads < 2048);
+  p.slots = p.blocks + p.workers;
   if (p.shared) {
     const size_t n = size_t(p.slots) * c.kv_heads * p.block_rows;
     p.part_bytes = (n * c.head_dim * 4 + 255) / 256 * 256;
@@ -296,27 +386,23 @@ AttendPlan attend_plan(const wz_cache& c, const wz_ragged& r, int q_heads) {
 }
 
 hipError_t launch_attend(const AttendArgs& a, const AttendPlan& p, hipStream_t s) {
-  const dim3 grid(p.slots * a.cache.kv_heads), block(kThreads);
+  const int64_t groups = int64_t(p.shared ? p.workers : p.blocks) * a.cache.kv_heads;
   const int D = a.cache.head_dim;
   if (p.block_rows > 64) {
     const hipError_t e = launch_attend_prompt(a, p, s);
     if (e != hipSuccess) return e;
   } else if (D == 128) {
-    if (p.block_rows == 16) hipLaunchKernelGGL((k_attend_token<128, 1>), grid, block, 0, s, a, p.blocks);
-    else if (p.block_rows == 32) hipLaunchKernelGGL((k_attend_token<128, 2>), grid, block, 0, s, a, p.blocks);
-    else hipLaunchKernelGGL((k_attend_token<128, 4>), grid, block, 0, s, a, p.blocks);
+    launch_token<128>(a, p, groups, s);
   } else {
-    if (p.block_rows == 16) hipLaunchKernelGGL((k_attend_token<64, 1>), grid, block, 0, s, a, p.blocks);
-    else if (p.block_rows == 32) hipLaunchKernelGGL((k_attend_token<64, 2>), grid, block, 0, s, a, p.blocks);
-    else hipLaunchKernelGGL((k_attend_token<64, 4>), grid, block, 0, s, a, p.blocks);
+    launch_token<64>(a, p, groups, s);
   }
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || !p.shared) return e;
   switch (p.block_rows) {
-    case 16: return D == 128 ? join<128, 16>(a, p.blocks, s) : join<64, 16>(a, p.blocks, s);
-    case 32: return D == 128 ? join<128, 32>(a, p.blocks, s) : join<64, 32>(a, p.blocks, s);
-    case 64: return D == 128 ? join<128, 64>(a, p.blocks, s) : join<64, 64>(a, p.blocks, s);
-    default: return D == 128 ? join<128, 128>(a, p.blocks, s) : join<64, 128>(a, p.blocks, s);
+    case 16: return D == 128 ? join<128, 16>(a, p, s) : join<64, 16>(a, p, s);
+    case 32: return D == 128 ? join<128, 32>(a, p, s) : join<64, 32>(a, p, s);
+    case 64: return D == 128 ? join<128, 64>(a, p, s) : join<64, 64>(a, p, s);
+    default: return D == 128 ? join<128, 128>(a, p, s) : join<64, 128>(a, p, s);
   }
 }
 

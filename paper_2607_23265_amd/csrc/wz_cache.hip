@@ -338,9 +338,9 @@ __global__ __launch_bounds__(kThreads) void k_append(AppendArgs a, int page_grou
     const int lo = max(q.place0, 0), hi = min(q.place0 + q.n, q.kv);
     return hi > lo ? (hi - 1) / P - lo / P + 1 : 0;
   };
-  int b, nth;
-  if (!find_item(a.batch.batch, id / a.cache.kv_heads, touched, &b, &nth)) return;
-  append_page<In, D, P>(a, b, sequence(a.batch, b), nth, id % a.cache.kv_heads, smem);
+  const Found f = find_item(a.batch.batch, id / a.cache.kv_heads, touched);
+  if (f.seq < 0) return;
+  append_page<In, D, P>(a, f.seq, sequence(a.batch, f.seq), f.local, id % a.cache.kv_heads, smem);
 }
 
 template <typename In, int D>

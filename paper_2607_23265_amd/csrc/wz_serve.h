@@ -33,9 +33,12 @@ __device__ __forceinline__ Seq sequence(const wz_ragged& r, int b) {
 
 // Where work item `id` lies when sequence b has count(b) items: its sequence
 // and its number among that sequence's.  Every wave finds it by itself, 64
-// sequences at a time; false behind the last item.
+// sequences at a time; seq is -1 behind the last item.
+struct Found {
+  int seq, local;
+};
 template <typename Count>
-__device__ __forceinline__ bool find_item(int batch, int id, Count count, int* seq, int* local) {
+__device__ __forceinline__ Found find_item(int batch, int id, Count count) {
   const int lane = __lane_id();
   int base = 0;
   for (int b0 = 0; b0 < batch; b0 += kWave) {
@@ -44,13 +47,11 @@ __device__ __forceinline__ bool find_item(int batch, int id, Count count, int* s
     const int total = __builtin_amdgcn_readlane(incl, kWave - 1);
     if (id - base < total) {
       const int l = __builtin_ctzll(__ballot(incl > id - base));
-      *seq = b0 + l;
-      *local = id - base - (__builtin_amdgcn_readlane(incl, l) - __builtin_amdgcn_readlane(c, l));
-      return true;
+      return Found{b0 + l, id - base - (__builtin_amdgcn_readlane(incl, l) - __builtin_amdgcn_readlane(c, l))};
     }
     base += total;
   }
-  return false;
+  return Found{-1, 0};
 }
 
 // The page that `table` entry holds, or -1 where it is none of the cache's.
@@ -82,16 +83,18 @@ struct AttendArgs {
   int64_t q_stride, out_stride;
   float scale2;  // the scores' factor times log2(e)
   int q_heads, causal, window;
-  // the plan (attend_plan): slots items for each key/value head
-  int slots;
-  int shared;        // items of one row block share its tokens, through the workspace
+  int blocks;        // the plan's (attend_plan), for each key/value head
+  int workers;       // shared: workgroups that share the blocks' tokens, through the workspace
+  int shared;
   float* part;       // shared: [slots][kv_heads][rows of a block][head_dim] unnormalised sums
   float* part_ml;    // shared: [slots][kv_heads][rows of a block][2] maximum (log2) and sum
 };
 struct AttendPlan {
   int block_rows;    // rows of a block: 16, 32, 64 (token kernel) or more (prompt kernel)
-  int slots, blocks; // upper bounds over the batch, for each key/value head
-  bool shared;
+  int blocks;        // upper bound of the batch's blocks, for each key/value head
+  int workers;       // shared: workgroups for each key/value head
+  int slots;         // of the workspace, for each key/value head
+  bool shared;       // several workgroups share a block's tokens
   size_t part_bytes, ml_bytes, bytes;
 };
 AttendPlan attend_plan(const wz_cache& c, const wz_ragged& r, int q_heads);

@@ -63,7 +63,7 @@ wz_status check_attention(const wz_cache* cache, const wz_ragged* batch, const w
       !std::isfinite(cfg->scale))
     return WZ_ERR_PARAM;
   const AttendPlan p = attend_plan(*cache, *batch, cfg->q_heads);
-  if (int64_t(p.slots) * cache->kv_heads > 0x7fffffff) return WZ_ERR_SHAPE;
+  if (int64_t(p.slots) * cache->kv_heads * 16 > 0x7fffffff) return WZ_ERR_SHAPE;  // a grid's workgroups
   return WZ_OK;
 }
 
@@ -144,7 +144,7 @@ wz_status wz_cache_attention(const wz_cache* cache, const wz_ragged* batch, cons
   a.q_stride = q_stride, a.out_stride = out_stride;
   a.scale2 = cfg->scale * 1.44269504088896341f;
   a.q_heads = cfg->q_heads, a.causal = cfg->causal, a.window = cfg->window;
-  a.slots = p.slots, a.shared = p.shared;
+  a.blocks = p.blocks, a.workers = p.workers, a.shared = p.shared;
   return from_hip(launch_attend(a, p, static_cast<hipStream_t>(stream)));
 }
 

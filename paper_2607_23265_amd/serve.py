@@ -15,6 +15,7 @@ EXPORTS = ("wz_cache_append", "wz_cache_attention", "wz_attention_workspace_byte
            "wz_matmul_int")
 E4M3 = torch.float8_e4m3fn
 _DTYPE = {torch.float32: wz.WZ_F32, torch.bfloat16: wz.WZ_BF16}
+_FLOATS, _BF16, _INT8 = tuple(_DTYPE), (torch.bfloat16,), (torch.int8,)
 _P, _I, _L, _S = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_size_t
 
 
@@ -66,7 +67,7 @@ def lib():
 
 
 def _dense(name, t, dtype, device=None):
-    if not t.is_cuda or not t.is_contiguous() or t.dtype != dtype or (device is not None and t.device != device):
+    if not t.is_cuda or not t.is_contiguous() or t.dtype is not dtype or (device is not None and t.device != device):
         raise ValueError(f"{name} must be a contiguous {dtype} tensor" + (f" on {device}" if device else " on a GPU"))
     return t
 
@@ -83,13 +84,19 @@ def _rows(name, t, heads, dim, device, dtypes):
     return stride[0] if t.shape[0] > 1 else max(stride[0], t.shape[1] * dim)
 
 
+# The current stream's handle without a torch.cuda.Stream made for it (0.1 us instead of 2, of a call's 10).
+_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
+    lambda index: torch.cuda.current_stream(index).cuda_stream)
+
+
 def _call(device, where, f, *args):
     """f(*args, stream) on `device`'s current stream, with that device current."""
-    if torch.cuda.current_device() == device.index:
-        st = f(*args, torch.cuda.current_stream(device).cuda_stream)
+    index = device.index
+    if torch.cuda.current_device() == index:
+        st = f(*args, _stream(index))
     else:
         with torch.cuda.device(device):
-            st = f(*args, torch.cuda.current_stream(device).cuda_stream)
+            st = f(*args, _stream(index))
     if st != 0:
         raise wz.WZError(st, where)
 
@@ -168,7 +175,7 @@ def cache_append(cache, batch, k, v, rotation=None, positions=None, q=None, q_ou
     rotated by positions [axes, tokens] int32; returns the rotated queries [tokens, q_heads, head_dim] bfloat16 if q
     is given (into q_out if that is)."""
     dev, dim, tokens = cache.device, cache.head_dim, k.shape[0]
-    types = (k.dtype,) if k.dtype in _DTYPE else tuple(_DTYPE)
+    types = (k.dtype,) if k.dtype in _DTYPE else _FLOATS
     ks = _rows("k", k, cache.kv_heads, dim, dev, types)
     vs = _rows("v", v, cache.kv_heads, dim, dev, types)
     if v.shape[0] != tokens or batch.device != dev:
@@ -177,8 +184,8 @@ def cache_append(cache, batch, k, v, rotation=None, positions=None, q=None, q_ou
     if q is not None:
         qs, heads = _rows("q", q, None, dim, dev, types), q.shape[1]
         if q_out is None:
-            q_out = torch.empty(q.shape, dtype=torch.bfloat16, device=dev)
-        qos = _rows("q_out", q_out, heads, dim, dev, (torch.bfloat16,))
+            q_out = q.new_empty(q.shape, dtype=torch.bfloat16)
+        qos = _rows("q_out", q_out, heads, dim, dev, _BF16)
         if q.shape[0] != tokens or q_out.shape[0] != tokens:
             raise ValueError("q and q_out must have the tokens of k")
     turn = None
@@ -209,10 +216,10 @@ def cache_attention(cache, batch, q, scale=None, causal=True, window=0, out=None
     defaults to head_dim ** -0.5; lse [tokens, q_heads] float32 receives the rows' log-sum-exp; ws is a uint8 workspace
     (allocated if not given and needed)."""
     dev, dim = cache.device, cache.head_dim
-    qs, tokens, heads = _rows("q", q, None, dim, dev, (torch.bfloat16,)), q.shape[0], q.shape[1]
+    qs, tokens, heads = _rows("q", q, None, dim, dev, _BF16), q.shape[0], q.shape[1]
     if out is None:
-        out = torch.empty((tokens, heads, dim), dtype=torch.bfloat16, device=dev)
-    os_ = _rows("out", out, heads, dim, dev, (torch.bfloat16,))
+        out = q.new_empty((tokens, heads, dim))
+    os_ = _rows("out", out, heads, dim, dev, _BF16)
     if out.shape[0] != tokens or batch.device != dev:
         raise ValueError("out must have the rows of q, and the batch must be on their device")
     if lse is not None and _dense("lse", lse, torch.float32, dev).shape != (tokens, heads):
@@ -221,7 +228,7 @@ def cache_attention(cache, batch, q, scale=None, causal=True, window=0, out=None
     c, r = ctypes.byref(cache.c), batch.of(tokens)
     if ws is None:
         need = lib().wz_attention_workspace_bytes(c, r, cfg)
-        ws = torch.empty(need, dtype=torch.uint8, device=dev) if need else None
+        ws = q.new_empty(need, dtype=torch.uint8) if need else None
     else:
         _dense("ws", ws, torch.uint8, dev)
     _call(dev, "wz_cache_attention", lib().wz_cache_attention, c, r, cfg, q.data_ptr(), qs, out.data_ptr(), os_,
@@ -241,13 +248,13 @@ def _matrix(name, t, dtypes, device=None):
 
 def quantize_rows(x, out=None, scale=None):
     """wz_quantize_rows: x [rows, cols] float32 or bfloat16 -> (int8 [rows, cols], scale [rows] float32)."""
-    xs, dev = _matrix("x", x, tuple(_DTYPE)), x.device
+    xs, dev = _matrix("x", x, _FLOATS), x.device
     rows, cols = x.shape
     if out is None:
-        out = torch.empty((rows, cols), dtype=torch.int8, device=dev)
+        out = x.new_empty((rows, cols), dtype=torch.int8)
     if scale is None:
-        scale = torch.empty(rows, dtype=torch.float32, device=dev)
-    qs = _matrix("out", out, (torch.int8,), dev)
+        scale = x.new_empty(rows, dtype=torch.float32)
+    qs = _matrix("out", out, _INT8, dev)
     if out.shape != x.shape or _dense("scale", scale, torch.float32, dev).shape != (rows,):
         raise ValueError("out must have the shape of x, and scale [rows]")
     _call(dev, "wz_quantize_rows", lib().wz_quantize_rows, x.data_ptr(), xs, rows, cols, _DTYPE[x.dtype],
@@ -258,8 +265,8 @@ def quantize_rows(x, out=None, scale=None):
 def matmul_int(a, a_scale, w, w_scale, bias=None, out=None, out_dtype=torch.bfloat16):
     """wz_matmul_int: a [M, K] and w [N, K] int8 with scales [M] and [N] -> a w^T, scaled, + bias [N], as out_dtype
     [M, N] (or the type of out)."""
-    as_, dev = _matrix("a", a, (torch.int8,)), a.device
-    ws = _matrix("w", w, (torch.int8,), dev)
+    as_, dev = _matrix("a", a, _INT8), a.device
+    ws = _matrix("w", w, _INT8, dev)
     M, K = a.shape
     N = w.shape[0]
     if w.shape[1] != K:
@@ -269,8 +276,8 @@ def matmul_int(a, a_scale, w, w_scale, bias=None, out=None, out_dtype=torch.bflo
             (bias is not None and _dense("bias", bias, torch.float32, dev).numel() != N)):
         raise ValueError("a_scale must be [M], w_scale and bias [N]")
     if out is None:
-        out = torch.empty((M, N), dtype=out_dtype, device=dev)
-    os_ = _matrix("out", out, tuple(_DTYPE), dev)
+        out = a.new_empty((M, N), dtype=out_dtype)
+    os_ = _matrix("out", out, _FLOATS, dev)
     if out.shape != (M, N):
         raise ValueError("out must be [M, N]")
     _call(dev, "wz_matmul_int", lib().wz_matmul_int, a.data_ptr(), as_, a_scale.data_ptr(), w.data_ptr(), ws,

@@ -147,10 +147,12 @@ def test_attention_arguments(L):
     assert attend(L, q=None) == NULL and attend(L, q=AT + 8) == ALIGN and attend(L, qs=3576) == SHAPE
     assert attend(L, out=None) == NULL and attend(L, out=AT + 2) == ALIGN and attend(L, os=3590) == SHAPE
     assert attend(L, lse=AT + 2) == ALIGN
-    need = L.wz_attention_workspace_bytes(ctypes.byref(cache()), ctypes.byref(ragged()),
+    long = ragged(max_kv=64000, table_stride=1000)
+    need = L.wz_attention_workspace_bytes(ctypes.byref(cache()), ctypes.byref(long),
                                           ctypes.byref(serve._Attention(28, 1, 0, 0.1)))
     assert 0 < need <= 128 << 20 and need % 256 == 0
-    assert attend(L, ws=None) == NULL and attend(L, bytes=need - 1) == WORKSPACE and attend(L, ws=AT + 16) == WORKSPACE
+    assert attend(L, r=long, ws=None) == NULL and attend(L, r=long, bytes=need - 1) == WORKSPACE
+    assert attend(L, r=long, ws=AT + 16) == WORKSPACE
 
 
 def test_nothing_to_do(L):
