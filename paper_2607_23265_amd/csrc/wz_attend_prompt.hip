@@ -14,8 +14,8 @@
 //   O^T = V^T P   as they stand.  A column's maximum and sum are a lane's own
 //                 and one swap of halves.
 //
-// 16-byte chunks of a row in LDS are exchanged by the row's last three bits, so
-// that eight lanes that read eight rows hit all banks.
+// 16-byte chunks of a row in LDS are exchanged by the row's number, so that
+// sixteen lanes that read sixteen rows hit all 64 banks.
 #include "wz_attend.h"
 
 namespace wz {
@@ -26,6 +26,13 @@ typedef float f32x16 __attribute__((ext_vector_type(16)));
 constexpr int kWaves = 4;
 constexpr int kThreads = kWaves * kWave;
 constexpr int kRows = 32 * kWaves;
+
+// A running maximum is followed only once it is passed by this much (in powers
+// of two): the sums are rescaled on few tiles, and probabilities stay below 2^8.
+constexpr float kSlack = 8.f;
+
+// Classes of instructions for the scheduler.
+constexpr int kVector = 0x2, kProducts = 0x8;
 
 template <int D>
 struct Stages {
@@ -38,7 +45,7 @@ struct Stages {
 template <int D>
 __device__ __forceinline__ void attend_block(const AttendArgs& a, const Partition<kRows>& part, int h, int b, int kb,
                                              int off, int count, int slot, Stages<D>& lds) {
-  constexpr int KK = D / 16, DT = D / 32;
+  constexpr int KK = D / 16, DT = D / 32, kExchange = D / 8 - 1;
   constexpr int kKeyPieces = kTile * (D / 16) / kThreads, kValPieces = D * (kTile / 16) / kThreads;
   auto& kt = lds.k;
   auto& vt = lds.v;
@@ -58,12 +65,20 @@ __device__ __forceinline__ void attend_block(const AttendArgs& a, const Partitio
   int lo, hi;
   row_range(a, s, row, G, &lo, &hi);
   if (!valid) hi = 0;
+  // scores are compared before they are scaled, so the factor's sign goes to
+  // the query (exact)
+  const float scale2 = fabsf(a.scale2);
+  const uint32_t flip = a.scale2 < 0.f ? 0x80008000u : 0u;
   bf16x8 qf[KK];
   {
     const uint16_t* src =
         static_cast<const uint16_t*>(a.q) + int64_t(s.start + row / G) * a.q_stride + (h * G + row % G) * D + 8 * g;
 #pragma unroll
-    for (int k = 0; k < KK; ++k) qf[k] = valid ? *reinterpret_cast<const bf16x8*>(src + 16 * k) : bf16x8{};
+    for (int k = 0; k < KK; ++k) {
+      u32x4 u{};
+      if (valid) u = *reinterpret_cast<const u32x4*>(src + 16 * k);
+      qf[k] = __builtin_bit_cast(bf16x8, u ^ flip);
+    }
   }
   f32x16 o[DT];
 #pragma unroll
@@ -91,7 +106,7 @@ __device__ __forceinline__ void attend_block(const AttendArgs& a, const Partitio
     return x;
   };
   auto load = [&](int tile, const Pages& id) {
-    const int first = tile * kTile;
+    const int first = min(tile, T1 - 1) * kTile;
     const bool vin = uint32_t(id.v) < uint32_t(a.cache.pages);
     in_next = uint32_t(__ballot(vin)) & 0xfu;
 #pragma unroll
@@ -111,61 +126,77 @@ __device__ __forceinline__ void attend_block(const AttendArgs& a, const Partitio
     }
     __builtin_amdgcn_sched_barrier(0);
   };
-  auto store = [&](int buf, int tile) {
-    // values behind the sequence's end may be any bytes and must be zeros
-    if (tile * kTile + kTile > s.kv || in_next != 0xfu) {
-      const int count = in_next >> (tid % 4) & 1u ? min(max(s.kv - (tile * kTile + 16 * (tid % 4)), 0), 16) : 0;
+  // values behind the sequence's end may be any bytes and must be zeros
+  auto cut = [&](int tile) {
+    const int first = min(tile, T1 - 1) * kTile;
+    if (first + kTile > s.kv || in_next != 0xfu) {
+      const int count = in_next >> (tid % 4) & 1u ? min(max(s.kv - (first + 16 * (tid % 4)), 0), 16) : 0;
 #pragma unroll
       for (int i = 0; i < kValPieces; ++i) vx[i] = first_codes(vx[i], count);
     }
-#pragma unroll
-    for (int i = 0; i < kKeyPieces; ++i) {
+  };
+  auto store_piece = [&](int buf, int i) {  // keys' pieces, then values'
+    if (i < kKeyPieces) {
       const int p = tid + i * kThreads, tok = p / (D / 16), part16 = p % (D / 16);
       const int r = (tok & 32) | (tok & 16) | (tok & 4) << 1 | (tok & 8) >> 1 | (tok & 3);
       __bf16* at = kt[buf] + r * D;
-      *reinterpret_cast<bf16x8*>(at + 8 * ((2 * part16) ^ (r & 7))) = decode8(kx[i][0], kx[i][1], ks[i]);
-      *reinterpret_cast<bf16x8*>(at + 8 * ((2 * part16 + 1) ^ (r & 7))) = decode8(kx[i][2], kx[i][3], ks[i]);
-    }
-#pragma unroll
-    for (int i = 0; i < kValPieces; ++i) {
-      const int p = tid + i * kThreads, d = p / 4, part16 = p % 4;
+      *reinterpret_cast<bf16x8*>(at + 8 * ((2 * part16) ^ (r & kExchange))) = decode8(kx[i][0], kx[i][1], ks[i]);
+      *reinterpret_cast<bf16x8*>(at + 8 * ((2 * part16 + 1) ^ (r & kExchange))) = decode8(kx[i][2], kx[i][3], ks[i]);
+    } else if (i < kKeyPieces + kValPieces) {
+      const int k = i - kKeyPieces, p = tid + k * kThreads, d = p / 4, part16 = p % 4;
       __bf16* at = vt[buf] + d * kTile;
-      *reinterpret_cast<bf16x8*>(at + 8 * ((2 * part16) ^ (d & 7))) = decode8(vx[i][0], vx[i][1], vs);
-      *reinterpret_cast<bf16x8*>(at + 8 * ((2 * part16 + 1) ^ (d & 7))) = decode8(vx[i][2], vx[i][3], vs);
+      *reinterpret_cast<bf16x8*>(at + 8 * ((2 * part16) ^ (d >> 1 & 7))) = decode8(vx[k][0], vx[k][1], vs);
+      *reinterpret_cast<bf16x8*>(at + 8 * ((2 * part16 + 1) ^ (d >> 1 & 7))) = decode8(vx[k][2], vx[k][3], vs);
     }
   };
+  static_assert(kKeyPieces + kValPieces <= KK / 2, "a piece is stored with every batch of products");
 
-  uint32_t in = 0;
+  uint32_t in = 0, in_stored = 0;
   if (T0 < T1) {
-    const Pages now = pages(T0);
-    ids = pages(T0 + 1);
+    const Pages now = pages(T0), then = pages(T0 + 1);
+    ids = pages(T0 + 2);
     load(T0, now);
+    cut(T0);
+#pragma unroll
+    for (int i = 0; i < kKeyPieces + kValPieces; ++i) store_piece(0, i);
     in = in_next;
-    store(0, T0);
+    load(T0 + 1, then);
   }
   for (int tile = T0; tile < T1; ++tile) {
     const int buf = (tile - T0) & 1;
     __syncthreads();
-    const bool more = tile + 1 < T1;
-    if (more) {
+    cut(tile + 1);
+    // Scores.  Fragments are read from LDS four at a time, one batch ahead of
+    // its products; the next tile, which has arrived, goes to the other buffer
+    // between them.
+    f32x16 sc[2] = {};
+    bf16x8 f[2][4];
+    const __bf16* const keys = kt[buf] + c * D;
+    auto read_keys = [&](int j) {  // batch j of KK / 2: products 4 j .. 4 j + 3, by 32 tokens and then by 16 channels
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        f[j % 2][i] = *reinterpret_cast<const bf16x8*>(keys + (4 * j + i) / KK * 32 * D +
+                                                       8 * ((2 * ((4 * j + i) % KK) + g) ^ (c & kExchange)));
+      __builtin_amdgcn_sched_barrier(0);
+    };
+    read_keys(0);
+#pragma unroll
+    for (int j = 0; j < KK / 2; ++j) {
+      if (j + 1 < KK / 2) read_keys(j + 1);
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        sc[(4 * j + i) / KK] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f[j % 2][i], qf[(4 * j + i) % KK],
+                                                                       sc[(4 * j + i) / KK], 0, 0, 0);
+      store_piece(buf ^ 1, j);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    in_stored = in_next;
+    {
       const Pages now = ids;
-      ids = pages(tile + 2);
-      load(tile + 1, now);
+      ids = pages(tile + 3);
+      load(tile + 2, now);
     }
-    f32x16 sc[2];
-#pragma unroll
-    for (int t = 0; t < 2; ++t) {
-      sc[t] = f32x16{};
-      const __bf16* at = kt[buf] + (32 * t + c) * D;
-#pragma unroll
-      for (int k = 0; k < KK; ++k)
-        sc[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
-            *reinterpret_cast<const bf16x8*>(at + 8 * ((2 * k + g) ^ (c & 7))), qf[k], sc[t], 0, 0, 0);
-    }
-    const bool masked = tile * kTile < blk.full_lo || tile * kTile + kTile > blk.full_hi || in != 0xfu;
-#pragma unroll
-    for (int t = 0; t < 2; ++t) sc[t] *= a.scale2;
-    if (masked) {
+    if (tile * kTile < blk.full_lo || tile * kTile + kTile > blk.full_hi || in != 0xfu) {
 #pragma unroll
       for (int t = 0; t < 2; ++t)
 #pragma unroll
@@ -174,6 +205,7 @@ __device__ __forceinline__ void attend_block(const AttendArgs& a, const Partitio
           sc[t][i] = j >= lo && j < hi && (in >> (2 * t + i / 8) & 1u) ? sc[t][i] : -INFINITY;
         }
     }
+    in = in_stored;
     float top = -INFINITY;
 #pragma unroll
     for (int t = 0; t < 2; ++t)
@@ -181,35 +213,51 @@ __device__ __forceinline__ void attend_block(const AttendArgs& a, const Partitio
       for (int i = 0; i < 16; ++i) top = fmaxf(top, sc[t][i]);
     {
       const auto u = __builtin_amdgcn_permlane32_swap(__float_as_uint(top), __float_as_uint(top), false, false);
-      top = fmaxf(__uint_as_float(u[0]), __uint_as_float(u[1]));
+      top = fmaxf(__uint_as_float(u[0]), __uint_as_float(u[1])) * scale2;
     }
-    const float mx = fmaxf(m, top), use = mx == -INFINITY ? 0.f : mx;
-    if (__any(mx > m)) {
-      const float f = __builtin_amdgcn_exp2f(m - use);
+    if (__any(top > m + kSlack)) {
+      const float mx = fmaxf(m, top), f = __builtin_amdgcn_exp2f(m - (mx == -INFINITY ? 0.f : mx));
       l *= f;
 #pragma unroll
-      for (int d = 0; d < DT; ++d)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) o[d][i] *= f;
+      for (int d = 0; d < DT; ++d) o[d] *= f;
+      m = mx;
     }
-    m = mx;
+    const float use = m == -INFINITY ? 0.f : m;
+    // Products with the values, 16 tokens at a time, the probabilities of the
+    // next 16 between them.
+    bf16x8 p[2], v[2][DT];
+    auto read_values = [&](int u) {
 #pragma unroll
-    for (int u = 0; u < 4; ++u) {  // 16 tokens
-      bf16x8 p;
+      for (int d = 0; d < DT; ++d)
+        v[u % 2][d] = *reinterpret_cast<const bf16x8*>(vt[buf] + (32 * d + c) * kTile + 8 * ((2 * u + g) ^ (c >> 1 & 7)));
+      __builtin_amdgcn_sched_barrier(0);
+    };
+    auto probabilities = [&](int u) {
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        const float e = __builtin_amdgcn_exp2f(sc[u / 2][8 * (u % 2) + i] - use);
+        const float e = __builtin_amdgcn_exp2f(fmaf(sc[u / 2][8 * (u % 2) + i], scale2, -use));
         l += e;
-        p[i] = __bf16(e);
+        p[u % 2][i] = __bf16(e);
       }
+    };
+    read_values(0);
+    probabilities(0);
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      if (u < 3) read_values(u + 1);
 #pragma unroll
       for (int d = 0; d < DT; ++d)
-        o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
-            *reinterpret_cast<const bf16x8*>(vt[buf] + (32 * d + c) * kTile + 8 * ((2 * u + g) ^ (c & 7))), p, o[d], 0,
-            0, 0);
+        o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v[u % 2][d], p[u % 2], o[d], 0, 0, 0);
+      if (u < 3) probabilities(u + 1);
+      // products and vector work in turn
+#pragma unroll
+      for (int d = 0; d < DT; ++d) {
+        __builtin_amdgcn_sched_group_barrier(kProducts, 1, 0);
+        __builtin_amdgcn_sched_group_barrier(kVector, 32 / DT, 0);
+      }
+      __builtin_amdgcn_sched_barrier(0);
     }
-    if (more) store(buf ^ 1, tile + 1);
-    in = in_next;
   }
   {
     const auto u = __builtin_amdgcn_permlane32_swap(__float_as_uint(l), __float_as_uint(l), false, false);

@@ -366,13 +366,14 @@ AttendPlan attend_plan(const wz_cache& c, const wz_ragged& r, int q_heads) {
   const int G = q_heads / c.kv_heads;
   const int64_t rows = int64_t(r.max_tokens) * G;
   AttendPlan p{};
+  auto blocks = [&](int br) {
+    const int64_t each = (rows + br - 1) / br;
+    return std::min({int64_t(r.batch) * each, int64_t(r.tokens) * G / br + r.batch, int64_t(r.tokens) * G});
+  };
   p.block_rows = rows <= 16 ? 16 : rows <= 32 ? 32 : rows <= 64 ? 64 : 128;
-  const int64_t each = (rows + p.block_rows - 1) / p.block_rows;
-  const int64_t blocks = std::min({int64_t(r.batch) * each, int64_t(r.tokens) * G / p.block_rows + r.batch,
-                                   int64_t(r.tokens) * G});
-  p.blocks = int(std::min(blocks, int64_t(1) << 28));
+  p.blocks = int(std::min(blocks(p.block_rows), int64_t(1) << 28));
   const int64_t tiles = (int64_t(r.max_kv) + kTile - 1) / kTile;
-  p.workers = int(std::max<int64_t>(1, 2 * kCUs / c.kv_heads));  // two workgroups of four waves to a CU
+  p.workers = int(std::max<int64_t>(1, 2 * kCUs / c.kv_heads));  // as many as run at once
   p.shared = tiles > 24 && p.blocks * tiles < (int64_t(1) << 30) &&
              (p.block_rows > 64 ? p.blocks < p.workers : int64_t(p.blocks) * c.kv_heads < 2048);
   p.slots = p.blocks + p.workers;

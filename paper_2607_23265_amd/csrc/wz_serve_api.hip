@@ -142,7 +142,9 @@ wz_status wz_cache_attention(const wz_cache* cache, const wz_ragged* batch, cons
   }
   a.cache = *cache, a.batch = *batch, a.q = q, a.out = out, a.lse = lse;
   a.q_stride = q_stride, a.out_stride = out_stride;
-  a.scale2 = cfg->scale * 1.44269504088896341f;
+  // (not zero: a masked score of -inf has to stay what it is)
+  const float scale2 = cfg->scale * 1.44269504088896341f;
+  a.scale2 = std::copysign(std::max(std::fabs(scale2), 0x1p-126f), scale2);
   a.q_heads = cfg->q_heads, a.causal = cfg->causal, a.window = cfg->window;
   a.blocks = p.blocks, a.workers = p.workers, a.shared = p.shared;
   return from_hip(launch_attend(a, p, static_cast<hipStream_t>(stream)));
