@@ -55,7 +55,8 @@ __device__ __forceinline__ void attend_block(const AttendArgs& a, const Partitio
   const int T0 = blk.lo / kTile + off;
   const int T1 = min((max(blk.hi, blk.lo) + kTile - 1) / kTile, T0 + count);
 
-  const int tid = threadIdx.x, lane = __lane_id(), w = tid / kWave, c = lane & 31, g = lane >> 5;
+  const int tid = threadIdx.x, lane = __lane_id(), w = __builtin_amdgcn_readfirstlane(tid / kWave);
+  const int c = lane & 31, g = lane >> 5;
   const int P = a.cache.page_size, logP = __builtin_ctz(P);
   const uint8_t* const kc = static_cast<const uint8_t*>(a.cache.k);
   const uint8_t* const vc = static_cast<const uint8_t*>(a.cache.v);
@@ -85,85 +86,77 @@ __device__ __forceinline__ void attend_block(const AttendArgs& a, const Partitio
   for (int d = 0; d < DT; ++d) o[d] = f32x16{};
   float m = -INFINITY, l = 0.f;
 
-  // Staging: this thread's pieces of a tile, 16 codes each.  Nothing branches
-  // around a load: what lies behind the last tile is the last tile again, and a
-  // block of 16 tokens that has no page reads page 0 and is masked.
+  // Staging: this wave's pieces of a tile, 16 codes a lane.  A piece is of one
+  // block of 16 tokens, so its page and scale are the same in the whole wave and
+  // its lanes' offsets never change.  Nothing branches around a load: what lies
+  // behind the last tile is the last tile again, and a block that has no page
+  // reads page 0 and is masked.
   u32x4 kx[kKeyPieces], vx[kValPieces];
-  float ks[kKeyPieces], vs;
-  uint32_t in_next = 0;  // bit k: tokens 16 k .. of the tile loaded last lie in pages of the cache
-  struct Pages {
-    int k[kKeyPieces], v;
-  } ids;
+  float ks4 = 0.f, vs4 = 0.f;  // scales of block lane % 4
+  uint32_t in_next = 0;        // bit k: block k of the tile loaded last lies in a page of the cache
   const int* const row_of = a.batch.table + int64_t(b) * a.batch.table_stride;
   const int entries = max((s.kv + P - 1) >> logP, 1);
-  auto pages = [&](int tile) {
-    const int tok = min(tile, T1 - 1) * kTile;
-    Pages x;
-#pragma unroll
-    for (int i = 0; i < kKeyPieces; ++i)
-      x.k[i] = row_of[min((tok + (tid + i * kThreads) / (D / 16) / 16 * 16) >> logP, entries - 1)];
-    x.v = row_of[min((tok + 16 * (tid % 4)) >> logP, entries - 1)];
-    return x;
+  const int ktok = tid / (D / 16), kpart = tid % (D / 16);
+  const int koff = (ktok & 15) * D + 16 * kpart, voff = lane * P;
+  auto key_block = [&](int i) { return (w * kWave + i * kThreads) / D; };  // (tok / 16)
+  auto pages = [&](int tile) {  // of block lane % 4
+    return row_of[min((min(tile, T1 - 1) * kTile + 16 * (lane & 3)) >> logP, entries - 1)];
   };
-  auto load = [&](int tile, const Pages& id) {
+  auto load = [&](int tile, int id) {
     const int first = min(tile, T1 - 1) * kTile;
-    const bool vin = uint32_t(id.v) < uint32_t(a.cache.pages);
-    in_next = uint32_t(__ballot(vin)) & 0xfu;
+    const bool there = uint32_t(id) < uint32_t(a.cache.pages);
+    in_next = uint32_t(__ballot(there)) & 0xfu;
+    const int page = there ? id : 0;
+    const int64_t scale_at = int64_t(page) * Hkv + h;
+    ks4 = a.cache.k_scale[scale_at];
+    const float scale = a.cache.v_scale[scale_at];
+    vs4 = there ? scale : 1.f;
 #pragma unroll
     for (int i = 0; i < kKeyPieces; ++i) {
-      const int p = tid + i * kThreads, tok = p / (D / 16), part16 = p % (D / 16);
-      const int64_t at = int64_t(uint32_t(id.k[i]) < uint32_t(a.cache.pages) ? id.k[i] : 0) * Hkv + h;
-      kx[i] = *reinterpret_cast<const u32x4*>(kc + at * (P * D) + ((first + tok) & (P - 1)) * D + 16 * part16);
-      ks[i] = a.cache.k_scale[at];
+      const int blk16 = key_block(i), in_page = (first + 16 * blk16) & (P - 1);
+      const int64_t at = (int64_t(__builtin_amdgcn_readlane(page, blk16)) * Hkv + h) * (P * D) + in_page * D;
+      kx[i] = *reinterpret_cast<const u32x4*>(kc + at + koff);
     }
-    const int64_t at = int64_t(vin ? id.v : 0) * Hkv + h;
-    const float scale = a.cache.v_scale[at];
-    vs = vin ? scale : 1.f;
+    const int in_page = (first + 16 * w) & (P - 1);
+    const int64_t at = (int64_t(__builtin_amdgcn_readlane(page, w)) * Hkv + h) * (P * D) + in_page;
 #pragma unroll
-    for (int i = 0; i < kValPieces; ++i) {
-      const int p = tid + i * kThreads, d = p / 4;
-      vx[i] = *reinterpret_cast<const u32x4*>(vc + at * (P * D) + d * P + ((first + 16 * (p % 4)) & (P - 1)));
-    }
+    for (int i = 0; i < kValPieces; ++i) vx[i] = *reinterpret_cast<const u32x4*>(vc + at + 64 * i * P + voff);
     __builtin_amdgcn_sched_barrier(0);
   };
+  auto lane_of = [](float x, int i) { return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(x), i)); };
   // values behind the sequence's end may be any bytes and must be zeros
   auto cut = [&](int tile) {
     const int first = min(tile, T1 - 1) * kTile;
     if (first + kTile > s.kv || in_next != 0xfu) {
-      const int count = in_next >> (tid % 4) & 1u ? min(max(s.kv - (first + 16 * (tid % 4)), 0), 16) : 0;
+      const int count = in_next >> w & 1u ? min(max(s.kv - (first + 16 * w), 0), 16) : 0;
 #pragma unroll
       for (int i = 0; i < kValPieces; ++i) vx[i] = first_codes(vx[i], count);
     }
   };
   auto store_piece = [&](int buf, int i) {  // keys' pieces, then values'
     if (i < kKeyPieces) {
-      const int p = tid + i * kThreads, tok = p / (D / 16), part16 = p % (D / 16);
+      const int tok = ktok + i * (kThreads * 16 / D);
       const int r = (tok & 32) | (tok & 16) | (tok & 4) << 1 | (tok & 8) >> 1 | (tok & 3);
+      const float scale = lane_of(ks4, key_block(i));
       __bf16* at = kt[buf] + r * D;
-      *reinterpret_cast<bf16x8*>(at + 8 * ((2 * part16) ^ (r & kExchange))) = decode8(kx[i][0], kx[i][1], ks[i]);
-      *reinterpret_cast<bf16x8*>(at + 8 * ((2 * part16 + 1) ^ (r & kExchange))) = decode8(kx[i][2], kx[i][3], ks[i]);
+      *reinterpret_cast<bf16x8*>(at + 8 * ((2 * kpart) ^ (r & kExchange))) = decode8(kx[i][0], kx[i][1], scale);
+      *reinterpret_cast<bf16x8*>(at + 8 * ((2 * kpart + 1) ^ (r & kExchange))) = decode8(kx[i][2], kx[i][3], scale);
     } else if (i < kKeyPieces + kValPieces) {
-      const int k = i - kKeyPieces, p = tid + k * kThreads, d = p / 4, part16 = p % 4;
+      const int k = i - kKeyPieces, d = lane + 64 * k;
+      const float scale = lane_of(vs4, w);
       __bf16* at = vt[buf] + d * kTile;
-      *reinterpret_cast<bf16x8*>(at + 8 * ((2 * part16) ^ (d >> 1 & 7))) = decode8(vx[k][0], vx[k][1], vs);
-      *reinterpret_cast<bf16x8*>(at + 8 * ((2 * part16 + 1) ^ (d >> 1 & 7))) = decode8(vx[k][2], vx[k][3], vs);
+      *reinterpret_cast<bf16x8*>(at + 8 * ((2 * w) ^ (d >> 1 & 7))) = decode8(vx[k][0], vx[k][1], scale);
+      *reinterpret_cast<bf16x8*>(at + 8 * ((2 * w + 1) ^ (d >> 1 & 7))) = decode8(vx[k][2], vx[k][3], scale);
     }
   };
   static_assert(kKeyPieces + kValPieces <= KK / 2, "a piece is stored with every batch of products");
 
-  uint32_t in = 0, in_stored = 0;
-  if (T0 < T1) {
-    const Pages now = pages(T0), then = pages(T0 + 1);
-    ids = pages(T0 + 2);
-    load(T0, now);
-    cut(T0);
-#pragma unroll
-    for (int i = 0; i < kKeyPieces + kValPieces; ++i) store_piece(0, i);
-    in = in_next;
-    load(T0 + 1, then);
-  }
-  for (int tile = T0; tile < T1; ++tile) {
-    const int buf = (tile - T0) & 1;
+  uint32_t in = 0;
+  int ids = 0;
+  // One tile, in buffer `buf` (known to the compiler, which turns it into
+  // offsets of the instructions).
+  auto turn = [&](int tile, auto buffer) {
+    constexpr int buf = decltype(buffer)::value;
     __syncthreads();
     cut(tile + 1);
     // Scores.  Fragments are read from LDS four at a time, one batch ahead of
@@ -172,11 +165,11 @@ __device__ __forceinline__ void attend_block(const AttendArgs& a, const Partitio
     f32x16 sc[2] = {};
     bf16x8 f[2][4];
     const __bf16* const keys = kt[buf] + c * D;
-    auto read_keys = [&](int j) {  // batch j of KK / 2: products 4 j .. 4 j + 3, by 32 tokens and then by 16 channels
+    auto read_keys = [&](int j) {  // batch j of KK / 2: products 4 j .. 4 j + 3, the two halves of the tile in turn
 #pragma unroll
       for (int i = 0; i < 4; ++i)
-        f[j % 2][i] = *reinterpret_cast<const bf16x8*>(keys + (4 * j + i) / KK * 32 * D +
-                                                       8 * ((2 * ((4 * j + i) % KK) + g) ^ (c & kExchange)));
+        f[j % 2][i] = *reinterpret_cast<const bf16x8*>(keys + i % 2 * 32 * D +
+                                                       8 * ((2 * (2 * j + i / 2) + g) ^ (c & kExchange)));
       __builtin_amdgcn_sched_barrier(0);
     };
     read_keys(0);
@@ -185,14 +178,13 @@ __device__ __forceinline__ void attend_block(const AttendArgs& a, const Partitio
       if (j + 1 < KK / 2) read_keys(j + 1);
 #pragma unroll
       for (int i = 0; i < 4; ++i)
-        sc[(4 * j + i) / KK] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f[j % 2][i], qf[(4 * j + i) % KK],
-                                                                       sc[(4 * j + i) / KK], 0, 0, 0);
+        sc[i % 2] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f[j % 2][i], qf[2 * j + i / 2], sc[i % 2], 0, 0, 0);
       store_piece(buf ^ 1, j);
       __builtin_amdgcn_sched_barrier(0);
     }
-    in_stored = in_next;
+    const uint32_t in_stored = in_next;
     {
-      const Pages now = ids;
+      const int now = ids;
       ids = pages(tile + 3);
       load(tile + 2, now);
     }
@@ -257,6 +249,20 @@ __device__ __forceinline__ void attend_block(const AttendArgs& a, const Partitio
         __builtin_amdgcn_sched_group_barrier(kVector, 32 / DT, 0);
       }
       __builtin_amdgcn_sched_barrier(0);
+    }
+  };
+  if (T0 < T1) {
+    const int now = pages(T0), then = pages(T0 + 1);
+    ids = pages(T0 + 2);
+    load(T0, now);
+    cut(T0);
+#pragma unroll
+    for (int i = 0; i < kKeyPieces + kValPieces; ++i) store_piece(0, i);
+    in = in_next;
+    load(T0 + 1, then);
+    for (int tile = T0; tile < T1; tile += 2) {
+      turn(tile, std::integral_constant<int, 0>{});
+      if (tile + 1 < T1) turn(tile + 1, std::integral_constant<int, 1>{});
     }
   }
   {
