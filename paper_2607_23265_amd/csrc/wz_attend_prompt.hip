@@ -23,7 +23,7 @@ namespace {
 
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 
-constexpr int kWaves = 4;
+constexpr int kWaves = 4;  // of a group
 constexpr int kThreads = kWaves * kWave;
 constexpr int kRows = 32 * kWaves;
 
@@ -42,20 +42,23 @@ struct Stages {
 
 // Tiles [off, off + count) of block kb of sequence b, key/value head h; slot:
 // where its part goes, -1 if the block is this workgroup's alone.
-template <int D>
+// KG groups of four waves take the tiles in turn, each with stages of its own,
+// and add up at the end.
+template <int D, int KG>
 __device__ __forceinline__ void attend_block(const AttendArgs& a, const Partition<kRows>& part, int h, int b, int kb,
-                                             int off, int count, int slot, Stages<D>& lds) {
+                                             int off, int count, int slot, Stages<D> (&stages)[KG]) {
   constexpr int KK = D / 16, DT = D / 32, kExchange = D / 8 - 1;
   constexpr int kKeyPieces = kTile * (D / 16) / kThreads, kValPieces = D * (kTile / 16) / kThreads;
-  auto& kt = lds.k;
-  auto& vt = lds.v;
   const int Hkv = a.cache.kv_heads, G = part.G;
   const Seq s = sequence(a.batch, b);
   const Block blk = part.block(s, kb);
   const int T0 = blk.lo / kTile + off;
   const int T1 = min((max(blk.hi, blk.lo) + kTile - 1) / kTile, T0 + count);
 
-  const int tid = threadIdx.x, lane = __lane_id(), w = __builtin_amdgcn_readfirstlane(tid / kWave);
+  const int lane = __lane_id(), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+  const int w = wave % kWaves, group = wave / kWaves, tid = threadIdx.x % kThreads;
+  auto& kt = stages[group].k;
+  auto& vt = stages[group].v;
   const int c = lane & 31, g = lane >> 5;
   const int P = a.cache.page_size, logP = __builtin_ctz(P);
   const uint8_t* const kc = static_cast<const uint8_t*>(a.cache.k);
@@ -158,7 +161,8 @@ __device__ __forceinline__ void attend_block(const AttendArgs& a, const Partitio
   auto turn = [&](int tile, auto buffer) {
     constexpr int buf = decltype(buffer)::value;
     __syncthreads();
-    cut(tile + 1);
+    if (KG > 1 && tile >= T1) return;  // (the other group has one tile more)
+    cut(tile + KG);
     // Scores.  Fragments are read from LDS four at a time, one batch ahead of
     // its products; the next tile, which has arrived, goes to the other buffer
     // between them.
@@ -185,8 +189,8 @@ __device__ __forceinline__ void attend_block(const AttendArgs& a, const Partitio
     const uint32_t in_stored = in_next;
     {
       const int now = ids;
-      ids = pages(tile + 3);
-      load(tile + 2, now);
+      ids = pages(tile + 3 * KG);
+      load(tile + 2 * KG, now);
     }
     if (tile * kTile < blk.full_lo || tile * kTile + kTile > blk.full_hi || in != 0xfu) {
 #pragma unroll
@@ -252,22 +256,47 @@ __device__ __forceinline__ void attend_block(const AttendArgs& a, const Partitio
     }
   };
   if (T0 < T1) {
-    const int now = pages(T0), then = pages(T0 + 1);
-    ids = pages(T0 + 2);
-    load(T0, now);
-    cut(T0);
+    const int first = T0 + group, now = pages(first), then = pages(first + KG);
+    ids = pages(first + 2 * KG);
+    load(first, now);
+    cut(first);
 #pragma unroll
     for (int i = 0; i < kKeyPieces + kValPieces; ++i) store_piece(0, i);
     in = in_next;
-    load(T0 + 1, then);
-    for (int tile = T0; tile < T1; tile += 2) {
-      turn(tile, std::integral_constant<int, 0>{});
-      if (tile + 1 < T1) turn(tile + 1, std::integral_constant<int, 1>{});
+    load(first + KG, then);
+    for (int tile = T0; tile < T1; tile += 2 * KG) {  // (the same number of turns in every group)
+      turn(tile + group, std::integral_constant<int, 0>{});
+      if (tile + KG < T1) turn(tile + KG + group, std::integral_constant<int, 1>{});
     }
   }
   {
     const auto u = __builtin_amdgcn_permlane32_swap(__float_as_uint(l), __float_as_uint(l), false, false);
     l = __uint_as_float(u[0]) + __uint_as_float(u[1]);
+  }
+  if constexpr (KG > 1) {
+    static_assert(KG == 2, "");
+    __syncthreads();  // no stage is read any more: the second group leaves its sums in its own
+    float* const mine = reinterpret_cast<float*>(&stages[1]) + w * (DT * 16 * kWave) + lane;
+    __shared__ float ml[2][kThreads];
+    if (group == 1) {
+#pragma unroll
+      for (int d = 0; d < DT; ++d)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) mine[(16 * d + i) * kWave] = o[d][i];
+      ml[0][tid] = m, ml[1][tid] = l;
+    }
+    __syncthreads();
+    if (group == 1) return;
+    const float m1 = ml[0][tid], l1 = ml[1][tid], mx = fmaxf(m, m1);
+    // (a group without a score has a sum of 0, or of NaN if every score was)
+    const float f0 = m == -INFINITY ? l : __builtin_amdgcn_exp2f(m - mx);
+    const float f1 = m1 == -INFINITY ? l1 : __builtin_amdgcn_exp2f(m1 - mx);
+    l = (m == -INFINITY ? l : l * f0) + (m1 == -INFINITY ? l1 : l1 * f1);
+    m = mx;
+#pragma unroll
+    for (int d = 0; d < DT; ++d)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) o[d][i] = o[d][i] * f0 + mine[(16 * d + i) * kWave] * f1;
   }
   if (!valid) return;
   if (slot >= 0) {
@@ -294,23 +323,29 @@ __device__ __forceinline__ void attend_block(const AttendArgs& a, const Partitio
   if (a.lse && g == 0) a.lse[int64_t(t) * a.q_heads + head] = l == 0.f ? -INFINITY : m * kLn2 + logf(l);
 }
 
-template <int D>
-__global__ __launch_bounds__(kThreads, 2) void k_attend_prompt(AttendArgs a) {
-  __shared__ __align__(16) Stages<D> lds;
+template <int D, int KG>
+__global__ __launch_bounds__(KG* kThreads, 2) void k_attend_prompt(AttendArgs a) {
+  __shared__ __align__(16) Stages<D> stages[KG];
   const int Hkv = a.cache.kv_heads, h = blockIdx.x % Hkv, all = gridDim.x / Hkv;
   const Partition<kRows> part(a);
   // the last blocks first: in a causal batch they are the longest
   part.each_piece(all - 1 - int(blockIdx.x) / Hkv, [&](int b, int k, int off, int count, int slot) {
-    attend_block<D>(a, part, h, b, k, off, count, slot, lds);
+    attend_block<D, KG>(a, part, h, b, k, off, count, slot, stages);
   });
+}
+
+template <int D>
+void launch(const AttendArgs& a, const AttendPlan& p, hipStream_t s) {
+  const dim3 grid(uint32_t((p.shared ? p.workers : p.blocks) * a.cache.kv_heads));
+  if (p.groups == 2) hipLaunchKernelGGL((k_attend_prompt<D, 2>), grid, dim3(2 * kThreads), 0, s, a);
+  else hipLaunchKernelGGL((k_attend_prompt<D, 1>), grid, dim3(kThreads), 0, s, a);
 }
 
 }  // namespace
 
 hipError_t launch_attend_prompt(const AttendArgs& a, const AttendPlan& p, hipStream_t s) {
-  const dim3 grid(uint32_t((p.shared ? p.workers : p.blocks) * a.cache.kv_heads)), block(kThreads);
-  if (a.cache.head_dim == 128) hipLaunchKernelGGL((k_attend_prompt<128>), grid, block, 0, s, a);
-  else hipLaunchKernelGGL((k_attend_prompt<64>), grid, block, 0, s, a);
+  if (a.cache.head_dim == 128) launch<128>(a, p, s);
+  else launch<64>(a, p, s);
   return hipGetLastError();
 }
 

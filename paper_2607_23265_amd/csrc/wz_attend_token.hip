@@ -373,7 +373,12 @@ AttendPlan attend_plan(const wz_cache& c, const wz_ragged& r, int q_heads) {
   p.block_rows = rows <= 16 ? 16 : rows <= 32 ? 32 : rows <= 64 ? 64 : 128;
   p.blocks = int(std::min(blocks(p.block_rows), int64_t(1) << 28));
   const int64_t tiles = (int64_t(r.max_kv) + kTile - 1) / kTile;
-  p.workers = int(std::max<int64_t>(1, 2 * kCUs / c.kv_heads));  // as many as run at once
+  // A CU runs two workgroups of four waves at once, or one prompt workgroup of
+  // eight, which is faster while blocks are about as many as CUs or fewer
+  // (shared, it leaves half as many parts).
+  p.groups = int64_t(p.blocks) * c.kv_heads <= kCUs * 5 / 4 ? 2 : 1;
+  const int at_once = p.block_rows == 128 && p.groups == 2 ? kCUs : 2 * kCUs;
+  p.workers = int(std::max(1, at_once / c.kv_heads));
   p.shared = tiles > 24 && p.blocks * tiles < (int64_t(1) << 30) &&
              (p.block_rows > 64 ? p.blocks < p.workers : int64_t(p.blocks) * c.kv_heads < 2048);
   p.slots = p.blocks + p.workers;

@@ -90,7 +90,8 @@ struct AttendArgs {
   float* part_ml;    // shared: [slots][kv_heads][rows of a block][2] maximum (log2) and sum
 };
 struct AttendPlan {
-  int block_rows;    // rows of a block: 16, 32, 64 (token kernel) or more (prompt kernel)
+  int block_rows;    // rows of a block: 16, 32, 64 (token kernel) or 128 (prompt kernel)
+  int groups;        // prompt kernel: of four waves that take a block's tiles in turn
   int blocks;        // upper bound of the batch's blocks, for each key/value head
   int workers;       // shared: workgroups for each key/value head
   int slots;         // of the workspace, for each key/value head
