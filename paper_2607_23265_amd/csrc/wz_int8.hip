@@ -140,23 +140,25 @@ __device__ __forceinline__ void wait_loads() {
   asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(N) : "memory");
 }
 
-// Tiles of BM x BN, WM x WN waves, KB bytes of k at a time through ST stages of
+// Tiles of BM x BN, WM x WN waves, 128 bytes of k at a time through ST stages of
 // LDS that the loads write directly, ST - 1 stages ahead of the work.  KS such
-// groups of waves take the steps in turn and add up their integers at the end.  Chunks of 16 bytes are exchanged within a row by the row's number, so
-// that eight lanes that read eight rows hit all banks; the loads' lanes fetch
+// groups of waves take the steps in turn and add up their integers at the end.
+// Chunks of 16 bytes are exchanged within a row by the row's number, so that
+// sixteen lanes that read sixteen rows hit all 64 banks; the loads' lanes fetch
 // in that order.
-template <typename Out, int BM, int BN, int WM, int WN, int KB, int ST, int KS>
+constexpr int KB = 128;  // bytes of a row in a stage
+template <typename Out, int BM, int BN, int WM, int WN, int ST, int KS>
 __global__ __launch_bounds__(WM* WN* KS* kWave) void k_matmul_tile(MatmulArgs p, int tiles_m, int tiles_n) {
   constexpr int kWaves = WM * WN, MT = BM / WM / 32, NT = BN / WN / 32;
   constexpr int kChunks = KB / 16, kLoadRows = kWave / kChunks;  // chunks of a row, rows of one load
   constexpr int kLoadsA = BM / kLoadRows / kWaves, kLoadsB = BN / kLoadRows / kWaves;
-  static_assert((KB == 64 || KB == 128) && BM % (WM * 32) == 0 && BN % (WN * 32) == 0 &&
+  static_assert(BM % (WM * 32) == 0 && BN % (WN * 32) == 0 &&
                     BM % (kLoadRows * kWaves) == 0 && BN % (kLoadRows * kWaves) == 0, "");
   constexpr int kStage = (BM + BN) * KB;
   __shared__ __align__(16) int8_t lds[ST * KS * kStage];  // [ST][KS][rows of a, then of w][KB]
   const int lane = __lane_id(), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   const int w = wave % kWaves, group = wave / kWaves, c = lane & 31, g = lane >> 5;
-  auto exchange = [](int row) { return KB == 128 ? row & 7 : (row >> 1) & 3; };
+  auto exchange = [](int row) { return row >> 1 & 7; };
 
   // Workgroups go to the XCDs in turn: each XCD gets a run of tiles that lie
   // together (columns of 8 row tiles), whose rows and weights its L2 holds.
@@ -171,26 +173,31 @@ __global__ __launch_bounds__(WM* WN* KS* kWave) void k_matmul_tile(MatmulArgs p,
 
   // a row behind the last one is behind its buffer's end and reads as zeros;
   // so is, by its offset, what lies behind the end of a row
-  const int lr = lane / kChunks, lc = 16 * ((lane % kChunks) ^ exchange(lr));  // this lane's row and byte of a load
+  const int lr = lane / kChunks;  // this lane's row of a load
   i32x4 abuf = descriptor(p.a + int64_t(m0) * p.a_stride, min(BM, p.M - m0) * int(p.a_stride));
   i32x4 bbuf = descriptor(p.w + int64_t(n0) * p.w_stride, min(BN, p.N - n0) * int(p.w_stride));
   // a scalar register that the vector unit wrote may be a load's descriptor
   // five instructions later; the compiler does not look into the assembly
   asm volatile("s_nop 4" : "+s"(abuf), "+s"(bbuf));
-  int ao[kLoadsA], bo[kLoadsB];
+  int ao[kLoadsA], bo[kLoadsB], ac[kLoadsA], bc[kLoadsB];  // offsets, and bytes within the step
 #pragma unroll
-  for (int i = 0; i < kLoadsA; ++i) ao[i] = ((w * kLoadsA + i) * kLoadRows + lr) * int(p.a_stride) + lc;
+  for (int i = 0; i < kLoadsA; ++i) {
+    const int row = (w * kLoadsA + i) * kLoadRows + lr;
+    ac[i] = 16 * ((lane % kChunks) ^ exchange(row)), ao[i] = row * int(p.a_stride) + ac[i];
+  }
 #pragma unroll
-  for (int i = 0; i < kLoadsB; ++i) bo[i] = ((w * kLoadsB + i) * kLoadRows + lr) * int(p.w_stride) + lc;
+  for (int i = 0; i < kLoadsB; ++i) {
+    const int row = (w * kLoadsB + i) * kLoadRows + lr;
+    bc[i] = 16 * ((lane % kChunks) ^ exchange(row)), bo[i] = row * int(p.w_stride) + bc[i];
+  }
   const uint32_t base = lds_address(lds) + group * kStage;
   auto fetch = [&](int i, int s) {  // step s to stage i
     const int k = (s * KS + group) * KB;
-    const bool in = k + lc < p.K;
     const uint32_t to = base + i * KS * kStage;
 #pragma unroll
-    for (int x = 0; x < kLoadsA; ++x) load_to_lds(abuf, to + (w * kLoadsA + x) * 1024, in ? ao[x] : kOOB, k);
+    for (int x = 0; x < kLoadsA; ++x) load_to_lds(abuf, to + (w * kLoadsA + x) * 1024, k + ac[x] < p.K ? ao[x] : kOOB, k);
 #pragma unroll
-    for (int x = 0; x < kLoadsB; ++x) load_to_lds(bbuf, to + BM * KB + (w * kLoadsB + x) * 1024, in ? bo[x] : kOOB, k);
+    for (int x = 0; x < kLoadsB; ++x) load_to_lds(bbuf, to + BM * KB + (w * kLoadsB + x) * 1024, k + bc[x] < p.K ? bo[x] : kOOB, k);
   };
 
   i32x16 acc[MT][NT] = {};
@@ -257,11 +264,11 @@ __global__ __launch_bounds__(WM* WN* KS* kWave) void k_matmul_tile(MatmulArgs p,
   constexpr int kUnitBytes = kWaves * 32 * 128 <= (BM + BN) * KB && BN / WN * sizeof(Out) >= 128 ? 128 : 64;
   constexpr int kUnit = kUnitBytes / sizeof(Out);  // columns of a unit
   constexpr int kUnitChunks = kUnit * sizeof(Out) / 16, kPer = 16 / sizeof(Out);    // 16-byte chunks of its row, elements of one
-  static_assert(kWaves * 32 * kUnit * sizeof(Out) <= (BM + BN) * KB, "");
+  static_assert(kWaves * 32 * kUnit * sizeof(Out) <= (BM + BN) * KB && BN / WN % kUnit == 0, "");
   Out* const out = static_cast<Out*>(p.out);
   Out* const unit = reinterpret_cast<Out*>(lds) + w * 32 * kUnit;
   auto place = [&](int row, int chunk) {
-    return unit + row * kUnit + kPer * (chunk ^ (kUnitChunks == 8 ? row & 7 : (row >> 1) & (kUnitChunks - 1)));
+    return unit + row * kUnit + kPer * (chunk ^ (kUnitChunks == 8 ? row >> 1 & 7 : row >> 2 & 3));
   };
   float* const wsc = reinterpret_cast<float*>(lds + KS * kStage);  // [BN] scales, [BN] biases
   const int mw = m0 + (w / WN) * (BM / WM), nt = (w % WN) * (BN / WN);
@@ -334,12 +341,12 @@ __global__ __launch_bounds__(WM* WN* KS* kWave) void k_matmul_tile(MatmulArgs p,
   }
 }
 
-template <typename Out, int BM, int BN, int WM, int WN, int KB, int ST, int KS>
+template <typename Out, int BM, int BN, int WM, int WN, int ST, int KS>
 hipError_t tiles(const MatmulArgs& p, hipStream_t s) {
   const int64_t tm = (p.M + BM - 1) / BM, tn = (int64_t(p.N) + BN - 1) / BN;
   const int64_t groups = (tm * tn + kXcds - 1) / kXcds * kXcds;
   if (groups > 0x7fffffff) return hipErrorInvalidValue;
-  hipLaunchKernelGGL((k_matmul_tile<Out, BM, BN, WM, WN, KB, ST, KS>), dim3(uint32_t(groups)), dim3(WM * WN * KS * kWave),
+  hipLaunchKernelGGL((k_matmul_tile<Out, BM, BN, WM, WN, ST, KS>), dim3(uint32_t(groups)), dim3(WM * WN * KS * kWave),
                      0, s, p, int(tm), int(tn));
   return hipGetLastError();
 }
@@ -354,16 +361,16 @@ template <typename Out>
 hipError_t matmul(const MatmulArgs& p, hipStream_t s) {
   auto count = [&](int bm, int bn) { return (int64_t(p.M) + bm - 1) / bm * ((int64_t(p.N) + bn - 1) / bn); };
   auto turns = [&](int bm, int bn) { return double((count(bm, bn) + kCUs - 1) / kCUs); };
-  if (p.M <= 32 && count(32, 32) <= kCUs) return tiles<Out, 32, 32, 1, 1, 128, 4, 4>(p, s);
-  if (p.M <= 64 && count(64, 32) <= kCUs) return tiles<Out, 64, 32, 2, 1, 128, 3, 2>(p, s);
+  if (p.M <= 32 && count(32, 32) <= kCUs) return tiles<Out, 32, 32, 1, 1, 4, 4>(p, s);
+  if (p.M <= 64 && count(64, 32) <= kCUs) return tiles<Out, 64, 32, 2, 1, 3, 2>(p, s);
   const double n128 = turns(128, 128);
   const double t256 = 46 * turns(256, 256), t192 = 26 * turns(192, 128);
   const double t128 = 29 * std::floor(n128 / 2) + 18 * std::fmod(n128, 2), t64 = 6.4 * turns(64, 64);
   const double best = std::min({t256, t192, t128, t64});
-  if (best == t64) return tiles<Out, 64, 64, 2, 2, 128, 4, 1>(p, s);
-  if (best == t128) return tiles<Out, 128, 128, 2, 2, 128, 2, 1>(p, s);
-  if (best == t192) return tiles<Out, 192, 128, 2, 4, 128, 2, 1>(p, s);
-  return tiles<Out, 256, 256, 2, 4, 128, 2, 1>(p, s);
+  if (best == t64) return tiles<Out, 64, 64, 2, 2, 4, 1>(p, s);
+  if (best == t128) return tiles<Out, 128, 128, 2, 2, 2, 1>(p, s);
+  if (best == t192) return tiles<Out, 192, 128, 2, 4, 2, 1>(p, s);
+  return tiles<Out, 256, 256, 2, 4, 2, 1>(p, s);
 }
 
 }  // namespace
