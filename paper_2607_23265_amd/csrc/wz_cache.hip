@@ -14,105 +14,102 @@ namespace {
 
 constexpr int kThreads = 256;
 
-// Eight consecutive elements as fp32.
+// Eight consecutive elements as they lie in memory, and as fp32.
 template <typename In>
-__device__ __forceinline__ void load8(const In* p, float (&x)[8]) {
-  if constexpr (sizeof(In) == 2) {
-    const u32x4 u = *reinterpret_cast<const u32x4*>(p);
+struct Raw8 {
+  u32x4 u[sizeof(In) / 2];
+  __device__ __forceinline__ void load(const In* p) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) x[2 * i] = bf16_lo(u[i]), x[2 * i + 1] = bf16_hi(u[i]);
-  } else {
-    const f32x4 a = reinterpret_cast<const f32x4*>(p)[0], b = reinterpret_cast<const f32x4*>(p)[1];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) x[i] = a[i], x[4 + i] = b[i];
+    for (int i = 0; i < int(sizeof(In) / 2); ++i) u[i] = reinterpret_cast<const u32x4*>(p)[i];
   }
-}
+  __device__ __forceinline__ void get(float (&x)[8]) const {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      if constexpr (sizeof(In) == 2) x[i] = i % 2 ? bf16_hi(u[0][i / 2]) : bf16_lo(u[0][i / 2]);
+      else x[i] = __uint_as_float(u[i / 4][i % 4]);
+    }
+  }
+};
 template <typename In>
-__device__ __forceinline__ void load4(const In* p, float (&x)[4]) {
-  if constexpr (sizeof(In) == 2) {
-    const u32x2 u = *reinterpret_cast<const u32x2*>(p);
-    x[0] = bf16_lo(u[0]), x[1] = bf16_hi(u[0]), x[2] = bf16_lo(u[1]), x[3] = bf16_hi(u[1]);
-  } else {
-    const f32x4 a = *reinterpret_cast<const f32x4*>(p);
+struct Raw4 {
+  uint32_t u[sizeof(In)];
+  __device__ __forceinline__ void load(const In* p) {
+    if constexpr (sizeof(In) == 2) {
+      const u32x2 v = *reinterpret_cast<const u32x2*>(p);
+      u[0] = v[0], u[1] = v[1];
+    } else {
+      const u32x4 v = *reinterpret_cast<const u32x4*>(p);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) x[i] = a[i];
+      for (int i = 0; i < 4; ++i) u[i] = v[i];
+    }
   }
+  __device__ __forceinline__ float get(int i) const {
+    if constexpr (sizeof(In) == 2) return i % 2 ? bf16_hi(u[i / 2]) : bf16_lo(u[i / 2]);
+    else return __uint_as_float(u[i]);
+  }
+};
+
+// A head's row is shared by D / 16 lanes with two chunks of eight elements
+// each: lane j of the first rot_dim / 16 has the two halves of eight pairs
+// (interleaved: two chunks of four pairs each), the others two chunks that are
+// not rotated.
+struct Chunks {
+  int a, b;     // offsets in elements
+  bool turned;  // whether they are
+};
+__device__ __forceinline__ Chunks chunks_of(const wz_rotation& r, int lane) {
+  const int pairs = r.rot_dim / 16;
+  if (lane < pairs && !r.interleaved) return Chunks{8 * lane, 8 * lane + r.rot_dim / 2, true};
+  return Chunks{16 * lane, 16 * lane + 8, lane < pairs};
 }
 
-// Cosines and sines of COUNT frequencies from j on, for token t.
-template <int COUNT>
-__device__ __forceinline__ void angles(const wz_rotation& r, int tokens, int t, int j, float (&c)[COUNT],
-                                       float (&s)[COUNT]) {
-  auto row = [&](int f) {
-    int a = 0;
-    if (r.axes > 1) a = f < r.sections[0] ? 0 : f < r.sections[0] + r.sections[1] ? 1 : 2;
-    const int p = r.positions[int64_t(a) * tokens + t];
-    return min(max(p, 0), r.max_pos - 1);
-  };
-  const int half = r.rot_dim / 2;
+// The cosines and sines of a lane's eight frequencies for token t.
+struct Angles {
+  float c[8], s[8];
+};
+__device__ __forceinline__ void angles(const wz_rotation& r, int tokens, int t, int lane, Angles& x) {
+  const int half = r.rot_dim / 2, j = 8 * lane;
   auto section = [&](int f) {
     return r.axes == 1 ? 0 : f < r.sections[0] ? 0 : f < r.sections[0] + r.sections[1] ? 1 : 2;
   };
-  if (section(j) == section(j + COUNT - 1)) {
-    const float* p = r.table + int64_t(row(j)) * r.rot_dim + j;
+  auto row = [&](int axis) {
+    const int p = min(max(r.positions[int64_t(axis) * tokens + t], 0), r.max_pos - 1);
+    return r.table + int64_t(p) * r.rot_dim;
+  };
+  if (section(j) == section(j + 7)) {
+    const float* p = row(section(j)) + j;
 #pragma unroll
-    for (int i = 0; i < COUNT; i += 4) {
+    for (int i = 0; i < 8; i += 4) {
       const f32x4 u = *reinterpret_cast<const f32x4*>(p + i), w = *reinterpret_cast<const f32x4*>(p + half + i);
 #pragma unroll
-      for (int e = 0; e < 4; ++e) c[i + e] = u[e], s[i + e] = w[e];
+      for (int e = 0; e < 4; ++e) x.c[i + e] = u[e], x.s[i + e] = w[e];
     }
   } else {
-    for (int i = 0; i < COUNT; ++i) {
-      const float* p = r.table + int64_t(row(j + i)) * r.rot_dim + j + i;
-      c[i] = p[0], s[i] = p[half];
+    for (int i = 0; i < 8; ++i) {
+      const float* p = row(section(j + i)) + j + i;
+      x.c[i] = p[0], x.s[i] = p[half];
     }
   }
 }
 
-// The angles that the eight elements from 8 * chunk on turn by, and how.
-struct Turn {
-  int partner;  // offset in elements of the other halves of the pairs (0: inside the chunk, or none)
-  bool turned, second;
-  float c[8], s[8];  // interleaved: the first four
-};
-__device__ __forceinline__ Turn turn_of(const wz_rotation& r, int tokens, int t, int chunk) {
-  Turn u;
-  u.partner = 0, u.turned = chunk * 8 < r.rot_dim, u.second = false;
-  if (!u.turned) return u;
-  if (r.interleaved) {
-    float c[4], s[4];
-    angles<4>(r, tokens, t, chunk * 4, c, s);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) u.c[i] = c[i], u.s[i] = s[i];
-  } else {
-    const int half = r.rot_dim / 2;
-    u.second = chunk * 8 >= half;
-    u.partner = u.second ? -half : half;
-    angles<8>(r, tokens, t, chunk * 8 - (u.second ? half : 0), u.c, u.s);
-  }
-  return u;
-}
 // The rotated elements.  No fused multiply-add: a key rounds to the same code
 // wherever it is computed in plain fp32 products and sums.
-template <typename In>
-__device__ __forceinline__ void load_turned(const In* p, const Turn& u, bool interleaved, float (&x)[8]) {
+__device__ __forceinline__ void turn(const Angles& x, bool interleaved, float (&a)[8], float (&b)[8]) {
 #pragma clang fp contract(off)
-  load8(p, x);
-  if (!u.turned) return;
   if (interleaved) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const float a = x[2 * i], b = x[2 * i + 1];
-      x[2 * i] = a * u.c[i] - b * u.s[i];
-      x[2 * i + 1] = b * u.c[i] + a * u.s[i];
+    for (int i = 0; i < 8; ++i) {
+      float(&y)[8] = i < 4 ? a : b;
+      const float u = y[2 * (i % 4)], w = y[2 * (i % 4) + 1];
+      y[2 * (i % 4)] = u * x.c[i] - w * x.s[i];
+      y[2 * (i % 4) + 1] = w * x.c[i] + u * x.s[i];
     }
   } else {
-    float y[8];
-    load8(p + u.partner, y);
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      const float ac = x[i] * u.c[i], bs = y[i] * u.s[i];
-      x[i] = u.second ? ac + bs : ac - bs;
+      const float u = a[i], w = b[i];
+      a[i] = u * x.c[i] - w * x.s[i];
+      b[i] = w * x.c[i] + u * x.s[i];
     }
   }
 }
@@ -171,11 +168,12 @@ __device__ __forceinline__ uint32_t slots_mask(int s0, int lo, int hi) {
 
 template <typename In, int D, int P>
 __device__ void append_page(const AppendArgs& a, int b, const Seq& q, int nth, int h, char* smem) {
-  constexpr int kChunks = D / 8;               // chunks of 8 elements in a row
-  constexpr int kRows = kThreads / kChunks;    // rows the workgroup covers at once (keys)
+  constexpr int kLanes = D / 16;               // lanes of a key's row
+  constexpr int kRows = kThreads / kLanes;     // rows the workgroup covers at once (keys)
   constexpr int kPasses = (P + kRows - 1) / kRows;
   constexpr int kQuads = (P / 4) * (D / 4);    // 4 x 4 squares of values
   constexpr int kSquares = (kQuads + kThreads - 1) / kThreads;
+  constexpr int kSlots = kThreads / (D / 4) * 4;  // slots the workgroup covers at once (values)
   constexpr int kLd = P + 4;                   // bytes between channels of the turned values in LDS
   uint8_t* turned = reinterpret_cast<uint8_t*>(smem);            // [D][kLd]
   float* red = reinterpret_cast<float*>(smem + D * kLd);         // [8]
@@ -191,49 +189,73 @@ __device__ void append_page(const AppendArgs& a, int b, const Seq& q, int nth, i
   const int row0 = q.start + entry * P - q.place0;  // the call's row of slot 0
 
   for (int i = tid; i < P; i += kThreads) bad[i] = 0;
-  __syncthreads();
 
-  // keys: thread (chunk, row)
-  const int chunk = tid % kChunks, krow = tid / kChunks;
-  float kx[kPasses][8];
+  // All rows are asked for before the first is used; a slot that is not new
+  // reads a new one's row and leaves it (nothing branches around a load but
+  // for whole passes without a new slot).
+  auto row_of = [&](int slot) { return row0 + min(max(slot, s0), s1 - 1); };
+  auto empty = [&](int lo, int n) { return lo >= s1 || lo + n <= s0; };
+  // values: squares of 4 tokens x 4 channels, so that a token's four channels
+  // are one load and a channel's four tokens one store
+  Raw4<In> vr[kSquares][4];
+#pragma unroll
+  for (int i = 0; i < kSquares; ++i) {
+    if (empty(i * kSlots, kSlots)) continue;
+    const int sq = min(tid + i * kThreads, kQuads - 1), d = (sq % (D / 4)) * 4, t4 = (sq / (D / 4)) * 4;
+#pragma unroll
+    for (int r = 0; r < 4; ++r) vr[i][r].load(static_cast<const In*>(a.v) + row_of(t4 + r) * a.v_stride + h * D + d);
+  }
+  // keys: thread (lane of the row, row)
+  const int lane = tid % kLanes, krow = tid / kLanes;
+  const Chunks ch = chunks_of(a.turn, lane);
+  Raw8<In> kr[kPasses][2];
+#pragma unroll
+  for (int i = 0; i < kPasses; ++i) {
+    if (empty(i * kRows, kRows)) continue;
+    const In* src = static_cast<const In*>(a.k) + row_of(krow + i * kRows) * a.k_stride + h * D;
+    kr[i][0].load(src + ch.a), kr[i][1].load(src + ch.b);
+  }
+  __syncthreads();  // `bad` is clear
+  float kx[kPasses][2][8];
   float kmax = 0.f, vmax = 0.f;
 #pragma unroll
   for (int i = 0; i < kPasses; ++i) {
+    if (empty(i * kRows, kRows)) continue;
     const int slot = krow + i * kRows;
+    kr[i][0].get(kx[i][0]), kr[i][1].get(kx[i][1]);
+    if (ch.turned) {
+      Angles x;
+      angles(a.turn, a.batch.tokens, row_of(slot), lane, x);
+      turn(x, a.turn.interleaved, kx[i][0], kx[i][1]);
+    }
     if (slot >= s0 && slot < s1) {
-      const int t = row0 + slot;
-      const Turn u = turn_of(a.turn, a.batch.tokens, t, chunk);
-      load_turned(static_cast<const In*>(a.k) + t * a.k_stride + h * D + chunk * 8, u, a.turn.interleaved, kx[i]);
       bool nan = false;
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        if (finite(kx[i][e])) kmax = fmaxf(kmax, fabsf(kx[i][e]));
+      for (int e = 0; e < 16; ++e) {
+        const float x = kx[i][e / 8][e % 8];
+        if (finite(x)) kmax = fmaxf(kmax, fabsf(x));
         else nan = true;
       }
       if (nan) bad[slot] = 1;
     }
   }
-  // values: squares of 4 tokens x 4 channels, so that a token's four channels
-  // are one load and a channel's four tokens one store
   float vx[kSquares][4][4];
 #pragma unroll
   for (int i = 0; i < kSquares; ++i) {
-    const int sq = tid + i * kThreads, d = (sq % (D / 4)) * 4, t4 = (sq / (D / 4)) * 4;
+    const int sq = tid + i * kThreads, t4 = (sq / (D / 4)) * 4;
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
       const int slot = t4 + r;
+      const bool in = !empty(i * kSlots, kSlots) && sq < kQuads && slot >= s0 && slot < s1;
+      bool nan = false;
 #pragma unroll
-      for (int e = 0; e < 4; ++e) vx[i][r][e] = 0.f;
-      if (sq < kQuads && slot >= s0 && slot < s1) {
-        load4(static_cast<const In*>(a.v) + (row0 + slot) * a.v_stride + h * D + d, vx[i][r]);
-        bool nan = false;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          if (!finite(vx[i][r][e])) vx[i][r][e] = 0.f, nan = true;
-          vmax = fmaxf(vmax, fabsf(vx[i][r][e]));
-        }
-        if (nan) bad[slot] = 1;
+      for (int e = 0; e < 4; ++e) {
+        float x = in ? vr[i][r].get(e) : 0.f;
+        if (!finite(x)) x = 0.f, nan = true;
+        vmax = fmaxf(vmax, fabsf(x));
+        vx[i][r][e] = x;
       }
+      if (nan) bad[slot] = 1;
     }
   }
   block_max2(kmax, vmax, red);  // its barrier also covers `bad`
@@ -253,20 +275,23 @@ __device__ void append_page(const AppendArgs& a, int b, const Seq& q, int nth, i
   uint8_t* const kpage = static_cast<uint8_t*>(a.cache.k) + (int64_t(page) * Hkv + h) * P * D;
   uint8_t* const vpage = static_cast<uint8_t*>(a.cache.v) + (int64_t(page) * Hkv + h) * P * D;
   if (kmove != 1.f)
-    for (int i = tid; i < s0 * kChunks; i += kThreads) {
-      u32x2* p = reinterpret_cast<u32x2*>(kpage) + i;
-      const u32x2 u = *p;
-      *p = u32x2{rescaled4(u[0], kmove), rescaled4(u[1], kmove)};
+    for (int i = tid; i < s0 * (D / 16); i += kThreads) {
+      u32x4* p = reinterpret_cast<u32x4*>(kpage) + i;
+      const u32x4 u = *p;
+      *p = u32x4{rescaled4(u[0], kmove), rescaled4(u[1], kmove), rescaled4(u[2], kmove), rescaled4(u[3], kmove)};
     }
 #pragma unroll
   for (int i = 0; i < kPasses; ++i) {
     const int slot = krow + i * kRows;
     if (slot >= s0 && slot < s1) {
-      const float(&x)[8] = kx[i];
-      u32x2 u{e4m3x4(x[0] * kinv, x[1] * kinv, x[2] * kinv, x[3] * kinv),
-              e4m3x4(x[4] * kinv, x[5] * kinv, x[6] * kinv, x[7] * kinv)};
-      if (bad[slot]) u = u32x2{0x7f7f7f7fu, 0x7f7f7f7fu};
-      *reinterpret_cast<u32x2*>(kpage + slot * D + chunk * 8) = u;
+#pragma unroll
+      for (int c = 0; c < 2; ++c) {
+        const float(&x)[8] = kx[i][c];
+        u32x2 u{e4m3x4(x[0] * kinv, x[1] * kinv, x[2] * kinv, x[3] * kinv),
+                e4m3x4(x[4] * kinv, x[5] * kinv, x[6] * kinv, x[7] * kinv)};
+        if (bad[slot]) u = u32x2{0x7f7f7f7fu, 0x7f7f7f7fu};
+        *reinterpret_cast<u32x2*>(kpage + slot * D + (c ? ch.b : ch.a)) = u;
+      }
     }
   }
 #pragma unroll
@@ -280,6 +305,16 @@ __device__ void append_page(const AppendArgs& a, int b, const Seq& q, int nth, i
     }
   }
   __syncthreads();
+  // One or two new tokens: their bytes alone, without reading the pieces that
+  // they lie in (a wait for memory less: 21.1 -> 18.6 us for a token each of 141
+  // sequences and 16 heads).
+  if (s1 - s0 <= 2 && vmove == 1.f) {
+    for (int i = tid; i < D * (s1 - s0); i += kThreads) {
+      const int d = i % D, slot = s0 + i / D;
+      vpage[d * P + slot] = turned[d * kLd + slot];
+    }
+    return;
+  }
   constexpr int kPieces = D * (P / 16);
   for (int i = tid; i < kPieces; i += kThreads) {
     const int d = i / (P / 16), t16 = (i % (P / 16)) * 16;
@@ -303,25 +338,45 @@ __device__ void append_page(const AppendArgs& a, int b, const Seq& q, int nth, i
   }
 }
 
-// Query rows: thread (chunk, head group, token); it keeps its angles over the
-// heads it goes through.
+// Query rows: thread (lane of the row, head group, token); it keeps its angles
+// over the heads it goes through, four of them asked for at once.
 template <typename In, int D>
 __device__ void rotate_queries(const AppendArgs& a, int unit, int heads_at_once) {
-  constexpr int kChunks = D / 8;
-  const int chunk = threadIdx.x % kChunks, r = threadIdx.x / kChunks;
-  const int per = kThreads / kChunks / heads_at_once;
+  constexpr int kLanes = D / 16, kBatch = 4;
+  const int lane = threadIdx.x % kLanes, r = threadIdx.x / kLanes;
+  const int per = kThreads / kLanes / heads_at_once;
   const int t = unit * per + r / heads_at_once;
   if (t >= a.batch.tokens) return;
-  const Turn u = turn_of(a.turn, a.batch.tokens, t, chunk);
-  const In* src = static_cast<const In*>(a.q) + t * a.q_stride + chunk * 8;
-  uint16_t* dst = static_cast<uint16_t*>(a.q_out) + t * a.q_out_stride + chunk * 8;
-  for (int h = r % heads_at_once; h < a.q_heads; h += heads_at_once) {
-    float x[8];
-    load_turned(src + h * D, u, a.turn.interleaved, x);
-    u32x4 y;
+  const Chunks ch = chunks_of(a.turn, lane);
+  const In* src = static_cast<const In*>(a.q) + t * a.q_stride;
+  uint16_t* dst = static_cast<uint16_t*>(a.q_out) + t * a.q_out_stride;
+  Angles x;
+  bool known = false;
+  for (int h0 = r % heads_at_once; h0 < a.q_heads; h0 += kBatch * heads_at_once) {
+    Raw8<In> raw[kBatch][2];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) y[i] = f32_to_bf16_rne(x[2 * i]) | (f32_to_bf16_rne(x[2 * i + 1]) << 16);
-    *reinterpret_cast<u32x4*>(dst + h * D) = y;
+    for (int i = 0; i < kBatch; ++i) {
+      const int h = min(h0 + i * heads_at_once, a.q_heads - 1);
+      raw[i][0].load(src + h * D + ch.a), raw[i][1].load(src + h * D + ch.b);
+    }
+    if (!known && ch.turned) angles(a.turn, a.batch.tokens, t, lane, x);
+    known = true;
+#pragma unroll
+    for (int i = 0; i < kBatch; ++i) {
+      const int h = h0 + i * heads_at_once;
+      float y[2][8];
+      raw[i][0].get(y[0]), raw[i][1].get(y[1]);
+      if (ch.turned) turn(x, a.turn.interleaved, y[0], y[1]);
+      if (h < a.q_heads) {
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+          bf16x8 z;
+#pragma unroll
+          for (int e = 0; e < 8; ++e) z[e] = __bf16(y[c][e]);
+          *reinterpret_cast<bf16x8*>(dst + h * D + (c ? ch.b : ch.a)) = z;
+        }
+      }
+    }
   }
 }
 
@@ -366,10 +421,9 @@ hipError_t launch_append(const AppendArgs& a, int in_dtype, hipStream_t s) {
   const int64_t pages = std::min({int64_t(r.tokens), int64_t(r.batch) * ((r.max_tokens + P - 2) / P + 1),
                                   int64_t(r.tokens / P) + 2 * int64_t(r.batch)});
   const int64_t groups = pages * a.cache.kv_heads;
-  int heads_at_once = 1;
-  const int most = 4;
-  while (heads_at_once < most && heads_at_once < a.q_heads) heads_at_once *= 2;
-  const int per = kThreads / (D / 8) / heads_at_once;
+  int heads_at_once = 1;  // a thread has four heads or more where there are as many
+  while (heads_at_once < 8 && 4 * heads_at_once < a.q_heads) heads_at_once *= 2;
+  const int per = kThreads / (D / 16) / heads_at_once;
   const int64_t units = a.q ? (int64_t(r.tokens) + per - 1) / per : 0;
   if (groups + units > 0x7fffffff) return hipErrorInvalidValue;
   const bool bf = in_dtype == WZ_BF16;
