@@ -116,25 +116,27 @@ def attention(cache, start, kv_len, table, q, scale, causal=True, window=0):
             for j in np.flatnonzero(there):
                 p = table[b][j // P]
                 k[j], v[j] = K[p, h, j % P], V[p, h, :, j % P]
-            for i in range(n):
-                j = np.arange(total)
-                seen = there.copy()
-                if causal:
-                    seen &= j <= place0 + i
-                    if window:
-                        seen &= j > place0 + i - window
-                if not seen.any():
-                    continue
-                for g in range(h * G, (h + 1) * G):
-                    row = q[start[b] + i, g].astype(np.float64)
-                    s = k[seen] @ row * scale
-                    m = s.max()
-                    p = np.exp(s - m)
-                    total_p = p.sum()
-                    out[start[b] + i, g] = p @ v[seen] / total_p
-                    mag[start[b] + i, g] = p @ np.abs(v[seen]) / total_p
-                    lse[start[b] + i, g] = m + np.log(total_p)
-                    reach[start[b] + i, g] = (np.abs(k[seen]) @ np.abs(row)).max() * abs(scale)
+            j = np.arange(total)[None]
+            seen = np.broadcast_to(there[None], (n, total))
+            if causal:
+                place = place0 + np.arange(n)[:, None]
+                seen = seen & (j <= place)
+                if window:
+                    seen = seen & (j > place - window)
+            some = seen.any(1)
+            if not some.any():
+                continue
+            rows = start[b] + np.flatnonzero(some)
+            for g in range(h * G, (h + 1) * G):
+                x = q[rows, g].astype(np.float64)
+                with np.errstate(invalid="ignore"):
+                    s = np.where(seen[some], x @ k.T * scale, -np.inf)
+                    m = s.max(1, keepdims=True)
+                    p = np.where(seen[some], np.exp(s - m), 0.0)
+                    total_p = p.sum(1, keepdims=True)
+                    out[rows, g], mag[rows, g] = p @ v / total_p, p @ np.abs(v) / total_p
+                    lse[rows, g] = (m + np.log(total_p))[:, 0]
+                    reach[rows, g] = np.where(seen[some], np.abs(x) @ np.abs(k).T, 0.0).max(1) * abs(scale)
     return out, mag, lse, reach
 
 

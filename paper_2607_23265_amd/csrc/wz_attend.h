@@ -76,7 +76,7 @@ struct Partition {
       const Seq s = in ? sequence(a.batch, b0 + lane) : Seq{0, 0, 0, 0};
       const int mine = blocks(s);
       if constexpr (kUniform) {
-        const int each = tiles(s, 0), work = mine * each;
+        const int each = tiles(s, 0), work = a.shared ? mine * each : 0;  // (unshared, tiles are not asked for)
         const int ib = wave_incl_scan_i32(mine), it = wave_incl_scan_i32(work);
         const unsigned long long pass = __ballot(TILES ? nt + it > at : nb + ib > at);
         if (pass) {

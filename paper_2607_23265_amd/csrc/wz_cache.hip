@@ -412,26 +412,43 @@ hipError_t launch(const AppendArgs& a, int groups, int units, int heads_at_once,
 
 }  // namespace
 
-hipError_t launch_append(const AppendArgs& a, int in_dtype, hipStream_t s) {
-  const wz_ragged& r = a.batch;
-  const int P = a.cache.page_size, D = a.cache.head_dim;
-  if (r.tokens == 0 || r.max_tokens == 0) return hipSuccess;
+namespace {
+
+struct Grid {
+  int64_t groups, units;  // workgroups of pages, and of queries
+  int heads_at_once;
+};
+Grid append_grid(const wz_cache& c, const wz_ragged& r, int q_heads) {
+  const int P = c.page_size;
+  Grid g{};
   // pages that receive tokens: at most one a token, (n + P - 2) / P + 1 a
   // sequence, and tokens / P and two more a sequence together
-  const int64_t pages = std::min({int64_t(r.tokens), int64_t(r.batch) * ((r.max_tokens + P - 2) / P + 1),
-                                  int64_t(r.tokens / P) + 2 * int64_t(r.batch)});
-  const int64_t groups = pages * a.cache.kv_heads;
-  int heads_at_once = 1;  // a thread has four heads or more where there are as many
-  while (heads_at_once < 8 && 4 * heads_at_once < a.q_heads) heads_at_once *= 2;
-  const int per = kThreads / (D / 16) / heads_at_once;
-  const int64_t units = a.q ? (int64_t(r.tokens) + per - 1) / per : 0;
-  if (groups + units > 0x7fffffff) return hipErrorInvalidValue;
+  g.groups = c.kv_heads * std::min({int64_t(r.tokens), int64_t(r.batch) * ((r.max_tokens + P - 2) / P + 1),
+                                    int64_t(r.tokens / P) + 2 * int64_t(r.batch)});
+  g.heads_at_once = 1;  // a thread has four heads or more where there are as many
+  while (g.heads_at_once < 8 && 4 * g.heads_at_once < q_heads) g.heads_at_once *= 2;
+  const int per = kThreads / (c.head_dim / 16) / g.heads_at_once;
+  g.units = q_heads ? (int64_t(r.tokens) + per - 1) / per : 0;
+  return g;
+}
+
+}  // namespace
+
+int64_t append_groups(const wz_cache& c, const wz_ragged& r, int q_heads) {
+  const Grid g = append_grid(c, r, q_heads);
+  return g.groups + g.units;
+}
+
+hipError_t launch_append(const AppendArgs& a, int in_dtype, hipStream_t s) {
+  if (a.batch.tokens == 0 || a.batch.max_tokens == 0) return hipSuccess;
+  const Grid g = append_grid(a.cache, a.batch, a.q_heads);
+  const int groups = int(g.groups), units = int(g.units);
   const bool bf = in_dtype == WZ_BF16;
-  if (D == 128)
-    return bf ? launch<uint16_t, 128>(a, int(groups), int(units), heads_at_once, s)
-              : launch<float, 128>(a, int(groups), int(units), heads_at_once, s);
-  return bf ? launch<uint16_t, 64>(a, int(groups), int(units), heads_at_once, s)
-            : launch<float, 64>(a, int(groups), int(units), heads_at_once, s);
+  if (a.cache.head_dim == 128)
+    return bf ? launch<uint16_t, 128>(a, groups, units, g.heads_at_once, s)
+              : launch<float, 128>(a, groups, units, g.heads_at_once, s);
+  return bf ? launch<uint16_t, 64>(a, groups, units, g.heads_at_once, s)
+            : launch<float, 64>(a, groups, units, g.heads_at_once, s);
 }
 
 }  // namespace wz

@@ -72,6 +72,7 @@ struct AppendArgs {
   void* q_out;
   int q_heads;
 };
+int64_t append_groups(const wz_cache& c, const wz_ragged& r, int q_heads);  // workgroups it launches
 hipError_t launch_append(const AppendArgs& a, int in_dtype, hipStream_t s);
 
 struct AttendArgs {

@@ -9,6 +9,7 @@ using namespace wz;
 namespace {
 
 constexpr int kMostTokens = 1 << 24;
+constexpr int64_t kMostGroups = 1 << 23;  // workgroups of a launch: their threads have to stay below 2^32
 
 bool aligned(const void* p, uintptr_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
 wz_status check_ptr(const void* p, uintptr_t align) {
@@ -63,7 +64,7 @@ wz_status check_attention(const wz_cache* cache, const wz_ragged* batch, const w
       !std::isfinite(cfg->scale))
     return WZ_ERR_PARAM;
   const AttendPlan p = attend_plan(*cache, *batch, cfg->q_heads);
-  if (int64_t(p.slots) * cache->kv_heads * 16 > 0x7fffffff) return WZ_ERR_SHAPE;  // a grid's workgroups
+  if (int64_t(p.slots) * cache->kv_heads > kMostGroups) return WZ_ERR_SHAPE;
   return WZ_OK;
 }
 
@@ -97,6 +98,7 @@ wz_status wz_cache_append(const wz_cache* cache, const wz_ragged* batch, const w
     }
   }
   if (q && (q_heads < 1 || q_heads > 256 * 64)) return WZ_ERR_SHAPE;
+  if (append_groups(*cache, *batch, q ? q_heads : 0) > kMostGroups) return WZ_ERR_SHAPE;
   if (batch->tokens == 0 || batch->max_tokens == 0) return WZ_OK;
   WZ_TRY(check_arrays(*cache, *batch));
   if (rotation) {
@@ -167,7 +169,8 @@ wz_status wz_matmul_int(const int8_t* a, int64_t a_stride, const float* a_scale,
                         const float* w_scale, const float* bias, int32_t M, int32_t N, int32_t K, void* out,
                         int64_t out_stride, int32_t out_dtype, void* stream) {
   if (out_dtype != WZ_F32 && out_dtype != WZ_BF16) return WZ_ERR_DTYPE;
-  if (M < 0 || M >= kMostTokens || N < 1 || N >= kMostTokens || K < 16 || K > 65536 || K % 16 != 0)
+  if (M < 0 || M >= kMostTokens || N < 1 || N >= kMostTokens || K < 16 || K > 65536 || K % 16 != 0 ||
+      int64_t(M) * N > int64_t(1) << 38)
     return WZ_ERR_SHAPE;
   if (M == 0) return WZ_OK;
   WZ_TRY(check_rows(a, a_stride, K));

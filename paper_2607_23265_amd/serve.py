@@ -15,8 +15,9 @@ EXPORTS = ("wz_cache_append", "wz_cache_attention", "wz_attention_workspace_byte
            "wz_matmul_int")
 E4M3 = torch.float8_e4m3fn
 _DTYPE = {torch.float32: wz.WZ_F32, torch.bfloat16: wz.WZ_BF16}
-_FLOATS, _BF16, _INT8 = tuple(_DTYPE), (torch.bfloat16,), (torch.int8,)
+_FLOATS, _INT8 = tuple(_DTYPE), (torch.int8,)
 _P, _I, _L, _S = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_size_t
+_I3 = _I * 3
 
 
 class _Cache(ctypes.Structure):
@@ -34,7 +35,7 @@ class _Ragged(ctypes.Structure):
 class _Rotation(ctypes.Structure):
     """Mirror of wz_rotation."""
     _fields_ = [("table", _P), ("positions", _P), ("max_pos", _I), ("rot_dim", _I), ("axes", _I),
-                ("interleaved", _I), ("sections", _I * 3)]
+                ("interleaved", _I), ("sections", _I3)]
 
 
 class _Attention(ctypes.Structure):
@@ -72,16 +73,16 @@ def _dense(name, t, dtype, device=None):
     return t
 
 
-def _rows(name, t, heads, dim, device, dtypes):
-    """Row stride of t [tokens, heads, dim], whose heads must lie together."""
-    if (t.dim() != 3 or t.dtype not in dtypes or t.device != device or (heads and t.shape[1] != heads) or
-            t.shape[2] != dim):
-        raise ValueError(f"{name} must be [tokens, {heads or 'heads'}, {dim}] on {device}, of type " +
-                         " or ".join(map(str, dtypes)))
-    stride = t.stride()
-    if stride[2] != 1 or (stride[1] != dim and t.shape[1] > 1):
+def _rows(name, t, tokens, heads, dim, device, dtype):
+    """Row stride of t [tokens, heads, dim], whose heads must lie together (tokens, heads: None for any)."""
+    shape, stride = t.shape, t.stride()
+    if (len(shape) != 3 or shape[2] != dim or (heads is not None and shape[1] != heads) or
+            (tokens is not None and shape[0] != tokens) or t.dtype is not dtype or t.device != device):
+        raise ValueError(f"{name} must be [{'tokens' if tokens is None else tokens}, "
+                         f"{'heads' if heads is None else heads}, {dim}] on {device}, of type {dtype}")
+    if stride[2] != 1 or (stride[1] != dim and shape[1] > 1):
         raise ValueError(f"{name}: the heads of a row must lie together")
-    return stride[0] if t.shape[0] > 1 else max(stride[0], t.shape[1] * dim)
+    return stride[0] if shape[0] > 1 else max(stride[0], shape[1] * dim)
 
 
 # The current stream's handle without a torch.cuda.Stream made for it (0.1 us instead of 2, of a call's 10).
@@ -107,16 +108,15 @@ class PagedCache:
     __slots__ = ("k", "v", "k_scale", "v_scale", "device", "kv_heads", "head_dim", "page_size", "c")
 
     def __init__(self, k, v, k_scale, v_scale):
-        _dense("k", k, E4M3)
-        dev = self.device = k.device
+        dev = self.device = _dense("k", k, E4M3).device
         if k.dim() != 4:
             raise ValueError("k must be [pages, kv_heads, page_size, head_dim]")
         pages, heads, page, dim = k.shape
         if _dense("v", v, E4M3, dev).shape != (pages, heads, dim, page):
             raise ValueError("v must be [pages, kv_heads, head_dim, page_size]")
-        for name, t in (("k_scale", k_scale), ("v_scale", v_scale)):
-            if _dense(name, t, torch.float32, dev).shape != (pages, heads):
-                raise ValueError(f"{name} must be [pages, kv_heads]")
+        if (_dense("k_scale", k_scale, torch.float32, dev).shape != (pages, heads) or
+                _dense("v_scale", v_scale, torch.float32, dev).shape != (pages, heads)):
+            raise ValueError("k_scale and v_scale must be [pages, kv_heads]")
         self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
         self.kv_heads, self.head_dim, self.page_size = heads, dim, page
         self.c = _Cache(k.data_ptr(), v.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(), pages, heads, page, dim)
@@ -165,7 +165,7 @@ class Rotation:
         self.table, self.sections, self.interleaved = table, tuple(sections), bool(interleaved)
         padded = (*self.sections, 0, 0, 0)[:3]
         self.c = _Rotation(table.data_ptr(), None, table.shape[0], table.shape[1], max(1, len(self.sections)),
-                           int(self.interleaved), (_I * 3)(*padded))
+                           int(self.interleaved), _I3(*padded))
         if len(self.sections) == 1 and 2 * self.sections[0] != table.shape[1]:
             raise ValueError("the sections must sum to rot_dim / 2")
 
@@ -174,20 +174,19 @@ def cache_append(cache, batch, k, v, rotation=None, positions=None, q=None, q_ou
     """wz_cache_append: store the batch's new keys and values (k, v [tokens, kv_heads, head_dim] float32 or bfloat16),
     rotated by positions [axes, tokens] int32; returns the rotated queries [tokens, q_heads, head_dim] bfloat16 if q
     is given (into q_out if that is)."""
-    dev, dim, tokens = cache.device, cache.head_dim, k.shape[0]
-    types = (k.dtype,) if k.dtype in _DTYPE else _FLOATS
-    ks = _rows("k", k, cache.kv_heads, dim, dev, types)
-    vs = _rows("v", v, cache.kv_heads, dim, dev, types)
-    if v.shape[0] != tokens or batch.device != dev:
-        raise ValueError("k and v must have the same tokens, and the batch must be on their device")
+    dev, dim, tokens, dtype = cache.device, cache.head_dim, k.shape[0], k.dtype
+    if dtype not in _DTYPE or batch.device != dev:
+        raise ValueError("k must be float32 or bfloat16, and the batch on the cache's device")
+    ks = _rows("k", k, None, cache.kv_heads, dim, dev, dtype)
+    vs = _rows("v", v, tokens, cache.kv_heads, dim, dev, dtype)
+    q_at = out_at = None
     qs = qos = heads = 0
     if q is not None:
-        qs, heads = _rows("q", q, None, dim, dev, types), q.shape[1]
+        qs, heads = _rows("q", q, tokens, None, dim, dev, dtype), q.shape[1]
         if q_out is None:
-            q_out = q.new_empty(q.shape, dtype=torch.bfloat16)
-        qos = _rows("q_out", q_out, heads, dim, dev, _BF16)
-        if q.shape[0] != tokens or q_out.shape[0] != tokens:
-            raise ValueError("q and q_out must have the tokens of k")
+            q_out = q.new_empty((tokens, heads, dim), dtype=torch.bfloat16)
+        qos = _rows("q_out", q_out, tokens, heads, dim, dev, torch.bfloat16)
+        q_at, out_at = q.data_ptr(), q_out.data_ptr()
     turn = None
     if rotation is not None:
         if positions is None:
@@ -200,8 +199,7 @@ def cache_append(cache, batch, k, v, rotation=None, positions=None, q=None, q_ou
         turn.positions = positions.data_ptr()
         turn = ctypes.byref(turn)
     _call(dev, "wz_cache_append", lib().wz_cache_append, ctypes.byref(cache.c), batch.of(tokens), turn, k.data_ptr(),
-          ks, v.data_ptr(), vs, None if q is None else q.data_ptr(), qs, heads,
-          None if q is None else q_out.data_ptr(), qos, _DTYPE[k.dtype])
+          ks, v.data_ptr(), vs, q_at, qs, heads, out_at, qos, _DTYPE[dtype])
     return q_out if q is not None else None
 
 
@@ -216,12 +214,14 @@ def cache_attention(cache, batch, q, scale=None, causal=True, window=0, out=None
     defaults to head_dim ** -0.5; lse [tokens, q_heads] float32 receives the rows' log-sum-exp; ws is a uint8 workspace
     (allocated if not given and needed)."""
     dev, dim = cache.device, cache.head_dim
-    qs, tokens, heads = _rows("q", q, None, dim, dev, _BF16), q.shape[0], q.shape[1]
+    if batch.device != dev:
+        raise ValueError("the batch must be on the cache's device")
+    qs = _rows("q", q, None, None, dim, dev, torch.bfloat16)
+    tokens, heads = q.shape[0], q.shape[1]
     if out is None:
-        out = q.new_empty((tokens, heads, dim))
-    os_ = _rows("out", out, heads, dim, dev, _BF16)
-    if out.shape[0] != tokens or batch.device != dev:
-        raise ValueError("out must have the rows of q, and the batch must be on their device")
+        out, os_ = q.new_empty((tokens, heads, dim)), heads * dim
+    else:
+        os_ = _rows("out", out, tokens, heads, dim, dev, torch.bfloat16)
     if lse is not None and _dense("lse", lse, torch.float32, dev).shape != (tokens, heads):
         raise ValueError("lse must be [tokens, q_heads]")
     cfg = ctypes.byref(_Attention(heads, int(causal), window, dim ** -0.5 if scale is None else scale))

@@ -86,6 +86,17 @@ CASES = [
     ([70], [0], 1, 1, 128, 16, True, 0),
     ([70, 70], [1000, 70], 1, 1, 64, 64, False, 0),
     ([300], [1300], 1, 1, 64, 64, True, 1),              # each token sees itself
+    # long: several workgroups to a block, for each number of rows
+    ([1, 1, 1], [5000, 64, 1700], 2, 14, 128, 16, True, 0),
+    ([1] * 80, [1600 + 7 * i for i in range(80)], 1, 4, 64, 128, True, 0),
+    ([3, 1], [2500, 1601], 1, 8, 64, 64, True, 0),
+    ([12, 2], [1700, 3000], 1, 5, 128, 32, True, 900),
+    ([70, 5], [2100, 1600], 2, 4, 128, 64, True, 0),
+    ([96], [1700], 64, 512, 64, 64, True, 0),            # 384 blocks of a prompt
+    ([200, 70], [1800, 1900], 1, 3, 64, 16, False, 0),
+    ([90], [3000], 1, 2, 64, 32, True, 2000),
+    ([350, 200], [350, 201], 32, 128, 64, 64, True, 0),  # more blocks than workgroups run at once
+    ([1300], [1300], 1, 1, 64, 64, True, 0),             # blocks of 1 to 21 tiles
 ]
 
 
@@ -116,8 +127,8 @@ def test_loud_and_quiet_pages():
 
 
 def test_entries_without_a_page():
-    for new in (2, 90):
-        c = Case([new, new], [333, 200], 2, 64, 16, seed=22).fill()
+    for new, kv in ((2, 333), (90, 333), (2, 2000), (90, 2000)):
+        c = Case([new, new], [kv, 200], 2, 64, 16, seed=22).fill()
         c.table[0, 3], c.table[0, 20], c.table[1, :13] = -1, c.pages + 5, -3  # the second sequence has nothing at all
         _run(c, 4)
 
@@ -138,7 +149,7 @@ def test_not_numbers_stay_with_the_rows_that_see_them():
 
 def test_every_score_not_a_number():
     """Sequences whose every key is NaN, alone and shared by several workgroups."""
-    for new, kv in ((1, 40), (1, 3000), (70, 1000)):
+    for new, kv in ((1, 40), (1, 3000), (70, 1000), (70, 3000)):
         c = Case([new], [kv], 1, 64, 64, seed=24).fill()
         c.cache["k"][:] = 127
         out, lse = _run(c, 1)

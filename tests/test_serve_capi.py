@@ -155,6 +155,14 @@ def test_attention_arguments(L):
     assert attend(L, r=long, ws=AT + 16) == WORKSPACE
 
 
+def test_too_many_workgroups(L):
+    many = ragged(batch=65536, tokens=65536, max_tokens=1)
+    assert attend(L, c=cache(kv_heads=256), r=many, cfg=dict(q_heads=256), qs=256 * 128, os=256 * 128) == SHAPE
+    assert append(L, c=cache(kv_heads=256), r=many, ks=256 * 128, vs=256 * 128, q=None) == SHAPE
+    f = serve._Attention(256, 1, 0, 0.1)
+    assert L.wz_attention_workspace_bytes(ctypes.byref(cache(kv_heads=256)), ctypes.byref(many), ctypes.byref(f)) == 0
+
+
 def test_nothing_to_do(L):
     assert append(L, r=ragged(tokens=0), k=None, v=None) == OK
     assert attend(L, r=ragged(tokens=0), q=None) == OK
@@ -186,6 +194,7 @@ def test_int8_arguments(L):
         return L.wz_matmul_int(a, as_, sa, w, ws, sw, b, M, N, K, o, os_, dtype, None)
     assert mul(dtype=5) == DTYPE and mul(M=-1) == SHAPE and mul(N=0) == SHAPE and mul(K=20) == SHAPE
     assert mul(as_=48) == SHAPE and mul(ws=72) == SHAPE and mul(os_=4) == SHAPE and mul(K=65552, as_=70000) == SHAPE
+    assert mul(M=1 << 20, N=1 << 19, os_=1 << 19) == SHAPE
     assert mul(as_=(1 << 22) + 16) == SHAPE and mul(ws=(1 << 22) + 16) == SHAPE
     assert mul(a=None) == NULL and mul(w=AT + 8) == ALIGN and mul(sa=None) == NULL and mul(sw=AT + 2) == ALIGN
     assert mul(b=AT + 2) == ALIGN and mul(o=None) == NULL and mul(o=AT + 1) == ALIGN
