@@ -82,7 +82,7 @@ def _rows(name, t, tokens, heads, dim, device, dtype):
                          f"{'heads' if heads is None else heads}, {dim}] on {device}, of type {dtype}")
     if stride[2] != 1 or (stride[1] != dim and shape[1] > 1):
         raise ValueError(f"{name}: the heads of a row must lie together")
-    return stride[0] if shape[0] > 1 else max(stride[0], shape[1] * dim)
+    return stride[0] if shape[0] > 1 else shape[1] * dim  # (a single row has no stride)
 
 
 # The current stream's handle without a torch.cuda.Stream made for it (0.1 us instead of 2, of a call's 10).
@@ -243,7 +243,7 @@ def _matrix(name, t, dtypes, device=None):
     s = t.stride()
     if s[1] != 1 and t.shape[1] > 1:
         raise ValueError(f"{name}: the elements of a row must lie together")
-    return s[0] if t.shape[0] > 1 else max(s[0], t.shape[1])
+    return s[0] if t.shape[0] > 1 else t.shape[1]  # (a single row has no stride)
 
 
 def quantize_rows(x, out=None, scale=None):
@@ -251,11 +251,14 @@ def quantize_rows(x, out=None, scale=None):
     xs, dev = _matrix("x", x, _FLOATS), x.device
     rows, cols = x.shape
     if out is None:
-        out = x.new_empty((rows, cols), dtype=torch.int8)
+        out, qs = x.new_empty((rows, cols), dtype=torch.int8), cols
+    else:
+        qs = _matrix("out", out, _INT8, dev)
     if scale is None:
         scale = x.new_empty(rows, dtype=torch.float32)
-    qs = _matrix("out", out, _INT8, dev)
-    if out.shape != x.shape or _dense("scale", scale, torch.float32, dev).shape != (rows,):
+    else:
+        _dense("scale", scale, torch.float32, dev)
+    if out.shape != x.shape or scale.shape != (rows,):
         raise ValueError("out must have the shape of x, and scale [rows]")
     _call(dev, "wz_quantize_rows", lib().wz_quantize_rows, x.data_ptr(), xs, rows, cols, _DTYPE[x.dtype],
           out.data_ptr(), qs, scale.data_ptr())
@@ -276,10 +279,11 @@ def matmul_int(a, a_scale, w, w_scale, bias=None, out=None, out_dtype=torch.bflo
             (bias is not None and _dense("bias", bias, torch.float32, dev).numel() != N)):
         raise ValueError("a_scale must be [M], w_scale and bias [N]")
     if out is None:
-        out = a.new_empty((M, N), dtype=out_dtype)
-    os_ = _matrix("out", out, _FLOATS, dev)
-    if out.shape != (M, N):
-        raise ValueError("out must be [M, N]")
+        out, os_ = a.new_empty((M, N), dtype=out_dtype), N
+    else:
+        os_ = _matrix("out", out, _FLOATS, dev)
+    if out.shape != (M, N) or out.dtype not in _DTYPE:
+        raise ValueError("out must be [M, N] float32 or bfloat16")
     _call(dev, "wz_matmul_int", lib().wz_matmul_int, a.data_ptr(), as_, a_scale.data_ptr(), w.data_ptr(), ws,
           w_scale.data_ptr(), None if bias is None else bias.data_ptr(), M, N, K, out.data_ptr(), os_,
           _DTYPE[out.dtype])

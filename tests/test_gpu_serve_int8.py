@@ -89,6 +89,18 @@ def test_no_rows():
     assert y.shape == (0, 5) and q.shape == (0, 64)
 
 
+def test_one_row_of_a_matrix_of_any_stride():
+    x = torch.randn(3, 67, device=DEV)
+    q, s = serve.quantize_rows(x[:1, :64])
+    want, scale = so.quantize_rows(x[:1, :64].cpu().numpy())
+    w = torch.randint(-9, 9, (5, 67), dtype=torch.int8, device=DEV)[:1, :64]
+    y = serve.matmul_int(q, s, w, torch.ones(1, device=DEV), out=torch.empty(3, 7, device=DEV)[:1, :1])
+    torch.cuda.synchronize()
+    np.testing.assert_array_equal(q.cpu().numpy(), want)
+    ref = so.matmul_int(want, scale, w.cpu().numpy(), np.ones(1, np.float32))[0]
+    np.testing.assert_allclose(y.cpu().numpy(), ref, rtol=2.0 ** -21)
+
+
 def test_not_a_number_row():
     x = torch.ones(3, 64, device=DEV)
     x[1, 7] = float("nan")
