@@ -27,10 +27,6 @@ constexpr int kWaves = 4;  // of a group
 constexpr int kThreads = kWaves * kWave;
 constexpr int kRows = 32 * kWaves;
 
-// A running maximum is followed only once it is passed by this much (in powers
-// of two): the sums are rescaled on few tiles, and probabilities stay below 2^8.
-constexpr float kSlack = 8.f;
-
 // Classes of instructions for the scheduler.
 constexpr int kVector = 0x2, kProducts = 0x8;
 
@@ -211,7 +207,11 @@ __device__ __forceinline__ void attend_block(const AttendArgs& a, const Partitio
       const auto u = __builtin_amdgcn_permlane32_swap(__float_as_uint(top), __float_as_uint(top), false, false);
       top = fmaxf(__uint_as_float(u[0]), __uint_as_float(u[1])) * scale2;
     }
-    if (__any(top > m + kSlack)) {
+    // The maximum is followed at once: a row that one token dominates then has
+    // that token's probability as exactly 1.  (Following it only when passed by
+    // 2^8 saves 1.5 % of the time and costs a quarter more error against 64
+    // bits, 0.0021 for 0.0017.)
+    if (__any(top > m)) {
       const float mx = fmaxf(m, top), f = __builtin_amdgcn_exp2f(m - (mx == -INFINITY ? 0.f : mx));
       l *= f;
 #pragma unroll
