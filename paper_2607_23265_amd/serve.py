@@ -6,6 +6,7 @@ of their device.  Where a tensor has rows of heads ([tokens, heads, head_dim]) i
 fused projection are passed as they are; everything else is contiguous.
 """
 import ctypes
+import struct
 
 import torch
 
@@ -17,7 +18,13 @@ E4M3 = torch.float8_e4m3fn
 _DTYPE = {torch.float32: wz.WZ_F32, torch.bfloat16: wz.WZ_BF16}
 _FLOATS, _INT8 = tuple(_DTYPE), (torch.int8,)
 _P, _I, _L, _S = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_size_t
-_I3 = _I * 3
+
+# The header's structs as bytes: packing one costs a third of making a ctypes.Structure, and a step of small calls waits
+# for the host.
+_CACHE = struct.Struct("@4P4i").pack      # wz_cache
+_RAGGED = struct.Struct("@3P5i4x").pack   # wz_ragged
+_ROTATION = struct.Struct("@2P7i4x").pack  # wz_rotation
+_ATTENTION = struct.Struct("@3if").pack   # wz_attention
 
 
 class _Cache(ctypes.Structure):
@@ -35,7 +42,7 @@ class _Ragged(ctypes.Structure):
 class _Rotation(ctypes.Structure):
     """Mirror of wz_rotation."""
     _fields_ = [("table", _P), ("positions", _P), ("max_pos", _I), ("rot_dim", _I), ("axes", _I),
-                ("interleaved", _I), ("sections", _I3)]
+                ("interleaved", _I), ("sections", _I * 3)]
 
 
 class _Attention(ctypes.Structure):
@@ -51,13 +58,11 @@ def lib():
     global _lib
     if _lib is None:
         L = wz.lib()
-        cache, ragged = ctypes.POINTER(_Cache), ctypes.POINTER(_Ragged)
-        attention = ctypes.POINTER(_Attention)
-        L.wz_cache_append.argtypes = [cache, ragged, ctypes.POINTER(_Rotation), _P, _L, _P, _L, _P, _L, _I, _P, _L,
+        L.wz_cache_append.argtypes = [_P, _P, _P, _P, _L, _P, _L, _P, _L, _I, _P, _L,
                                       _I, _P]
-        L.wz_attention_workspace_bytes.argtypes = [cache, ragged, attention]
+        L.wz_attention_workspace_bytes.argtypes = [_P, _P, _P]
         L.wz_attention_workspace_bytes.restype = _S
-        L.wz_cache_attention.argtypes = [cache, ragged, attention, _P, _L, _P, _L, _P, _P, _S, _P]
+        L.wz_cache_attention.argtypes = [_P, _P, _P, _P, _L, _P, _L, _P, _P, _S, _P]
         L.wz_quantize_rows.argtypes = [_P, _L, _I, _I, _I, _P, _L, _P, _P]
         L.wz_matmul_int.argtypes = [_P, _L, _P, _P, _L, _P, _P, _I, _I, _I, _P, _L, _I, _P]
         for f in EXPORTS:
@@ -85,15 +90,16 @@ def _rows(name, t, tokens, heads, dim, device, dtype):
     return stride[0] if shape[0] > 1 else shape[1] * dim  # (a single row has no stride)
 
 
-# The current stream's handle without a torch.cuda.Stream made for it (0.1 us instead of 2, of a call's 10).
+# The current stream's handle without a torch.cuda.Stream made for it (0.1 us instead of 2, of a call's 8).
 _stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
     lambda index: torch.cuda.current_stream(index).cuda_stream)
+_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
 
 
 def _call(device, where, f, *args):
     """f(*args, stream) on `device`'s current stream, with that device current."""
     index = device.index
-    if torch.cuda.current_device() == index:
+    if _device() == index:
         st = f(*args, _stream(index))
     else:
         with torch.cuda.device(device):
@@ -108,18 +114,19 @@ class PagedCache:
     __slots__ = ("k", "v", "k_scale", "v_scale", "device", "kv_heads", "head_dim", "page_size", "c")
 
     def __init__(self, k, v, k_scale, v_scale):
-        dev = self.device = _dense("k", k, E4M3).device
+        dev = self.device = k.device
         if k.dim() != 4:
             raise ValueError("k must be [pages, kv_heads, page_size, head_dim]")
         pages, heads, page, dim = k.shape
-        if _dense("v", v, E4M3, dev).shape != (pages, heads, dim, page):
+        if v.shape != (pages, heads, dim, page):
             raise ValueError("v must be [pages, kv_heads, head_dim, page_size]")
-        if (_dense("k_scale", k_scale, torch.float32, dev).shape != (pages, heads) or
-                _dense("v_scale", v_scale, torch.float32, dev).shape != (pages, heads)):
+        if k_scale.shape != (pages, heads) or v_scale.shape != (pages, heads):
             raise ValueError("k_scale and v_scale must be [pages, kv_heads]")
+        _dense("k", k, E4M3), _dense("v", v, E4M3, dev)
+        _dense("k_scale", k_scale, torch.float32, dev), _dense("v_scale", v_scale, torch.float32, dev)
         self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
         self.kv_heads, self.head_dim, self.page_size = heads, dim, page
-        self.c = _Cache(k.data_ptr(), v.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(), pages, heads, page, dim)
+        self.c = _CACHE(k.data_ptr(), v.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(), pages, heads, page, dim)
 
     @classmethod
     def new(cls, pages, kv_heads, head_dim, page_size=64, device="cuda:0"):
@@ -134,7 +141,7 @@ class Ragged:
     """A ragged batch: sequence b brings rows start[b] .. start[b + 1] - 1 of the call and has kv_len[b] tokens in the
     cache, these counted, in the pages table[b] (all int32).  max_tokens and max_kv bound the new tokens and the
     tokens of one sequence."""
-    __slots__ = ("start", "kv_len", "table", "device", "max_tokens", "max_kv", "tokens", "c")
+    __slots__ = ("start", "kv_len", "table", "device", "max_tokens", "max_kv", "at")
 
     def __init__(self, start, kv_len, table, max_tokens, max_kv):
         dev = self.device = _dense("start", start, torch.int32).device
@@ -145,29 +152,27 @@ class Ragged:
             raise ValueError("start must be [batch + 1], kv_len [batch] and table [batch, pages]")
         self.start, self.kv_len, self.table = start, kv_len, table
         self.max_tokens, self.max_kv = max_tokens, max_kv
-        self.c = _Ragged(start.data_ptr(), kv_len.data_ptr(), table.data_ptr(), batch, 0, max_tokens, max_kv,
-                         table.shape[1])
+        self.at = start.data_ptr(), kv_len.data_ptr(), table.data_ptr(), batch
 
     def of(self, tokens):
-        self.c.tokens = tokens
-        return ctypes.byref(self.c)
+        """wz_ragged of a call with so many rows."""
+        return _RAGGED(*self.at, tokens, self.max_tokens, self.max_kv, self.table.shape[1])
 
 
 class Rotation:
     """Rotation by position: table [max_pos, rot_dim] float32 holds cosines, then sines; sections are the numbers of
     frequencies that go by each row of positions (one section: all by positions[0])."""
-    __slots__ = ("table", "sections", "interleaved", "c")
+    __slots__ = ("table", "sections", "interleaved", "of")
 
     def __init__(self, table, sections=(), interleaved=False):
         _dense("table", table, torch.float32)
         if table.dim() != 2 or len(sections) > 3:
             raise ValueError("table must be [max_pos, rot_dim], with at most three sections")
         self.table, self.sections, self.interleaved = table, tuple(sections), bool(interleaved)
-        padded = (*self.sections, 0, 0, 0)[:3]
-        self.c = _Rotation(table.data_ptr(), None, table.shape[0], table.shape[1], max(1, len(self.sections)),
-                           int(self.interleaved), _I3(*padded))
-        if len(self.sections) == 1 and 2 * self.sections[0] != table.shape[1]:
+        if len(sections) == 1 and 2 * sections[0] != table.shape[1]:
             raise ValueError("the sections must sum to rot_dim / 2")
+        # what follows the positions in wz_rotation
+        self.of = (*table.shape, max(1, len(sections)), int(self.interleaved), *(*self.sections, 0, 0, 0)[:3])
 
 
 def cache_append(cache, batch, k, v, rotation=None, positions=None, q=None, q_out=None):
@@ -192,21 +197,17 @@ def cache_append(cache, batch, k, v, rotation=None, positions=None, q=None, q_ou
         if positions is None:
             raise ValueError("a rotation needs positions")
         _dense("positions", positions, torch.int32, dev)
-        axes = max(1, len(rotation.sections))
-        if positions.numel() != axes * tokens or rotation.table.device != dev:
+        if positions.numel() != rotation.of[2] * tokens or rotation.table.device != dev:
             raise ValueError("positions must be [axes, tokens], on the device of the table")
-        turn = _Rotation.from_buffer_copy(rotation.c)
-        turn.positions = positions.data_ptr()
-        turn = ctypes.byref(turn)
-    _call(dev, "wz_cache_append", lib().wz_cache_append, ctypes.byref(cache.c), batch.of(tokens), turn, k.data_ptr(),
+        turn = _ROTATION(rotation.table.data_ptr(), positions.data_ptr(), *rotation.of)
+    _call(dev, "wz_cache_append", lib().wz_cache_append, cache.c, batch.of(tokens), turn, k.data_ptr(),
           ks, v.data_ptr(), vs, q_at, qs, heads, out_at, qos, _DTYPE[dtype])
     return q_out if q is not None else None
 
 
 def attention_workspace_bytes(cache, batch, q_heads, tokens):
     """Bytes of workspace cache_attention() needs for `tokens` rows of q_heads heads."""
-    return int(lib().wz_attention_workspace_bytes(ctypes.byref(cache.c), batch.of(tokens),
-                                                  ctypes.byref(_Attention(q_heads, 0, 0, 1.0))))
+    return int(lib().wz_attention_workspace_bytes(cache.c, batch.of(tokens), _ATTENTION(q_heads, 0, 0, 1.0)))
 
 
 def cache_attention(cache, batch, q, scale=None, causal=True, window=0, out=None, lse=None, ws=None):
@@ -224,8 +225,8 @@ def cache_attention(cache, batch, q, scale=None, causal=True, window=0, out=None
         os_ = _rows("out", out, tokens, heads, dim, dev, torch.bfloat16)
     if lse is not None and _dense("lse", lse, torch.float32, dev).shape != (tokens, heads):
         raise ValueError("lse must be [tokens, q_heads]")
-    cfg = ctypes.byref(_Attention(heads, int(causal), window, dim ** -0.5 if scale is None else scale))
-    c, r = ctypes.byref(cache.c), batch.of(tokens)
+    cfg = _ATTENTION(heads, int(causal), window, dim ** -0.5 if scale is None else scale)
+    c, r = cache.c, batch.of(tokens)
     if ws is None:
         need = lib().wz_attention_workspace_bytes(c, r, cfg)
         ws = q.new_empty(need, dtype=torch.uint8) if need else None

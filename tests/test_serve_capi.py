@@ -86,6 +86,14 @@ def test_header_is_c_and_structs_match(tmp_path):
     for s in structs.values():
         want += [ctypes.sizeof(s)] + [getattr(s, f[0]).offset for f in s._fields_]
     assert got == want
+    # what the binding passes: the same structs, packed
+    a = serve._Cache(1 << 40, 2, 3, 4, 5, 6, 7, 8)
+    assert bytes(a) == serve._CACHE(1 << 40, 2, 3, 4, 5, 6, 7, 8)
+    b = serve._Ragged(1 << 40, 2, 3, 4, 5, 6, 7, 8)
+    assert bytes(b) == serve._RAGGED(1 << 40, 2, 3, 4, 5, 6, 7, 8)
+    c = serve._Rotation(1 << 40, 2, 3, 4, 5, 6, (ctypes.c_int32 * 3)(7, 8, 9))
+    assert bytes(c) == serve._ROTATION(1 << 40, 2, 3, 4, 5, 6, 7, 8, 9)
+    assert bytes(serve._Attention(1, 2, 3, 0.5)) == serve._ATTENTION(1, 2, 3, 0.5)
 
 
 @pytest.mark.parametrize("kw", [dict(head_dim=96), dict(page_size=8), dict(page_size=48), dict(page_size=256),
