@@ -60,8 +60,8 @@ typedef struct {
  * [0, tokens], a negative length, an n_b above max_tokens or a kv_len above
  * max_kv is cut to that range, and a page number outside [0, pages) is never
  * followed: its tokens are neither stored nor attended to.  New tokens at a
- * negative place (n_b > kv_len[b]) are not stored and their output rows are
- * zero.  Distinct sequences may share pages only if none of them is appended
+ * negative place (n_b > kv_len[b]) are not stored, and where attention is
+ * causal their rows see nothing.  Distinct sequences may share pages only if none of them is appended
  * to in the call.  A call is refused (WZ_ERR_SHAPE) where its bounds would take
  * more than 2^23 workgroups (pages that receive tokens, or blocks of 16 rows
  * and more, times kv_heads).                                                 */
@@ -170,8 +170,7 @@ wz_status wz_quantize_rows(const void* x, int64_t x_stride, int32_t rows,
  * multiplies first), rounded to out_dtype.  a [M][K] and w [N][K] int8, rows
  * a_stride and w_stride bytes apart; out [M][N], rows out_stride elements
  * apart; bias [N] fp32 or NULL.  Supported: 0 <= M < 2^24; 1 <= N < 2^24; M * N
- * <= 2^38;
- * 16 <= K <= 65536 (a sum is then at most 2^30), a multiple of 16; a_stride,
+ * <= 2^38; 16 <= K <= 65536 (a sum is then at most 2^30), a multiple of 16; a_stride,
  * w_stride multiples of 16, K to 2^22; out_stride >= N; a and w 16-byte
  * aligned, out aligned to its element.  One kernel launch.                   */
 wz_status wz_matmul_int(const int8_t* a, int64_t a_stride,

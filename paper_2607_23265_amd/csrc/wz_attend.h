@@ -136,7 +136,9 @@ struct Partition {
     }
     int at = me * run;
     const int end = min(at + run, total);
-    while (at < end && find<true>(at, &x)) {
+    // (rows that overlap, against the contract, may make more blocks than the
+    // workspace has slots for)
+    while (at < end && find<true>(at, &x) && x.block < a.blocks) {
       const int count = min(end - at, x.tiles - x.off);
       f(x.seq, x.k, x.off, count, count == x.tiles ? -1 : me + x.block);
       at += count;

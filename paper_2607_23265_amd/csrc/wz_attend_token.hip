@@ -379,7 +379,9 @@ AttendPlan attend_plan(const wz_cache& c, const wz_ragged& r, int q_heads) {
   p.groups = int64_t(p.blocks) * c.kv_heads <= kCUs * 5 / 4 ? 2 : 1;
   const int at_once = p.block_rows == 128 && p.groups == 2 ? kCUs : 2 * kCUs;
   p.workers = int(std::max(1, at_once / c.kv_heads));
-  p.shared = tiles > 24 && p.blocks * tiles < (int64_t(1) << 30) &&
+  // (every sequence at its bounds, so that no array's contents make the tiles pass 32 bits)
+  const int64_t most = int64_t(r.batch) * ((rows + p.block_rows - 1) / p.block_rows) * (tiles + 1);
+  p.shared = tiles > 24 && most < (int64_t(1) << 30) &&
              (p.block_rows > 64 ? p.blocks < p.workers : int64_t(p.blocks) * c.kv_heads < 2048);
   p.slots = p.blocks + p.workers;
   if (p.shared) {

@@ -182,6 +182,7 @@ __device__ void append_page(const AppendArgs& a, int b, const Seq& q, int nth, i
   const int tid = threadIdx.x, Hkv = a.cache.kv_heads;
   const int place_lo = max(q.place0, 0), end = min(q.place0 + q.n, q.kv);
   const int entry = place_lo / P + nth;
+  if (nth < 0 || entry * P >= end) return;  // (only where rows overlap, against the contract, in more than 2^31 pages)
   const int page = page_of(a.batch, a.cache.pages, b, entry);
   if (page < 0) return;
   const int s0 = max(place_lo - entry * P, 0);   // slots [s0, s1) are new, [0, s0) held before

@@ -118,10 +118,9 @@ __device__ __forceinline__ Out finish(int acc, float sa, float sw, float bias) {
 // stages apart once more than a few loads are under way, would otherwise wait
 // for all of them before every read of LDS; wait_loads() is the only wait.
 __device__ __forceinline__ void load_to_lds(i32x4 buffer, uint32_t to, int offset, int uniform) {
-  // (m0 holds nothing else in this kernel: no other instruction here reads it)
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds" ::"s"(to), "v"(offset),
                "s"(buffer), "s"(uniform)
-               : "memory");
+               : "memory", "m0");
 }
 __device__ __forceinline__ uint32_t lds_address(const void* p) {
   return uint32_t(reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) const void*)p));
@@ -194,10 +193,11 @@ __global__ __launch_bounds__(WM* WN* KS* kWave) void k_matmul_tile(MatmulArgs p,
   auto fetch = [&](int i, int s) {  // step s to stage i
     const int k = (s * KS + group) * KB;
     const uint32_t to = base + i * KS * kStage;
+    const int step = k < p.K ? k : 0;  // behind the last step every lane's offset is out of range by itself
 #pragma unroll
-    for (int x = 0; x < kLoadsA; ++x) load_to_lds(abuf, to + (w * kLoadsA + x) * 1024, k + ac[x] < p.K ? ao[x] : kOOB, k);
+    for (int x = 0; x < kLoadsA; ++x) load_to_lds(abuf, to + (w * kLoadsA + x) * 1024, k + ac[x] < p.K ? ao[x] : kOOB, step);
 #pragma unroll
-    for (int x = 0; x < kLoadsB; ++x) load_to_lds(bbuf, to + BM * KB + (w * kLoadsB + x) * 1024, k + bc[x] < p.K ? bo[x] : kOOB, k);
+    for (int x = 0; x < kLoadsB; ++x) load_to_lds(bbuf, to + BM * KB + (w * kLoadsB + x) * 1024, k + bc[x] < p.K ? bo[x] : kOOB, step);
   };
 
   i32x16 acc[MT][NT] = {};

@@ -144,9 +144,9 @@ wz_status wz_cache_attention(const wz_cache* cache, const wz_ragged* batch, cons
   }
   a.cache = *cache, a.batch = *batch, a.q = q, a.out = out, a.lse = lse;
   a.q_stride = q_stride, a.out_stride = out_stride;
-  // (not zero: a masked score of -inf has to stay what it is)
+  // (neither zero nor infinite: a masked score of -inf has to stay what it is)
   const float scale2 = cfg->scale * 1.44269504088896341f;
-  a.scale2 = std::copysign(std::max(std::fabs(scale2), 0x1p-126f), scale2);
+  a.scale2 = std::copysign(std::min(std::max(std::fabs(scale2), 0x1p-126f), 0x1.fffffep127f), scale2);
   a.q_heads = cfg->q_heads, a.causal = cfg->causal, a.window = cfg->window;
   a.blocks = p.blocks, a.workers = p.workers, a.shared = p.shared;
   return from_hip(launch_attend(a, p, static_cast<hipStream_t>(stream)));
@@ -175,7 +175,8 @@ wz_status wz_matmul_int(const int8_t* a, int64_t a_stride, const float* a_scale,
   if (M == 0) return WZ_OK;
   WZ_TRY(check_rows(a, a_stride, K));
   WZ_TRY(check_rows(w, w_stride, K));
-  if (a_stride % 16 != 0 || w_stride % 16 != 0 || a_stride > (1 << 22) || w_stride > (1 << 22) || out_stride < N || out_stride > (int64_t(1) << 40))
+  if (a_stride % 16 != 0 || w_stride % 16 != 0 || a_stride > (1 << 22) || w_stride > (1 << 22) || out_stride < N ||
+      out_stride > (int64_t(1) << 40))
     return WZ_ERR_SHAPE;
   WZ_TRY(check_ptr(a_scale, 4));
   WZ_TRY(check_ptr(w_scale, 4));
