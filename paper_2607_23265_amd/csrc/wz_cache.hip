@@ -63,21 +63,23 @@ __device__ __forceinline__ Chunks chunks_of(const wz_rotation& r, int lane) {
   return Chunks{16 * lane, 16 * lane + 8, lane < pairs};
 }
 
-// The cosines and sines of a lane's eight frequencies for token t.
+// The row of positions that frequency f goes by, and token t's position there.
+__device__ __forceinline__ int section_of(const wz_rotation& r, int f) {
+  return r.axes == 1 ? 0 : f < r.sections[0] ? 0 : f < r.sections[0] + r.sections[1] ? 1 : 2;
+}
+__device__ __forceinline__ int position_of(const wz_rotation& r, int tokens, int t, int axis) {
+  return r.positions[int64_t(axis) * tokens + t];
+}
+// The cosines and sines of a lane's eight frequencies for token t; position: its
+// position for the first of them, asked for earlier.
 struct Angles {
   float c[8], s[8];
 };
-__device__ __forceinline__ void angles(const wz_rotation& r, int tokens, int t, int lane, Angles& x) {
+__device__ __forceinline__ void angles(const wz_rotation& r, int tokens, int t, int lane, int position, Angles& x) {
   const int half = r.rot_dim / 2, j = 8 * lane;
-  auto section = [&](int f) {
-    return r.axes == 1 ? 0 : f < r.sections[0] ? 0 : f < r.sections[0] + r.sections[1] ? 1 : 2;
-  };
-  auto row = [&](int axis) {
-    const int p = min(max(r.positions[int64_t(axis) * tokens + t], 0), r.max_pos - 1);
-    return r.table + int64_t(p) * r.rot_dim;
-  };
-  if (section(j) == section(j + 7)) {
-    const float* p = row(section(j)) + j;
+  auto row = [&](int p) { return r.table + int64_t(min(max(p, 0), r.max_pos - 1)) * r.rot_dim; };
+  if (section_of(r, j) == section_of(r, j + 7)) {
+    const float* p = row(position) + j;
 #pragma unroll
     for (int i = 0; i < 8; i += 4) {
       const f32x4 u = *reinterpret_cast<const f32x4*>(p + i), w = *reinterpret_cast<const f32x4*>(p + half + i);
@@ -86,7 +88,7 @@ __device__ __forceinline__ void angles(const wz_rotation& r, int tokens, int t, 
     }
   } else {
     for (int i = 0; i < 8; ++i) {
-      const float* p = row(section(j + i)) + j + i;
+      const float* p = row(position_of(r, tokens, t, section_of(r, j + i))) + j + i;
       x.c[i] = p[0], x.s[i] = p[half];
     }
   }
@@ -183,19 +185,28 @@ __device__ void append_page(const AppendArgs& a, int b, const Seq& q, int nth, i
   const int place_lo = max(q.place0, 0), end = min(q.place0 + q.n, q.kv);
   const int entry = place_lo / P + nth;
   if (nth < 0 || entry * P >= end) return;  // (only where rows overlap, against the contract, in more than 2^31 pages)
-  const int page = page_of(a.batch, a.cache.pages, b, entry);
-  if (page < 0) return;
   const int s0 = max(place_lo - entry * P, 0);   // slots [s0, s1) are new, [0, s0) held before
   const int s1 = min(end - entry * P, P);
   const int row0 = q.start + entry * P - q.place0;  // the call's row of slot 0
 
   for (int i = tid; i < P; i += kThreads) bad[i] = 0;
 
+  // Positions and the page first, whatever waits for them behind the rows: a
+  // small call is a chain of waits for memory (a step of 64 sequences took
+  // 5.9 us with positions, angles and old scales each asked for when needed).
   // All rows are asked for before the first is used; a slot that is not new
   // reads a new one's row and leaves it (nothing branches around a load but
   // for whole passes without a new slot).
   auto row_of = [&](int slot) { return row0 + min(max(slot, s0), s1 - 1); };
   auto empty = [&](int lo, int n) { return lo >= s1 || lo + n <= s0; };
+  const int lane = tid % kLanes, krow = tid / kLanes;  // of keys: lane of the row, row
+  const Chunks ch = chunks_of(a.turn, lane);
+  int position[kPasses];
+#pragma unroll
+  for (int i = 0; i < kPasses; ++i)
+    position[i] = ch.turned && !empty(i * kRows, kRows) ? position_of(a.turn, a.batch.tokens, row_of(krow + i * kRows),
+                                                                      section_of(a.turn, 8 * lane)) : 0;
+  const int found = page_of(a.batch, a.cache.pages, b, entry), page = max(found, 0);
   // values: squares of 4 tokens x 4 channels, so that a token's four channels
   // are one load and a channel's four tokens one store
   Raw4<In> vr[kSquares][4];
@@ -206,9 +217,6 @@ __device__ void append_page(const AppendArgs& a, int b, const Seq& q, int nth, i
 #pragma unroll
     for (int r = 0; r < 4; ++r) vr[i][r].load(static_cast<const In*>(a.v) + row_of(t4 + r) * a.v_stride + h * D + d);
   }
-  // keys: thread (lane of the row, row)
-  const int lane = tid % kLanes, krow = tid / kLanes;
-  const Chunks ch = chunks_of(a.turn, lane);
   Raw8<In> kr[kPasses][2];
 #pragma unroll
   for (int i = 0; i < kPasses; ++i) {
@@ -216,6 +224,9 @@ __device__ void append_page(const AppendArgs& a, int b, const Seq& q, int nth, i
     const In* src = static_cast<const In*>(a.k) + row_of(krow + i * kRows) * a.k_stride + h * D;
     kr[i][0].load(src + ch.a), kr[i][1].load(src + ch.b);
   }
+  float* const kscale = a.cache.k_scale + int64_t(page) * Hkv + h;
+  float* const vscale = a.cache.v_scale + int64_t(page) * Hkv + h;
+  const float ok = s0 > 0 ? *kscale : 0.f, ov = s0 > 0 ? *vscale : 0.f;
   __syncthreads();  // `bad` is clear
   float kx[kPasses][2][8];
   float kmax = 0.f, vmax = 0.f;
@@ -226,7 +237,7 @@ __device__ void append_page(const AppendArgs& a, int b, const Seq& q, int nth, i
     kr[i][0].get(kx[i][0]), kr[i][1].get(kx[i][1]);
     if (ch.turned) {
       Angles x;
-      angles(a.turn, a.batch.tokens, row_of(slot), lane, x);
+      angles(a.turn, a.batch.tokens, row_of(slot), lane, position[i], x);
       turn(x, a.turn.interleaved, kx[i][0], kx[i][1]);
     }
     if (slot >= s0 && slot < s1) {
@@ -260,12 +271,10 @@ __device__ void append_page(const AppendArgs& a, int b, const Seq& q, int nth, i
     }
   }
   block_max2(kmax, vmax, red);  // its barrier also covers `bad`
+  if (found < 0) return;
 
-  float* const kscale = a.cache.k_scale + int64_t(page) * Hkv + h;
-  float* const vscale = a.cache.v_scale + int64_t(page) * Hkv + h;
   float ks = pow2(scale_exp(kmax)), vs = pow2(scale_exp(vmax)), kmove = 1.f, vmove = 1.f;
   if (s0 > 0) {
-    const float ok = *kscale, ov = *vscale;
     if (ok < ks) kmove = ok / ks; else ks = ok;
     if (ov < vs) vmove = ov / vs; else vs = ov;
   }
@@ -351,6 +360,7 @@ __device__ void rotate_queries(const AppendArgs& a, int unit, int heads_at_once)
   const Chunks ch = chunks_of(a.turn, lane);
   const In* src = static_cast<const In*>(a.q) + t * a.q_stride;
   uint16_t* dst = static_cast<uint16_t*>(a.q_out) + t * a.q_out_stride;
+  const int position = ch.turned ? position_of(a.turn, a.batch.tokens, t, section_of(a.turn, 8 * lane)) : 0;
   Angles x;
   bool known = false;
   for (int h0 = r % heads_at_once; h0 < a.q_heads; h0 += kBatch * heads_at_once) {
@@ -360,7 +370,7 @@ __device__ void rotate_queries(const AppendArgs& a, int unit, int heads_at_once)
       const int h = min(h0 + i * heads_at_once, a.q_heads - 1);
       raw[i][0].load(src + h * D + ch.a), raw[i][1].load(src + h * D + ch.b);
     }
-    if (!known && ch.turned) angles(a.turn, a.batch.tokens, t, lane, x);
+    if (!known && ch.turned) angles(a.turn, a.batch.tokens, t, lane, position, x);
     known = true;
 #pragma unroll
     for (int i = 0; i < kBatch; ++i) {
@@ -389,14 +399,13 @@ __global__ __launch_bounds__(kThreads) void k_append(AppendArgs a, int page_grou
     rotate_queries<In, D>(a, id - page_groups, heads_at_once);
     return;
   }
-  auto touched = [&](int b) {
-    const Seq q = sequence(a.batch, b);
+  auto touched = [](const Seq& q) {
     const int lo = max(q.place0, 0), hi = min(q.place0 + q.n, q.kv);
     return hi > lo ? (hi - 1) / P - lo / P + 1 : 0;
   };
-  const Found f = find_item(a.batch.batch, id / a.cache.kv_heads, touched);
+  const Found f = find_item(a.batch, id / a.cache.kv_heads, touched);
   if (f.seq < 0) return;
-  append_page<In, D, P>(a, f.seq, sequence(a.batch, f.seq), f.local, id % a.cache.kv_heads, smem);
+  append_page<In, D, P>(a, f.seq, f.s, f.local, id % a.cache.kv_heads, smem);
 }
 
 template <typename In, int D>

@@ -31,27 +31,36 @@ __device__ __forceinline__ Seq sequence(const wz_ragged& r, int b) {
   return s;
 }
 
-// Where work item `id` lies when sequence b has count(b) items: its sequence
-// and its number among that sequence's.  Every wave finds it by itself, 64
-// sequences at a time; seq is -1 behind the last item.
+// Lane l's sequence in every lane.
+__device__ __forceinline__ Seq sequence_of_lane(const Seq& s, int l) {
+  return Seq{__builtin_amdgcn_readlane(s.start, l), __builtin_amdgcn_readlane(s.n, l),
+             __builtin_amdgcn_readlane(s.kv, l), __builtin_amdgcn_readlane(s.place0, l)};
+}
+
+// Where work item `id` lies when a sequence has count(sequence) items: its
+// sequence and its number among that sequence's.  Every wave finds it by
+// itself, 64 sequences at a time; seq is -1 behind the last item.
 struct Found {
   int seq, local;
+  Seq s;
 };
 template <typename Count>
-__device__ __forceinline__ Found find_item(int batch, int id, Count count) {
+__device__ __forceinline__ Found find_item(const wz_ragged& r, int id, Count count) {
   const int lane = __lane_id();
   int base = 0;
-  for (int b0 = 0; b0 < batch; b0 += kWave) {
-    const int c = b0 + lane < batch ? count(b0 + lane) : 0;
-    const int incl = wave_incl_scan_i32(c);
+  for (int b0 = 0; b0 < r.batch; b0 += kWave) {
+    const bool in = b0 + lane < r.batch;
+    const Seq s = in ? sequence(r, b0 + lane) : Seq{0, 0, 0, 0};
+    const int c = in ? count(s) : 0, incl = wave_incl_scan_i32(c);
     const int total = __builtin_amdgcn_readlane(incl, kWave - 1);
     if (id - base < total) {
       const int l = __builtin_ctzll(__ballot(incl > id - base));
-      return Found{b0 + l, id - base - (__builtin_amdgcn_readlane(incl, l) - __builtin_amdgcn_readlane(c, l))};
+      const int before = __builtin_amdgcn_readlane(incl, l) - __builtin_amdgcn_readlane(c, l);
+      return Found{b0 + l, id - base - before, sequence_of_lane(s, l)};
     }
     base += total;
   }
-  return Found{-1, 0};
+  return Found{-1, 0, Seq{}};
 }
 
 // The page that `table` entry holds, or -1 where it is none of the cache's.
@@ -87,6 +96,7 @@ struct AttendArgs {
   int blocks;        // the plan's (attend_plan), for each key/value head
   int workers;       // shared: workgroups that share the blocks' tokens, through the workspace
   int shared;
+  int block_rows;    // shared: rows that a block has at most
   float* part;       // shared: [slots][kv_heads][rows of a block][head_dim] unnormalised sums
   float* part_ml;    // shared: [slots][kv_heads][rows of a block][2] maximum (log2) and sum
 };
