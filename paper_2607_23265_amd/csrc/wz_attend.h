@@ -10,6 +10,11 @@
 // short one and all finish together.  A workgroup leaves a part of every
 // block that it does not have to itself in slot (its number + the block's),
 // and a second kernel adds a block's parts up in order.
+//
+// Few rows in few blocks are cut so that no workgroup has tiles of two blocks,
+// since a piece of a block costs as much as a round of tiles: each block into
+// equal pieces of `run` tiles or fewer, one for each workgroup, whose number is
+// the piece's slot.
 #pragma once
 
 #include "wz_serve.h"
@@ -19,6 +24,15 @@ namespace wz {
 constexpr int kTile = 64;       // tokens of a tile
 constexpr int kMinRun = 4;      // tiles of a workgroup's run at least
 
+// Whether blocks are cut by themselves, and the tiles of their pieces at most: the
+// pieces, total / run and one more for each block at most, must not outnumber
+// the workgroups.
+__host__ __device__ inline bool lone_pieces(int64_t blocks, int workers) { return 4 * blocks <= workers; }
+__host__ __device__ inline int64_t lone_run(int64_t total, int64_t blocks, int workers) {
+  const int64_t run = (total + workers - blocks - 1) / (workers - blocks);
+  return run > kMinRun ? run : kMinRun;
+}
+
 struct Block {
   int rows, r0;            // rows of the sequence, first row of the block
   int lo, hi;              // places that any of its rows sees: [lo, hi)
@@ -27,8 +41,10 @@ struct Block {
 
 // A place in the shared plan: tile `off` of the `tiles` that block k of
 // sequence seq has; `block` blocks and `before` tiles lie in front of that one.
+// (Where blocks are cut by themselves, pieces take the place of tiles.)
 struct Spot {
   int seq, k, off, tiles, block, before;
+  Seq s;
 };
 
 template <int BR>
@@ -36,6 +52,7 @@ struct Partition {
   const AttendArgs& a;
   int G;
   int total, run;  // shared: tiles of all blocks, and of a workgroup's run
+  bool lone;       // shared: blocks are cut by themselves
 
   __device__ __forceinline__ int blocks(const Seq& s) const { return (s.n * G + BR - 1) / BR; }
   __device__ __forceinline__ Block block(const Seq& s, int k) const {
@@ -76,7 +93,8 @@ struct Partition {
       const Seq s = in ? sequence(a.batch, b0 + lane) : Seq{0, 0, 0, 0};
       const int mine = blocks(s);
       if constexpr (kUniform) {
-        const int each = tiles(s, 0), work = a.shared ? mine * each : 0;  // (unshared, tiles are not asked for)
+        const int all = tiles(s, 0), each = lone ? (all + run - 1) / run : all;
+        const int work = a.shared ? mine * each : 0;  // (unshared, tiles are not asked for)
         const int ib = wave_incl_scan_i32(mine), it = wave_incl_scan_i32(work);
         const unsigned long long pass = __ballot(TILES ? nt + it > at : nb + ib > at);
         if (pass) {
@@ -84,15 +102,14 @@ struct Partition {
           const int b1 = nb + __builtin_amdgcn_readlane(ib - mine, l), t1 = nt + __builtin_amdgcn_readlane(it - work, l);
           const int n = __builtin_amdgcn_readlane(each, l);
           const int k = TILES ? (at - t1) / n : at - b1;
-          *spot = Spot{b0 + l, k, TILES ? (at - t1) % n : 0, n, b1 + k, t1 + k * n};
+          *spot = Spot{b0 + l, k, TILES ? (at - t1) % n : 0, n, b1 + k, t1 + k * n, sequence_of_lane(s, l)};
           return true;
         }
         nb += __builtin_amdgcn_readlane(ib, kWave - 1), nt += __builtin_amdgcn_readlane(it, kWave - 1);
       } else {
         for (unsigned long long left = __ballot(mine > 0); left; left &= left - 1) {
           const int l = __builtin_ctzll(left);
-          const Seq one{__builtin_amdgcn_readlane(s.start, l), __builtin_amdgcn_readlane(s.n, l),
-                        __builtin_amdgcn_readlane(s.kv, l), __builtin_amdgcn_readlane(s.place0, l)};
+          const Seq one = sequence_of_lane(s, l);
           const int count = blocks(one);
           if (!TILES && at >= nb + count && !a.shared) {  // (tiles are not needed)
             nb += count;
@@ -104,7 +121,7 @@ struct Partition {
             const unsigned long long pass = __ballot(n > 0 && (TILES ? nt + it > at : nb + k0 + lane + 1 > at));
             if (pass) {
               const int i = __builtin_ctzll(pass), t1 = nt + __builtin_amdgcn_readlane(it - n, i);
-              *spot = Spot{b0 + l, k0 + i, TILES ? at - t1 : 0, __builtin_amdgcn_readlane(n, i), nb + k0 + i, t1};
+              *spot = Spot{b0 + l, k0 + i, TILES ? at - t1 : 0, __builtin_amdgcn_readlane(n, i), nb + k0 + i, t1, one};
               return true;
             }
             nt += __builtin_amdgcn_readlane(it, kWave - 1);
@@ -118,20 +135,33 @@ struct Partition {
   }
   // (the host shares only where the tiles of all blocks fit in an int)
   __device__ __forceinline__ Partition(const AttendArgs& args)
-      : a(args), G(args.q_heads / args.cache.kv_heads), total(0), run(0) {
+      : a(args), G(args.q_heads / args.cache.kv_heads), total(0), run(0), lone(false) {
     if (!a.shared) return;
     Spot all;
     find<true>(0x7fffffff, &all);
     total = all.before;
     run = max((total + a.workers - 1) / a.workers, kMinRun);
+    if (kUniform && lone_pieces(all.block, a.workers)) {
+      run = int(lone_run(total, all.block, a.workers));
+      lone = true;
+    }
   }
-  // Calls f(seq, k, off, count, slot) for every piece of a block that workgroup
-  // `me` has; slot is where its part goes, -1 if the block is all its own.
+  // Calls f(spot, count, slot) for every piece of a block that workgroup `me`
+  // has: `count` tiles from the spot on; slot is where its part goes, -1 if the
+  // block is all its own.
   template <typename F>
   __device__ __forceinline__ void each_piece(int me, F f) const {
     Spot x;
     if (!a.shared) {
-      if (find<false>(me, &x)) f(x.seq, x.k, 0, x.tiles, -1);
+      if (find<false>(me, &x)) f(x, x.tiles, -1);
+      return;
+    }
+    if (lone) {
+      if (!find<true>(me, &x) || x.block >= a.blocks) return;
+      const int all = tiles(x.s, 0), from = all * x.off / x.tiles, to = all * (x.off + 1) / x.tiles;
+      const int slot = x.tiles == 1 ? -1 : me;
+      x.off = from;
+      f(x, to - from, slot);
       return;
     }
     int at = me * run;
@@ -140,7 +170,7 @@ struct Partition {
     // workspace has slots for)
     while (at < end && find<true>(at, &x) && x.block < a.blocks) {
       const int count = min(end - at, x.tiles - x.off);
-      f(x.seq, x.k, x.off, count, count == x.tiles ? -1 : me + x.block);
+      f(x, count, count == x.tiles ? -1 : me + x.block);
       at += count;
       if (at < end) __syncthreads();  // LDS is used again
     }

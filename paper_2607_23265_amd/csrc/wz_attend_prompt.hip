@@ -36,19 +36,23 @@ struct Stages {
   __bf16 v[2][D * kTile];  // [channel][token]
 };
 
-// Tiles [off, off + count) of block kb of sequence b, key/value head h; slot:
-// where its part goes, -1 if the block is this workgroup's alone.
+// A value row (128 bytes of 256 of banks) exchanges its chunks so that eight
+// lanes that write eight rows and sixteen that read sixteen meet no bank twice.
+__device__ __forceinline__ int value_exchange(int channel) { return (channel & 7) ^ (channel >> 3 & 1); }
+
+// `count` tiles from spot x on, key/value head h; slot: where their part goes, -1
+// if the block is this workgroup's alone.
 // KG groups of four waves take the tiles in turn, each with stages of its own,
 // and add up at the end.
 template <int D, int KG>
-__device__ __forceinline__ void attend_block(const AttendArgs& a, const Partition<kRows>& part, int h, int b, int kb,
-                                             int off, int count, int slot, Stages<D> (&stages)[KG]) {
+__device__ __forceinline__ void attend_block(const AttendArgs& a, const Partition<kRows>& part, int h, const Spot& x,
+                                             int count, int slot, Stages<D> (&stages)[KG]) {
   constexpr int KK = D / 16, DT = D / 32, kExchange = D / 8 - 1;
   constexpr int kKeyPieces = kTile * (D / 16) / kThreads, kValPieces = D * (kTile / 16) / kThreads;
   const int Hkv = a.cache.kv_heads, G = part.G;
-  const Seq s = sequence(a.batch, b);
-  const Block blk = part.block(s, kb);
-  const int T0 = blk.lo / kTile + off;
+  const Seq s = x.s;
+  const Block blk = part.block(s, x.k);
+  const int T0 = blk.lo / kTile + x.off;
   const int T1 = min((max(blk.hi, blk.lo) + kTile - 1) / kTile, T0 + count);
 
   const int lane = __lane_id(), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
@@ -93,9 +97,12 @@ __device__ __forceinline__ void attend_block(const AttendArgs& a, const Partitio
   u32x4 kx[kKeyPieces], vx[kValPieces];
   float ks4 = 0.f, vs4 = 0.f;  // scales of block lane % 4
   uint32_t in_next = 0;        // bit k: block k of the tile loaded last lies in a page of the cache
-  const int* const row_of = a.batch.table + int64_t(b) * a.batch.table_stride;
+  const int* const row_of = a.batch.table + int64_t(x.seq) * a.batch.table_stride;
   const int entries = max((s.kv + P - 1) >> logP, 1);
-  const int ktok = tid / (D / 16), kpart = tid % (D / 16);
+  // LDS takes eight lanes' 16 bytes at once, over 128 bytes of banks.  A lane's
+  // two chunks are next to each other, so eight lanes hold four pieces each of
+  // two rows, which the exchange sends to even and to odd chunks.
+  const int ktok = tid / (D / 8) * 2 + (tid >> 2 & 1), kpart = (tid & 3) | (tid % (D / 8) >> 3 << 2);
   const int koff = (ktok & 15) * D + 16 * kpart, voff = lane * P;
   auto key_block = [&](int i) { return (w * kWave + i * kThreads) / D; };  // (tok / 16)
   auto pages = [&](int tile) {  // of block lane % 4
@@ -144,8 +151,8 @@ __device__ __forceinline__ void attend_block(const AttendArgs& a, const Partitio
       const int k = i - kKeyPieces, d = lane + 64 * k;
       const float scale = lane_of(vs4, w);
       __bf16* at = vt[buf] + d * kTile;
-      *reinterpret_cast<bf16x8*>(at + 8 * ((2 * w) ^ (d >> 1 & 7))) = decode8(vx[k][0], vx[k][1], scale);
-      *reinterpret_cast<bf16x8*>(at + 8 * ((2 * w + 1) ^ (d >> 1 & 7))) = decode8(vx[k][2], vx[k][3], scale);
+      *reinterpret_cast<bf16x8*>(at + 8 * ((2 * w) ^ value_exchange(d))) = decode8(vx[k][0], vx[k][1], scale);
+      *reinterpret_cast<bf16x8*>(at + 8 * ((2 * w + 1) ^ value_exchange(d))) = decode8(vx[k][2], vx[k][3], scale);
     }
   };
   static_assert(kKeyPieces + kValPieces <= KK / 2, "a piece is stored with every batch of products");
@@ -225,7 +232,7 @@ __device__ __forceinline__ void attend_block(const AttendArgs& a, const Partitio
     auto read_values = [&](int u) {
 #pragma unroll
       for (int d = 0; d < DT; ++d)
-        v[u % 2][d] = *reinterpret_cast<const bf16x8*>(vt[buf] + (32 * d + c) * kTile + 8 * ((2 * u + g) ^ (c >> 1 & 7)));
+        v[u % 2][d] = *reinterpret_cast<const bf16x8*>(vt[buf] + (32 * d + c) * kTile + 8 * ((2 * u + g) ^ value_exchange(c)));
       __builtin_amdgcn_sched_barrier(0);
     };
     auto probabilities = [&](int u) {
@@ -329,8 +336,8 @@ __global__ __launch_bounds__(KG* kThreads, 2) void k_attend_prompt(AttendArgs a)
   const int Hkv = a.cache.kv_heads, h = blockIdx.x % Hkv, all = gridDim.x / Hkv;
   const Partition<kRows> part(a);
   // the last blocks first: in a causal batch they are the longest
-  part.each_piece(all - 1 - int(blockIdx.x) / Hkv, [&](int b, int k, int off, int count, int slot) {
-    attend_block<D, KG>(a, part, h, b, k, off, count, slot, stages);
+  part.each_piece(all - 1 - int(blockIdx.x) / Hkv, [&](const Spot& x, int count, int slot) {
+    attend_block<D, KG>(a, part, h, x, count, slot, stages);
   });
 }
 

@@ -21,18 +21,18 @@
 namespace wz {
 namespace {
 
-// Tiles [off, off + count) of block k of sequence b, key/value head h; slot:
-// where its part goes, -1 if the block is this workgroup's alone.
+// `count` tiles from spot x on, key/value head h; slot: where their part goes, -1
+// if the block is this workgroup's alone.
 template <int D, int NT, int kWaves>
-__device__ __forceinline__ void attend_block(const AttendArgs& a, const Partition<16 * NT>& part, int h, int b, int k,
-                                             int off, int count, int slot, float* so, float (*sm)[16 * NT],
+__device__ __forceinline__ void attend_block(const AttendArgs& a, const Partition<16 * NT>& part, int h, const Spot& x,
+                                             int count, int slot, float* so, float (*sm)[16 * NT],
                                              float (*sl)[16 * NT]) {
   constexpr int BR = 16 * NT, KK = D / 32, DT = D / 16, kPieces = D / 64, kThreads = kWaves * kWave;
   constexpr int kLd = D + 4;
   const int Hkv = a.cache.kv_heads, G = part.G;
-  const Seq s = sequence(a.batch, b);
-  const Block blk = part.block(s, k);
-  const int T0 = blk.lo / kTile + off;
+  const Seq s = x.s;
+  const Block blk = part.block(s, x.k);
+  const int T0 = blk.lo / kTile + x.off;
   const int T1 = min((max(blk.hi, blk.lo) + kTile - 1) / kTile, T0 + count);
 
   const int lane = __lane_id(), w = threadIdx.x / kWave, c = lane & 15, q = lane >> 4;
@@ -75,7 +75,7 @@ __device__ __forceinline__ void attend_block(const AttendArgs& a, const Partitio
     bool vin;
   } bufs[2];
   const int last = T0 + w + (max(T1 - T0 - w, 1) - 1) / kWaves * kWaves;  // this wave's last tile
-  const int* const row = a.batch.table + int64_t(b) * a.batch.table_stride;
+  const int* const row = a.batch.table + int64_t(x.seq) * a.batch.table_stride;
   const int entries = max((s.kv + P - 1) >> logP, 1);
   // Pages of the lane's key block (c / 4) and value block (q) in a tile: asked
   // for before the loads of the tile in front, so that waiting for them does
@@ -258,8 +258,8 @@ __global__ __launch_bounds__(kWaves* kWave, NT == 1 ? 2 : 1) void k_attend_token
   __shared__ float sm[kWaves][BR], sl[kWaves][BR];
   const int Hkv = a.cache.kv_heads, h = blockIdx.x % Hkv, me = blockIdx.x / Hkv;
   const Partition<BR> part(a);
-  part.each_piece(me, [&](int b, int k, int off, int count, int slot) {
-    attend_block<D, NT, kWaves>(a, part, h, b, k, off, count, slot, so, sm, sl);
+  part.each_piece(me, [&](const Spot& x, int count, int slot) {
+    attend_block<D, NT, kWaves>(a, part, h, x, count, slot, so, sm, sl);
   });
 }
 
@@ -273,16 +273,18 @@ __global__ __launch_bounds__(256) void k_attend_join(AttendArgs a) {
   __shared__ float red[2][256 / kLanes];
   const int Hkv = a.cache.kv_heads, h = blockIdx.x % Hkv, at = blockIdx.x / Hkv;
   const Partition<BR> part(a);
+  const int per = (a.block_rows + kRows - 1) / kRows;  // workgroups of a block
   Spot x;
-  if (!part.template find<false>(at / (BR / kRows), &x)) return;
-  const Seq s = sequence(a.batch, x.seq);
-  const int first = x.before / part.run, last = (x.before + x.tiles - 1) / part.run;
+  if (!part.template find<false>(at / per, &x)) return;
+  const Seq s = x.s;
+  const int first = part.lone ? x.before : x.before / part.run;
+  const int last = part.lone ? x.before + x.tiles - 1 : (x.before + x.tiles - 1) / part.run;
   if (first == last) return;  // written by the only workgroup that had it
   const int lane = threadIdx.x % kLanes, all_groups = threadIdx.x / kLanes, d = 4 * lane;
   const int group = all_groups % PG, mine = all_groups / PG;
-  const int G = part.G, r = at % (BR / kRows) * kRows + mine, row = x.k * BR + r;
+  const int G = part.G, r = at % per * kRows + mine, row = x.k * BR + r;
   const bool in = row < s.n * G;  // (its slots exist in any case)
-  const int64_t step = int64_t(Hkv) * BR, slot0 = (int64_t(first + x.block) * Hkv + h) * BR + r;
+  const int64_t step = int64_t(Hkv) * BR, slot0 = (int64_t(first + (part.lone ? 0 : x.block)) * Hkv + h) * BR + r;
   // a running maximum as in the kernels that left the parts; a part without a
   // score has a maximum of -inf and a sum of 0, or of NaN if every score was
   float top = -INFINITY, sum = 0.f;
@@ -345,7 +347,8 @@ hipError_t join(const AttendArgs& a, const AttendPlan& p, hipStream_t s) {
   // groups share rows where blocks have eight parts or more on average
   constexpr int kGroups = 1024 / D;
   const bool many = p.workers >= 8 * p.blocks;
-  const dim3 grid(uint32_t(p.blocks * (many ? BR : BR / kGroups) * a.cache.kv_heads)), block(256);
+  const int rows = many ? 1 : kGroups;  // of a workgroup
+  const dim3 grid(uint32_t(p.blocks * ((a.block_rows + rows - 1) / rows) * a.cache.kv_heads)), block(256);
   if (many) hipLaunchKernelGGL((k_attend_join<D, BR, kGroups>), grid, block, 0, s, a);
   else hipLaunchKernelGGL((k_attend_join<D, BR, 1>), grid, block, 0, s, a);
   return hipGetLastError();
@@ -375,13 +378,27 @@ AttendPlan attend_plan(const wz_cache& c, const wz_ragged& r, int q_heads) {
   const int64_t tiles = (int64_t(r.max_kv) + kTile - 1) / kTile;
   // A CU runs two workgroups of four waves at once, or one prompt workgroup of
   // eight, which is faster while blocks are about as many as CUs or fewer
-  // (shared, it leaves half as many parts).
+  // (shared, it leaves half as many parts).  Registers would hold four of few
+  // rows: more parts, shorter runs, and 74 us instead of 70 for the next tokens of
+  // four sequences of 60 000 to 131 000 (three: 72; of 64 of 500 to 8 200: 55 with
+  // two, 63, 54).
   p.groups = int64_t(p.blocks) * c.kv_heads <= kCUs * 5 / 4 ? 2 : 1;
   const int at_once = p.block_rows == 128 && p.groups == 2 ? kCUs : 2 * kCUs;
   p.workers = int(std::max(1, at_once / c.kv_heads));
+  // Few rows in few blocks: sharing costs a second launch, which is worth two of
+  // the rounds that the waves of the block's only workgroup (eight) or of a
+  // shared run (four) make over its tiles (single tokens of one sequence and four
+  // heads, 1286 tokens: 14.6 us alone, three rounds, and 11.9 shared, one; 800
+  // tokens: 12.0 and 11.5).
+  bool long_enough = tiles > 24;
+  if (p.block_rows <= 64 && lone_pieces(p.blocks, p.workers)) {
+    const int64_t run = lone_run(p.blocks * tiles, p.blocks, p.workers);
+    const int waves = p.block_rows == 16 ? 8 : 4;
+    long_enough = (tiles + waves - 1) / waves >= (run + 3) / 4 + 2;
+  }
   // (every sequence at its bounds, so that no array's contents make the tiles pass 32 bits)
   const int64_t most = int64_t(r.batch) * ((rows + p.block_rows - 1) / p.block_rows) * (tiles + 1);
-  p.shared = tiles > 24 && most < (int64_t(1) << 30) &&
+  p.shared = long_enough && most < (int64_t(1) << 30) &&
              (p.block_rows > 64 ? p.blocks < p.workers : int64_t(p.blocks) * c.kv_heads < 2048);
   p.slots = p.blocks + p.workers;
   if (p.shared) {
