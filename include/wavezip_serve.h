@@ -172,7 +172,8 @@ wz_status wz_quantize_rows(const void* x, int64_t x_stride, int32_t rows,
  * apart; bias [N] fp32 or NULL.  Supported: 0 <= M < 2^24; 1 <= N < 2^24; M * N
  * <= 2^38; 16 <= K <= 65536 (a sum is then at most 2^30), a multiple of 16; a_stride,
  * w_stride multiples of 16, K to 2^22; out_stride >= N; a and w 16-byte
- * aligned, out aligned to its element.  One kernel launch.                   */
+ * aligned, out aligned to its element.  One kernel launch, or two (the rows of
+ * whole rounds of large tiles, and those behind them).                       */
 wz_status wz_matmul_int(const int8_t* a, int64_t a_stride,
                         const float* a_scale, const int8_t* w,
                         int64_t w_stride, const float* w_scale,

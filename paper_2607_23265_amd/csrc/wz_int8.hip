@@ -350,27 +350,78 @@ hipError_t tiles(const MatmulArgs& p, hipStream_t s) {
                      0, s, p, int(tm), int(tn));
   return hipGetLastError();
 }
-// The tile by the time of a product with K = 3584, measured (us; other K scale
-// all alike): a CU works on one 256 x 256 tile in 46, one of 192 x 128 in 26, two
-// of 128 x 128 together in 29 and one alone in 18, one of 64 x 64 in 6.4.  Large
-// tiles read LDS less for the same products, small ones fill the chip.  Where
-// even these are too few for the CUs, four groups of waves share the steps of
-// a 32 x 32 tile (M <= 32: 6.3 us for 4608 columns, a 64 x 64 tile 8.8), or two
-// those of a 64 x 32 tile (M <= 64: 7.5 against 9.2).
+
+// A tile's time, measured with K = 3584 (us; the part of a round scales with K):
+// a launch takes `fixed` and `round` for every round of the CUs, which work on
+// `at_once` tiles each; the last round, with a share f of its tiles, takes 0.6 +
+// 0.4 f of one (256 x 256 tiles: 41.3 us with 108, 57.6 with 256, 149 with 666).
+// Large tiles read LDS less for the same products, small ones fill the chip; three
+// stages hide a step's loads behind two others where a CU has one tile (128 x
+// 128: 20.8 us with three, 23.5 with two), and two leave room for a second tile
+// (33.1 for both).
+template <typename Out>
+struct Tile {
+  int bm, bn;
+  double fixed, round;
+  int at_once;
+  hipError_t (*run)(const MatmulArgs&, hipStream_t);
+
+  int64_t columns(const MatmulArgs& p) const { return (int64_t(p.N) + bn - 1) / bn; }
+  int64_t count(const MatmulArgs& p) const { return (int64_t(p.M) + bm - 1) / bm * columns(p); }
+  double time(const MatmulArgs& p, double rounds) const { return fixed + round * (p.K / 3584.) * rounds; }
+  double time(const MatmulArgs& p) const {
+    const double rounds = double(count(p)) / (kCUs * at_once), full = std::floor(rounds), f = rounds - full;
+    return time(p, full + (f > 0 ? 0.6 + 0.4 * f : 0.));
+  }
+};
+
 template <typename Out>
 hipError_t matmul(const MatmulArgs& p, hipStream_t s) {
+  // Few rows: where even the smallest tiles are too few for the CUs, four groups
+  // of waves share the steps of a 32 x 32 tile (M <= 32: 6.3 us for 4608 columns,
+  // a 64 x 64 tile 8.8), or two those of a 64 x 32 tile (M <= 64: 7.5 against 9.2).
   auto count = [&](int bm, int bn) { return (int64_t(p.M) + bm - 1) / bm * ((int64_t(p.N) + bn - 1) / bn); };
-  auto turns = [&](int bm, int bn) { return double((count(bm, bn) + kCUs - 1) / kCUs); };
   if (p.M <= 32 && count(32, 32) <= kCUs) return tiles<Out, 32, 32, 1, 1, 4, 4>(p, s);
   if (p.M <= 64 && count(64, 32) <= kCUs) return tiles<Out, 64, 32, 2, 1, 3, 2>(p, s);
-  const double n128 = turns(128, 128);
-  const double t256 = 46 * turns(256, 256), t192 = 26 * turns(192, 128);
-  const double t128 = 29 * std::floor(n128 / 2) + 18 * std::fmod(n128, 2), t64 = 6.4 * turns(64, 64);
-  const double best = std::min({t256, t192, t128, t64});
-  if (best == t64) return tiles<Out, 64, 64, 2, 2, 4, 1>(p, s);
-  if (best == t128) return tiles<Out, 128, 128, 2, 2, 2, 1>(p, s);
-  if (best == t192) return tiles<Out, 192, 128, 2, 4, 2, 1>(p, s);
-  return tiles<Out, 256, 256, 2, 4, 2, 1>(p, s);
+  static constexpr Tile<Out> kTiles[] = {
+      {64, 64, 3.6, 5.8, 1, tiles<Out, 64, 64, 2, 2, 4, 1>},
+      {128, 64, 4.6, 9.4, 1, tiles<Out, 128, 64, 2, 2, 3, 1>},
+      {128, 128, 3.3, 17.6, 1, tiles<Out, 128, 128, 2, 2, 3, 1>},
+      {128, 128, 3.0, 30.2, 2, tiles<Out, 128, 128, 2, 2, 2, 1>},
+      {192, 128, 3.4, 22.5, 1, tiles<Out, 192, 128, 2, 4, 3, 1>},
+      {256, 256, 8.0, 49.7, 1, tiles<Out, 256, 256, 2, 4, 2, 1>},
+  };
+  auto fastest = [&](const MatmulArgs& q) {
+    const Tile<Out>* best = kTiles;
+    for (const Tile<Out>& t : kTiles)
+      if (t.time(q) < best->time(q)) best = &t;
+    return best;
+  };
+  // Rows of tiles that fill whole rounds, and what is left in tiles that fit it
+  // better, as a second launch, where that is faster than a last round of a few
+  // tiles (9459 x 14336: 2072 tiles of 256 x 256 are 8 rounds and 24 tiles).
+  const Tile<Out>* const whole = fastest(p);
+  double best = whole->time(p);
+  const Tile<Out>* first = nullptr;
+  int rows = 0;
+  for (const Tile<Out>& t : kTiles) {
+    const int64_t at_once = kCUs * t.at_once, rounds = t.count(p) / at_once;
+    const int64_t full = rounds * at_once / t.columns(p) * t.bm;
+    if (full <= 0 || full >= p.M) continue;
+    MatmulArgs rest = p;
+    rest.M = p.M - int(full);
+    const double time = t.time(p, double(rounds)) + fastest(rest)->time(rest);
+    if (time < best) best = time, first = &t, rows = int(full);
+  }
+  if (!first) return whole->run(p, s);
+  MatmulArgs part = p;
+  part.M = rows;
+  const hipError_t e = first->run(part, s);
+  if (e != hipSuccess) return e;
+  part.M = p.M - rows;
+  part.a += rows * p.a_stride, part.a_scale += rows;
+  part.out = static_cast<Out*>(p.out) + rows * p.out_stride;
+  return fastest(part)->run(part, s);
 }
 
 }  // namespace
