@@ -74,12 +74,16 @@ def algorithmic_bytes(wl, out_bytes):
 
 
 def kernel_sources_sha256():
-    """Digest of the kernel and C-ABI sources, to tell whether recorded counters still describe them."""
+    """Digest of the condensation pass's kernel and C-ABI sources (the serving operators' have no part in it), to tell
+    whether recorded counters still describe them."""
     h = hashlib.sha256()
+    serving = ("wz_attend", "wz_cache", "wz_int8", "wz_serve", "wavezip_serve")
     csrc = os.path.join("paper_2607_23265_amd", "csrc")
     files = sorted([os.path.join(csrc, f) for f in os.listdir(os.path.join(HERE, csrc)) if f.endswith((".hip", ".h"))] +
                    [os.path.join("include", f) for f in os.listdir(os.path.join(HERE, "include")) if f.endswith(".h")])
     for f in files:
+        if os.path.basename(f).startswith(serving):
+            continue
         h.update(f.encode())
         with open(os.path.join(HERE, f), "rb") as fh:
             h.update(fh.read())
