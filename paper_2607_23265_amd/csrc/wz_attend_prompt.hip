@@ -28,7 +28,7 @@ constexpr int kThreads = kWaves * kWave;
 constexpr int kRows = 32 * kWaves;
 
 // Classes of instructions for the scheduler.
-constexpr int kVector = 0x2, kProducts = 0x8;
+constexpr int kVector = 0x2, kScalar = 0x4, kProducts = 0x8;
 
 template <int D>
 struct Stages {
@@ -61,8 +61,6 @@ __device__ __forceinline__ void attend_block(const AttendArgs& a, const Partitio
   auto& vt = stages[group].v;
   const int c = lane & 31, g = lane >> 5;
   const int P = a.cache.page_size, logP = __builtin_ctz(P);
-  const uint8_t* const kc = static_cast<const uint8_t*>(a.cache.k);
-  const uint8_t* const vc = static_cast<const uint8_t*>(a.cache.v);
 
   const int row = blk.r0 + 32 * w + c;
   const bool valid = row < blk.rows;
@@ -103,30 +101,46 @@ __device__ __forceinline__ void attend_block(const AttendArgs& a, const Partitio
   // two chunks are next to each other, so eight lanes hold four pieces each of
   // two rows, which the exchange sends to even and to odd chunks.
   const int ktok = tid / (D / 8) * 2 + (tid >> 2 & 1), kpart = (tid & 3) | (tid % (D / 8) >> 3 << 2);
-  const int koff = (ktok & 15) * D + 16 * kpart, voff = lane * P;
+  const uint32_t koff = (ktok & 15) * D + 16 * kpart, voff = lane * P;
   auto key_block = [&](int i) { return (w * kWave + i * kThreads) / D; };  // (tok / 16)
+  const uint32_t page_bytes = uint32_t(Hkv) * P * D;  // of all heads
+  const uint8_t* const kbase = static_cast<const uint8_t*>(a.cache.k) + uint32_t(h) * P * D;
+  const uint8_t* const vbase = static_cast<const uint8_t*>(a.cache.v) + uint32_t(h) * P * D;
   auto pages = [&](int tile) {  // of block lane % 4
     return row_of[min((min(tile, T1 - 1) * kTile + 16 * (lane & 3)) >> logP, entries - 1)];
   };
-  auto load = [&](int tile, int id) {
-    const int first = min(tile, T1 - 1) * kTile;
+  // The page of block lane % 4 of a tile, and its scales, asked for: worked out
+  // in lanes, between products, since a wave waits for every step of a chain of
+  // scalar instructions (prompts of two long videos 1223 -> 1193 us).
+  struct Next {
+    uint64_t page;  // its first byte
+    float ks, vs;
+    uint32_t in;
+  };
+  auto find = [&](int id) {
+    Next n;
     const bool there = uint32_t(id) < uint32_t(a.cache.pages);
-    in_next = uint32_t(__ballot(there)) & 0xfu;
-    const int page = there ? id : 0;
-    const int64_t scale_at = int64_t(page) * Hkv + h;
-    ks4 = a.cache.k_scale[scale_at];
-    const float scale = a.cache.v_scale[scale_at];
-    vs4 = there ? scale : 1.f;
+    n.in = uint32_t(__ballot(there)) & 0xfu;
+    const uint32_t page = there ? id : 0;
+    n.page = uint64_t(page) * page_bytes;
+    const uint64_t scale_at = uint64_t(page) * uint32_t(Hkv);
+    n.ks = a.cache.k_scale[scale_at + h], n.vs = a.cache.v_scale[scale_at + h];
+    return n;
+  };
+  auto lane_of64 = [](uint64_t x, int i) {
+    const uint32_t lo = __builtin_amdgcn_readlane(uint32_t(x), i), hi = __builtin_amdgcn_readlane(uint32_t(x >> 32), i);
+    return uint64_t(hi) << 32 | lo;
+  };
+  auto load = [&](int tile, const Next& n) {
+    const uint32_t first = min(tile, T1 - 1) * kTile;
 #pragma unroll
-    for (int i = 0; i < kKeyPieces; ++i) {
-      const int blk16 = key_block(i), in_page = (first + 16 * blk16) & (P - 1);
-      const int64_t at = (int64_t(__builtin_amdgcn_readlane(page, blk16)) * Hkv + h) * (P * D) + in_page * D;
-      kx[i] = *reinterpret_cast<const u32x4*>(kc + at + koff);
-    }
-    const int in_page = (first + 16 * w) & (P - 1);
-    const int64_t at = (int64_t(__builtin_amdgcn_readlane(page, w)) * Hkv + h) * (P * D) + in_page;
+    for (int i = 0; i < kKeyPieces; ++i)
+      kx[i] = *reinterpret_cast<const u32x4*>(kbase + lane_of64(n.page, key_block(i)) +
+                                              (((first + 16 * key_block(i)) & (P - 1)) * D + koff));
+    const uint8_t* const values = vbase + lane_of64(n.page, w) + ((first + 16 * w) & (P - 1));
 #pragma unroll
-    for (int i = 0; i < kValPieces; ++i) vx[i] = *reinterpret_cast<const u32x4*>(vc + at + 64 * i * P + voff);
+    for (int i = 0; i < kValPieces; ++i) vx[i] = *reinterpret_cast<const u32x4*>(values + (64 * i * P + voff));
+    ks4 = n.ks, vs4 = n.vs, in_next = n.in;
     __builtin_amdgcn_sched_barrier(0);
   };
   auto lane_of = [](float x, int i) { return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(x), i)); };
@@ -149,7 +163,7 @@ __device__ __forceinline__ void attend_block(const AttendArgs& a, const Partitio
       *reinterpret_cast<bf16x8*>(at + 8 * ((2 * kpart + 1) ^ (r & kExchange))) = decode8(kx[i][2], kx[i][3], scale);
     } else if (i < kKeyPieces + kValPieces) {
       const int k = i - kKeyPieces, d = lane + 64 * k;
-      const float scale = lane_of(vs4, w);
+      const float there = lane_of(vs4, w), scale = in_next >> w & 1u ? there : 1.f;
       __bf16* at = vt[buf] + d * kTile;
       *reinterpret_cast<bf16x8*>(at + 8 * ((2 * w) ^ value_exchange(d))) = decode8(vx[k][0], vx[k][1], scale);
       *reinterpret_cast<bf16x8*>(at + 8 * ((2 * w + 1) ^ value_exchange(d))) = decode8(vx[k][2], vx[k][3], scale);
@@ -179,6 +193,7 @@ __device__ __forceinline__ void attend_block(const AttendArgs& a, const Partitio
                                                        8 * ((2 * (2 * j + i / 2) + g) ^ (c & kExchange)));
       __builtin_amdgcn_sched_barrier(0);
     };
+    Next next;
     read_keys(0);
 #pragma unroll
     for (int j = 0; j < KK / 2; ++j) {
@@ -187,14 +202,19 @@ __device__ __forceinline__ void attend_block(const AttendArgs& a, const Partitio
       for (int i = 0; i < 4; ++i)
         sc[i % 2] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f[j % 2][i], qf[2 * j + i / 2], sc[i % 2], 0, 0, 0);
       store_piece(buf ^ 1, j);
+      if (j == 0) {
+        next = find(ids);
+        ids = pages(tile + 3 * KG);
+      }
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        __builtin_amdgcn_sched_group_barrier(kProducts, 1, 0);
+        __builtin_amdgcn_sched_group_barrier(kVector | kScalar, 8, 0);
+      }
       __builtin_amdgcn_sched_barrier(0);
     }
     const uint32_t in_stored = in_next;
-    {
-      const int now = ids;
-      ids = pages(tile + 3 * KG);
-      load(tile + 2 * KG, now);
-    }
+    load(tile + 2 * KG, next);
     if (tile * kTile < blk.full_lo || tile * kTile + kTile > blk.full_hi || in != 0xfu) {
 #pragma unroll
       for (int t = 0; t < 2; ++t)
@@ -265,12 +285,12 @@ __device__ __forceinline__ void attend_block(const AttendArgs& a, const Partitio
   if (T0 < T1) {
     const int first = T0 + group, now = pages(first), then = pages(first + KG);
     ids = pages(first + 2 * KG);
-    load(first, now);
+    load(first, find(now));
     cut(first);
 #pragma unroll
     for (int i = 0; i < kKeyPieces + kValPieces; ++i) store_piece(0, i);
     in = in_next;
-    load(first + KG, then);
+    load(first + KG, find(then));
     for (int tile = T0; tile < T1; tile += 2 * KG) {  // (the same number of turns in every group)
       turn(tile + group, std::integral_constant<int, 0>{});
       if (tile + KG < T1) turn(tile + KG + group, std::integral_constant<int, 1>{});
