@@ -131,16 +131,22 @@ __device__ __forceinline__ void attend_block(const AttendArgs& a, const Partitio
     const uint32_t lo = __builtin_amdgcn_readlane(uint32_t(x), i), hi = __builtin_amdgcn_readlane(uint32_t(x >> 32), i);
     return uint64_t(hi) << 32 | lo;
   };
-  auto load = [&](int tile, const Next& n) {
+  auto load_piece = [&](int tile, const Next& n, int i) {  // keys' pieces, then values'
     const uint32_t first = min(tile, T1 - 1) * kTile;
+    if (i < kKeyPieces) {
+      const uint32_t in_page = ((first + 16 * key_block(i)) & (P - 1)) * D;
+      kx[i] = *reinterpret_cast<const u32x4*>(kbase + lane_of64(n.page, key_block(i)) + (in_page + koff));
+    } else if (i < kKeyPieces + kValPieces) {
+      const int k = i - kKeyPieces;
+      const uint32_t in_page = (first + 16 * w) & (P - 1);
+      vx[k] = *reinterpret_cast<const u32x4*>(vbase + lane_of64(n.page, w) + (in_page + 64 * k * P + voff));
+    }
+  };
+  auto loaded = [&](const Next& n) { ks4 = n.ks, vs4 = n.vs, in_next = n.in; };
+  auto load = [&](int tile, const Next& n) {
 #pragma unroll
-    for (int i = 0; i < kKeyPieces; ++i)
-      kx[i] = *reinterpret_cast<const u32x4*>(kbase + lane_of64(n.page, key_block(i)) +
-                                              (((first + 16 * key_block(i)) & (P - 1)) * D + koff));
-    const uint8_t* const values = vbase + lane_of64(n.page, w) + ((first + 16 * w) & (P - 1));
-#pragma unroll
-    for (int i = 0; i < kValPieces; ++i) vx[i] = *reinterpret_cast<const u32x4*>(values + (64 * i * P + voff));
-    ks4 = n.ks, vs4 = n.vs, in_next = n.in;
+    for (int i = 0; i < kKeyPieces + kValPieces; ++i) load_piece(tile, n, i);
+    loaded(n);
     __builtin_amdgcn_sched_barrier(0);
   };
   auto lane_of = [](float x, int i) { return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(x), i)); };
@@ -173,6 +179,7 @@ __device__ __forceinline__ void attend_block(const AttendArgs& a, const Partitio
 
   uint32_t in = 0;
   int ids = 0;
+  Next next;
   // One tile, in buffer `buf` (known to the compiler, which turns it into
   // offsets of the instructions).
   auto turn = [&](int tile, auto buffer) {
@@ -193,7 +200,6 @@ __device__ __forceinline__ void attend_block(const AttendArgs& a, const Partitio
                                                        8 * ((2 * (2 * j + i / 2) + g) ^ (c & kExchange)));
       __builtin_amdgcn_sched_barrier(0);
     };
-    Next next;
     read_keys(0);
 #pragma unroll
     for (int j = 0; j < KK / 2; ++j) {
@@ -201,20 +207,22 @@ __device__ __forceinline__ void attend_block(const AttendArgs& a, const Partitio
 #pragma unroll
       for (int i = 0; i < 4; ++i)
         sc[i % 2] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f[j % 2][i], qf[2 * j + i / 2], sc[i % 2], 0, 0, 0);
+      // a piece's registers are free with its store, and a load that goes out
+      // then has a whole turn to come back
       store_piece(buf ^ 1, j);
-      if (j == 0) {
-        next = find(ids);
-        ids = pages(tile + 3 * KG);
-      }
+      load_piece(tile + 2 * KG, next, j);
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         __builtin_amdgcn_sched_group_barrier(kProducts, 1, 0);
-        __builtin_amdgcn_sched_group_barrier(kVector | kScalar, 8, 0);
+        __builtin_amdgcn_sched_group_barrier(kVector | kScalar, 5, 0);
       }
       __builtin_amdgcn_sched_barrier(0);
     }
     const uint32_t in_stored = in_next;
-    load(tile + 2 * KG, next);
+    loaded(next);
+    next = find(ids);
+    ids = pages(tile + 4 * KG);
+    __builtin_amdgcn_sched_barrier(0);
     if (tile * kTile < blk.full_lo || tile * kTile + kTile > blk.full_hi || in != 0xfu) {
 #pragma unroll
       for (int t = 0; t < 2; ++t)
@@ -284,13 +292,15 @@ __device__ __forceinline__ void attend_block(const AttendArgs& a, const Partitio
   };
   if (T0 < T1) {
     const int first = T0 + group, now = pages(first), then = pages(first + KG);
-    ids = pages(first + 2 * KG);
+    const int after = pages(first + 2 * KG);
+    ids = pages(first + 3 * KG);
     load(first, find(now));
     cut(first);
 #pragma unroll
     for (int i = 0; i < kKeyPieces + kValPieces; ++i) store_piece(0, i);
     in = in_next;
     load(first + KG, find(then));
+    next = find(after);
     for (int tile = T0; tile < T1; tile += 2 * KG) {  // (the same number of turns in every group)
       turn(tile + group, std::integral_constant<int, 0>{});
       if (tile + KG < T1) turn(tile + KG + group, std::integral_constant<int, 1>{});
