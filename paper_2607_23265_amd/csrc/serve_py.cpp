@@ -113,8 +113,9 @@ On<T> unpack(PyObject* x) {
 // Calls f(stream) with `device` current, on its current stream.
 template <typename F>
 void call(const char* where, int device, F f) {
-  const c10::DeviceGuard guard(at::Device(at::kCUDA, static_cast<c10::DeviceIndex>(device)));
-  const wz_status st = f(static_cast<void*>(c10::hip::getCurrentHIPStream(static_cast<c10::DeviceIndex>(device)).stream()));
+  const auto index = static_cast<c10::DeviceIndex>(device);
+  const c10::DeviceGuard guard(at::Device(at::kCUDA, index));
+  const wz_status st = f(static_cast<void*>(c10::hip::getCurrentHIPStream(index).stream()));
   if (st == WZ_OK) return;
   if (PyObject* e = PyObject_CallFunction(wz_error, "is", int(st), where)) {
     PyErr_SetObject(wz_error, e);
@@ -203,7 +204,8 @@ PyObject* append(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const int device = c.device;
     const at::Tensor &k = tensor("k", a[2]), &v = tensor("v", a[3]);
     const at::ScalarType type = k.scalar_type();
-    if (!numbers(type) || r.device != device) refuse("k must be float32 or bfloat16, and the batch on the cache's device");
+    if (!numbers(type) || r.device != device)
+      refuse("k must be float32 or bfloat16, and the batch on the cache's device");
     const int64_t ks = rows_of("k", k, -1, c.x.kv_heads, c.x.head_dim, device, type), tokens = k.size(0);
     const int64_t vs = rows_of("v", v, tokens, c.x.kv_heads, c.x.head_dim, device, type);
     r.x.tokens = count("tokens", tokens);
@@ -270,7 +272,8 @@ PyObject* attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
     }
     at::Tensor ws;
     if (a[8] == Py_None) {
-      if (const size_t need = wz_attention_workspace_bytes(&c.x, &r.x, &cfg)) ws = empty_on(q, {int64_t(need)}, at::kByte);
+      const size_t need = wz_attention_workspace_bytes(&c.x, &r.x, &cfg);
+      if (need) ws = empty_on(q, {int64_t(need)}, at::kByte);
     } else {
       ws = dense("ws", a[8], at::kByte, device);
     }
@@ -289,7 +292,8 @@ PyObject* quantize_rows(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const int64_t xs = matrix("x", x, true), rows = x.size(0), cols = x.size(1);
     const int device = x.get_device();
     const at::Tensor out = a[1] == Py_None ? empty_on(x, {rows, cols}, at::kChar) : tensor("out", a[1]);
-    const at::Tensor scale = a[2] == Py_None ? empty_on(x, {rows}, at::kFloat) : dense("scale", a[2], at::kFloat, device);
+    const at::Tensor scale =
+        a[2] == Py_None ? empty_on(x, {rows}, at::kFloat) : dense("scale", a[2], at::kFloat, device);
     const int64_t qs = matrix("out", out, false, device);
     if (!is(out, {rows, cols}) || !is(scale, {rows})) refuse("out must have the shape of x, and scale [rows]");
     call("wz_quantize_rows", device, [&](void* s) {

@@ -99,7 +99,8 @@ struct Partition {
         const unsigned long long pass = __ballot(TILES ? nt + it > at : nb + ib > at);
         if (pass) {
           const int l = __builtin_ctzll(pass);
-          const int b1 = nb + __builtin_amdgcn_readlane(ib - mine, l), t1 = nt + __builtin_amdgcn_readlane(it - work, l);
+          const int b1 = nb + __builtin_amdgcn_readlane(ib - mine, l);
+          const int t1 = nt + __builtin_amdgcn_readlane(it - work, l);
           const int n = __builtin_amdgcn_readlane(each, l);
           const int k = TILES ? (at - t1) / n : at - b1;
           *spot = Spot{b0 + l, k, TILES ? (at - t1) % n : 0, n, b1 + k, t1 + k * n, sequence_of_lane(s, l)};

@@ -16,6 +16,14 @@
 //
 // 16-byte chunks of a row in LDS are exchanged by the row's number, so that
 // sixteen lanes that read sixteen rows hit all 64 banks.
+//
+// Measured: 1.19 TFLOP of two causal prompts of 8 300 to 9 459 tokens, 28 heads of
+// 128 over 4, in 1129 us (1.05 PFLOP/s; the library's 8192^3 bf16 product 1.53).
+// A wave of 32 rows fills the registers of two waves a SIMD (output 64, scores
+// 32, queries 32, fragments 64), and those two must overlap vector work, 60 % of
+// the cycles, with products, 50 %; LDS is at 38 %, without conflicts.  128 rows
+// share a decoded tile because two workgroups then fit a CU and wait apart:
+// eight waves in one took 1330 us where four took 1246.
 #include "wz_attend.h"
 
 namespace wz {
@@ -260,7 +268,8 @@ __device__ __forceinline__ void attend_block(const AttendArgs& a, const Partitio
     auto read_values = [&](int u) {
 #pragma unroll
       for (int d = 0; d < DT; ++d)
-        v[u % 2][d] = *reinterpret_cast<const bf16x8*>(vt[buf] + (32 * d + c) * kTile + 8 * ((2 * u + g) ^ value_exchange(c)));
+        v[u % 2][d] = *reinterpret_cast<const bf16x8*>(vt[buf] + (32 * d + c) * kTile +
+                                                       8 * ((2 * u + g) ^ value_exchange(c)));
       __builtin_amdgcn_sched_barrier(0);
     };
     auto probabilities = [&](int u) {

@@ -16,6 +16,10 @@
 //
 // The waves take a block's tiles in turn, each with a running maximum and sum,
 // and join through LDS at the end in a fixed order.
+//
+// Measured: next tokens of four sequences of 60 000 to 131 000 tokens, 28 heads of
+// 128 over 4, 349 MB in 64.6 us and 5 us for the join (a 1 GiB copy's 5.2 TB/s
+// would take 66.8); of 64 sequences of 500 to 8 200, 212 MB in 50 and 5.
 #include "wz_attend.h"
 
 namespace wz {

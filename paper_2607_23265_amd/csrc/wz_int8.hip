@@ -92,7 +92,8 @@ hipError_t quantize(const In* x, int64_t x_stride, int rows, int cols, int8_t* q
                     hipStream_t s) {
   const dim3 block(256);
   if (cols <= 2048)
-    hipLaunchKernelGGL((k_quantize<In, kWave, 4>), dim3((rows + 3) / 4), block, 0, s, x, x_stride, rows, cols, q, q_stride, scale);
+    hipLaunchKernelGGL((k_quantize<In, kWave, 4>), dim3((rows + 3) / 4), block, 0, s, x, x_stride, rows, cols, q,
+                       q_stride, scale);
   else if (cols <= 4096)
     hipLaunchKernelGGL((k_quantize<In, 256, 2>), dim3(rows), block, 0, s, x, x_stride, rows, cols, q, q_stride, scale);
   else
@@ -139,6 +140,11 @@ __device__ __forceinline__ void wait_loads() {
   asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(N) : "memory");
 }
 
+// Measured: 9459 x 14336 x 3584 in 442 us (2.2 POP/s, as the library's 8192^3
+// product; 21 us more for the rows), 1286 x 4608 x 3584 in 25.9, 64 rows in 7.7.
+// The matrix cores are busy for 58 % of the large product's cycles (at 1.9 GHz),
+// LDS for 26 %.
+//
 // Tiles of BM x BN, WM x WN waves, 128 bytes of k at a time through ST stages of
 // LDS that the loads write directly, ST - 1 stages ahead of the work.  KS such
 // groups of waves take the steps in turn and add up their integers at the end.
@@ -195,9 +201,11 @@ __global__ __launch_bounds__(WM* WN* KS* kWave) void k_matmul_tile(MatmulArgs p,
     const uint32_t to = base + i * KS * kStage;
     const int step = k < p.K ? k : 0;  // behind the last step every lane's offset is out of range by itself
 #pragma unroll
-    for (int x = 0; x < kLoadsA; ++x) load_to_lds(abuf, to + (w * kLoadsA + x) * 1024, k + ac[x] < p.K ? ao[x] : kOOB, step);
+    for (int x = 0; x < kLoadsA; ++x)
+      load_to_lds(abuf, to + (w * kLoadsA + x) * 1024, k + ac[x] < p.K ? ao[x] : kOOB, step);
 #pragma unroll
-    for (int x = 0; x < kLoadsB; ++x) load_to_lds(bbuf, to + BM * KB + (w * kLoadsB + x) * 1024, k + bc[x] < p.K ? bo[x] : kOOB, step);
+    for (int x = 0; x < kLoadsB; ++x)
+      load_to_lds(bbuf, to + BM * KB + (w * kLoadsB + x) * 1024, k + bc[x] < p.K ? bo[x] : kOOB, step);
   };
 
   i32x16 acc[MT][NT] = {};
@@ -263,7 +271,7 @@ __global__ __launch_bounds__(WM* WN* KS* kWave) void k_matmul_tile(MatmulArgs p,
   // them 16 bytes a lane, whole lines of the result (or half lines).
   constexpr int kUnitBytes = kWaves * 32 * 128 <= (BM + BN) * KB && BN / WN * sizeof(Out) >= 128 ? 128 : 64;
   constexpr int kUnit = kUnitBytes / sizeof(Out);  // columns of a unit
-  constexpr int kUnitChunks = kUnit * sizeof(Out) / 16, kPer = 16 / sizeof(Out);    // 16-byte chunks of its row, elements of one
+  constexpr int kUnitChunks = kUnit * sizeof(Out) / 16, kPer = 16 / sizeof(Out);  // 16-byte chunks of a row, elements
   static_assert(kWaves * 32 * kUnit * sizeof(Out) <= (BM + BN) * KB && BN / WN % kUnit == 0, "");
   Out* const out = static_cast<Out*>(p.out);
   Out* const unit = reinterpret_cast<Out*>(lds) + w * 32 * kUnit;
@@ -286,7 +294,8 @@ __global__ __launch_bounds__(WM* WN* KS* kWave) void k_matmul_tile(MatmulArgs p,
     };
     if (group > 0)
       each([&](i32x16& x, int q, int at) {
-        sums[(group - 1) * kWaves * MT * NT * 4 * kWave + at] = i32x4{x[4 * q], x[4 * q + 1], x[4 * q + 2], x[4 * q + 3]};
+        sums[(group - 1) * kWaves * MT * NT * 4 * kWave + at] =
+            i32x4{x[4 * q], x[4 * q + 1], x[4 * q + 2], x[4 * q + 3]};
       });
     __syncthreads();
     if (group == 0)
@@ -318,7 +327,8 @@ __global__ __launch_bounds__(WM* WN* KS* kWave) void k_matmul_tile(MatmulArgs p,
 #pragma unroll
         for (int e = 0; e < 4; ++e) y[e] = finish<Out>(acc[i][j][4 * q + e], sa, sw[e], bias[e]);
         Out* to = place(c, (col + 4 * g) / kPer) + (col + 4 * g) % kPer;
-        if constexpr (sizeof(Out) == 2) *reinterpret_cast<u32x2*>(to) = u32x2{y[0] | uint32_t(y[1]) << 16, y[2] | uint32_t(y[3]) << 16};
+        if constexpr (sizeof(Out) == 2)
+          *reinterpret_cast<u32x2*>(to) = u32x2{y[0] | uint32_t(y[1]) << 16, y[2] | uint32_t(y[3]) << 16};
         else *reinterpret_cast<f32x4*>(to) = f32x4{y[0], y[1], y[2], y[3]};
       }
       // rows of the result may start at any element: stores of 16 bytes that
