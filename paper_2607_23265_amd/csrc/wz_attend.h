@@ -23,6 +23,7 @@ namespace wz {
 
 constexpr int kTile = 64;       // tokens of a tile
 constexpr int kMinRun = 4;      // tiles of a workgroup's run at least
+constexpr int kStartTiles = 3;  // few rows: what beginning a block counts as
 
 // Whether blocks are cut by themselves, and the tiles of their pieces at most: the
 // pieces, total / run and one more for each block at most, must not outnumber
@@ -71,6 +72,11 @@ struct Partition {
   // sequence count as many as the widest may span, so that the sequence's sum
   // is a product.
   static constexpr bool kUniform = BR <= 64;
+  // A block counts as kStart tiles more than it has, at its front: what a
+  // workgroup loses when it begins one (next tokens of 64 sequences of 500 to
+  // 8 200 tokens 54.3 us without, 51.9, 51.5 and 51.3 with 2, 3 and 5; of 64 others
+  // 41.4, 41.0, 37.9 and 37.4; but few rows of 12 long sequences 94, 94, 93 and 99).
+  static constexpr int kStart = kUniform ? kStartTiles : 0;
   __device__ __forceinline__ int tiles(const Seq& s, int k) const {
     if constexpr (kUniform) {
       const int all = max(1, (s.kv + kTile - 1) / kTile);
@@ -93,7 +99,7 @@ struct Partition {
       const Seq s = in ? sequence(a.batch, b0 + lane) : Seq{0, 0, 0, 0};
       const int mine = blocks(s);
       if constexpr (kUniform) {
-        const int all = tiles(s, 0), each = lone ? (all + run - 1) / run : all;
+        const int all = tiles(s, 0), each = lone ? (all + run - 1) / run : all + kStart;
         const int work = a.shared ? mine * each : 0;  // (unshared, tiles are not asked for)
         const int ib = wave_incl_scan_i32(mine), it = wave_incl_scan_i32(work);
         const unsigned long long pass = __ballot(TILES ? nt + it > at : nb + ib > at);
@@ -170,9 +176,11 @@ struct Partition {
     // (rows that overlap, against the contract, may make more blocks than the
     // workspace has slots for)
     while (at < end && find<true>(at, &x) && x.block < a.blocks) {
-      const int count = min(end - at, x.tiles - x.off);
-      f(x, count, count == x.tiles ? -1 : me + x.block);
+      const int count = min(end - at, x.tiles - x.off), slot = count == x.tiles ? -1 : me + x.block;
+      const int to = max(x.off + count - kStart, 0);
       at += count;
+      x.off = max(x.off - kStart, 0);
+      f(x, to - x.off, slot);
       if (at < end) __syncthreads();  // LDS is used again
     }
   }

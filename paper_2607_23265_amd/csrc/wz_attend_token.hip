@@ -19,7 +19,7 @@
 //
 // Measured: next tokens of four sequences of 60 000 to 131 000 tokens, 28 heads of
 // 128 over 4, 349 MB in 64.6 us and 5 us for the join (a 1 GiB copy's 5.2 TB/s
-// would take 66.8); of 64 sequences of 500 to 8 200, 212 MB in 50 and 5.
+// would take 66.8); of 64 sequences of 500 to 8 200, 212 MB in 47 and 5.
 #include "wz_attend.h"
 
 namespace wz {
@@ -401,7 +401,7 @@ AttendPlan attend_plan(const wz_cache& c, const wz_ragged& r, int q_heads) {
     long_enough = (tiles + waves - 1) / waves >= (run + 3) / 4 + 2;
   }
   // (every sequence at its bounds, so that no array's contents make the tiles pass 32 bits)
-  const int64_t most = int64_t(r.batch) * ((rows + p.block_rows - 1) / p.block_rows) * (tiles + 1);
+  const int64_t most = int64_t(r.batch) * ((rows + p.block_rows - 1) / p.block_rows) * (tiles + 1 + kStartTiles);
   p.shared = long_enough && most < (int64_t(1) << 30) &&
              (p.block_rows > 64 ? p.blocks < p.workers : int64_t(p.blocks) * c.kv_heads < 2048);
   p.slots = p.blocks + p.workers;
