@@ -231,6 +231,11 @@ __device__ void append_page(const AppendArgs& a, int b, const Seq& q, int nth, i
   float* const kscale = a.cache.k_scale + int64_t(page) * Hkv + h;
   float* const vscale = a.cache.v_scale + int64_t(page) * Hkv + h;
   const float ok = s0 > 0 ? *kscale : 0.f, ov = s0 > 0 ? *vscale : 0.f;
+  Angles angle[kPasses];
+#pragma unroll
+  for (int i = 0; i < kPasses; ++i)
+    if (ch.turned && !empty(i * kRows, kRows))
+      angles(a.turn, a.batch.tokens, row_of(krow + i * kRows), lane, position[i], angle[i]);
   __syncthreads();  // `bad` is clear
   float kx[kPasses][2][8];
   float kmax = 0.f, vmax = 0.f;
@@ -239,11 +244,7 @@ __device__ void append_page(const AppendArgs& a, int b, const Seq& q, int nth, i
     if (empty(i * kRows, kRows)) continue;
     const int slot = krow + i * kRows;
     kr[i][0].get(kx[i][0]), kr[i][1].get(kx[i][1]);
-    if (ch.turned) {
-      Angles x;
-      angles(a.turn, a.batch.tokens, row_of(slot), lane, position[i], x);
-      turn(x, a.turn.interleaved, kx[i][0], kx[i][1]);
-    }
+    if (ch.turned) turn(angle[i], a.turn.interleaved, kx[i][0], kx[i][1]);
     if (slot >= s0 && slot < s1) {
       bool nan = false;
 #pragma unroll
