@@ -387,12 +387,14 @@ struct Tile {
 
 template <typename Out>
 hipError_t matmul(const MatmulArgs& p, hipStream_t s) {
-  // Few rows: where even the smallest tiles are too few for the CUs, four groups
-  // of waves share the steps of a 32 x 32 tile (M <= 32: 6.3 us for 4608 columns,
-  // a 64 x 64 tile 8.8), or two those of a 64 x 32 tile (M <= 64: 7.7 against 9.2).
+  // Where 32 x 32 or 64 x 32 tiles are no more than the CUs, a product waits for
+  // its steps of K one after the other: four groups of waves share those of a 32
+  // x 32 tile, two those of a 64 x 32 tile (a row of 4608 columns: 6.1 us, in 64 x
+  // 64 tiles 8.8; 64 rows 7.7 against 9.2; 300 x 256 x 8192: 9.1, 11.3 and 13.9 in
+  // tiles of 32 x 32, 64 x 32 and 64 x 64).
   auto count = [&](int bm, int bn) { return (int64_t(p.M) + bm - 1) / bm * ((int64_t(p.N) + bn - 1) / bn); };
-  if (p.M <= 32 && count(32, 32) <= kCUs) return tiles<Out, 32, 32, 1, 1, 4, 4>(p, s);
-  if (p.M <= 64 && count(64, 32) <= kCUs) return tiles<Out, 64, 32, 2, 1, 4, 2>(p, s);
+  if (count(32, 32) <= kCUs) return tiles<Out, 32, 32, 1, 1, 4, 4>(p, s);
+  if (count(64, 32) <= kCUs) return tiles<Out, 64, 32, 2, 1, 4, 2>(p, s);
   static constexpr Tile<Out> kTiles[] = {
       {64, 64, 3.6, 5.8, 1, tiles<Out, 64, 64, 2, 2, 4, 1>},
       {128, 64, 4.6, 9.4, 1, tiles<Out, 128, 64, 2, 2, 3, 1>},
