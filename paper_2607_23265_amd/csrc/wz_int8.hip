@@ -361,24 +361,24 @@ hipError_t tiles(const MatmulArgs& p, hipStream_t s) {
   return hipGetLastError();
 }
 
-// A tile's time, measured with K = 3584 (us; the part of a round scales with K):
-// a launch takes `fixed` and `round` for every round of the CUs, which work on
-// `at_once` tiles each; the last round, with a share f of its tiles, takes 0.6 +
-// 0.4 f of one (256 x 256 tiles: 41.3 us with 108, 57.6 with 256, 149 with 666).
-// Large tiles read LDS less for the same products, small ones fill the chip; three
-// stages hide a step's loads behind two others where a CU has one tile (128 x
-// 128: 20.8 us with three, 23.5 with two), and two leave room for a second tile
-// (33.1 for both).
+// A tile's time, measured (us): a launch takes `fixed`, and for every round of the
+// CUs, which work on `at_once` tiles each, `ends` for the tiles' first loads and
+// their results and `steps` for 3584 of K; the last round, with a share f of its
+// tiles, takes 0.6 + 0.4 f of one (256 x 256 tiles: 41.3 us with 108, 57.6 with 256,
+// 149 with 666).  Large tiles read LDS less for the same products, small ones fill
+// the chip; three stages hide a step's loads behind two others where a CU has one
+// tile (128 x 128: 20.8 us with three, 23.5 with two), and two leave room for a
+// second tile (33.1 for both).
 template <typename Out>
 struct Tile {
   int bm, bn;
-  double fixed, round;
+  double fixed, ends, steps;
   int at_once;
   hipError_t (*run)(const MatmulArgs&, hipStream_t);
 
   int64_t columns(const MatmulArgs& p) const { return (int64_t(p.N) + bn - 1) / bn; }
   int64_t count(const MatmulArgs& p) const { return (int64_t(p.M) + bm - 1) / bm * columns(p); }
-  double time(const MatmulArgs& p, double rounds) const { return fixed + round * (p.K / 3584.) * rounds; }
+  double time(const MatmulArgs& p, double rounds) const { return fixed + rounds * (ends + steps * (p.K / 3584.)); }
   double time(const MatmulArgs& p) const {
     const double rounds = double(count(p)) / (kCUs * at_once), full = std::floor(rounds), f = rounds - full;
     return time(p, full + (f > 0 ? 0.6 + 0.4 * f : 0.));
@@ -396,12 +396,12 @@ hipError_t matmul(const MatmulArgs& p, hipStream_t s) {
   if (count(32, 32) <= kCUs) return tiles<Out, 32, 32, 1, 1, 4, 4>(p, s);
   if (count(64, 32) <= kCUs) return tiles<Out, 64, 32, 2, 1, 4, 2>(p, s);
   static constexpr Tile<Out> kTiles[] = {
-      {64, 64, 3.6, 5.8, 1, tiles<Out, 64, 64, 2, 2, 4, 1>},
-      {128, 64, 4.6, 9.4, 1, tiles<Out, 128, 64, 2, 2, 3, 1>},
-      {128, 128, 3.3, 17.6, 1, tiles<Out, 128, 128, 2, 2, 3, 1>},
-      {128, 128, 3.0, 30.2, 2, tiles<Out, 128, 128, 2, 2, 2, 1>},
-      {192, 128, 3.4, 22.5, 1, tiles<Out, 192, 128, 2, 4, 3, 1>},
-      {256, 256, 8.0, 49.7, 1, tiles<Out, 256, 256, 2, 4, 2, 1>},
+      {64, 64, 3.9, 1.0, 4.7, 1, tiles<Out, 64, 64, 2, 2, 4, 1>},
+      {128, 64, 4.3, 1.35, 8.3, 1, tiles<Out, 128, 64, 2, 2, 3, 1>},
+      {128, 128, 3.1, 3.7, 14.0, 1, tiles<Out, 128, 128, 2, 2, 3, 1>},
+      {128, 128, 3.7, 3.9, 26.0, 2, tiles<Out, 128, 128, 2, 2, 2, 1>},
+      {192, 128, 2.5, 3.8, 19.6, 1, tiles<Out, 192, 128, 2, 4, 3, 1>},
+      {256, 256, 8.0, 5.0, 44.6, 1, tiles<Out, 256, 256, 2, 4, 2, 1>},
   };
   auto fastest = [&](const MatmulArgs& q) {
     const Tile<Out>* best = kTiles;

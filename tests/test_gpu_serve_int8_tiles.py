@@ -13,11 +13,15 @@ from paper_2607_23265_amd import serve
 pytestmark = pytest.mark.gpu
 DEV = "cuda:0"
 
-SHAPES = [(300, 3600, 1040),    # tiles of 64 x 64
-          (128, 14330, 3600),   # 128 x 64
-          (700, 4500, 1040),    # 128 x 128, one to a CU
+SHAPES = [(70, 510, 8192),      # 32 x 32, four groups of waves
+          (500, 1020, 2064),    # 64 x 32, two
+          (190, 4990, 528),     # 64 x 64
+          (300, 3600, 1040),    # 128 x 64
+          (128, 14330, 3600),
+          (690, 4590, 3600),    # 128 x 128, one to a CU
           (1500, 4100, 1040),   # 128 x 128, two
-          (1290, 4604, 1040),   # 192 x 128
+          (700, 4500, 1040),    # 192 x 128
+          (1290, 4604, 1040),
           (3900, 4090, 2064),   # 256 x 256
           (2318, 14330, 2064)]  # 2304 rows in tiles of 256 x 256, 14 in small ones
 
