@@ -129,7 +129,7 @@ typedef struct {
 /* Bytes of workspace wz_cache_attention needs (0 if the arguments are invalid
  * or none is needed): partial results of rows whose tokens several
  * workgroups share, at most 128 MiB.  Depends on batch, tokens, max_tokens,
- * max_kv and the head counts alone, not on the arrays' contents.             */
+ * max_kv, the head counts and the window alone, not on the arrays' contents. */
 size_t wz_attention_workspace_bytes(const wz_cache* cache,
                                     const wz_ragged* batch,
                                     const wz_attention* cfg);

@@ -237,12 +237,13 @@ PyObject* append(PyObject*, PyObject* const* a, Py_ssize_t n) {
   });
 }
 
-// (cache, batch, q_heads, tokens) -> bytes of workspace
+// (cache, batch, q_heads, tokens, window) -> bytes of workspace
 PyObject* workspace(PyObject*, PyObject* const* a, Py_ssize_t n) {
-  return guarded(n, 4, [&] {
+  return guarded(n, 5, [&] {
     const auto c = unpack<wz_cache>(a[0]);
     auto r = unpack<wz_ragged>(a[1]);
-    const wz_attention cfg{int32_t(integer("q_heads", a[2])), 0, 0, 1.f};
+    const int32_t window = int32_t(integer("window", a[4]));
+    const wz_attention cfg{int32_t(integer("q_heads", a[2])), window > 0, window, 1.f};
     r.x.tokens = int32_t(integer("tokens", a[3]));
     return PyLong_FromSize_t(wz_attention_workspace_bytes(&c.x, &r.x, &cfg));
   });

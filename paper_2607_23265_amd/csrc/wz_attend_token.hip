@@ -361,15 +361,19 @@ hipError_t join(const AttendArgs& a, const AttendPlan& p, hipStream_t s) {
 template <int D>
 void launch_token(const AttendArgs& a, const AttendPlan& p, int64_t groups, hipStream_t s) {
   const dim3 grid{uint32_t(groups)}, four{4 * kWave}, eight{8 * kWave};
-  if (p.block_rows == 64) hipLaunchKernelGGL((k_attend_token<D, 4, 4>), grid, four, 0, s, a);
-  else if (p.block_rows == 32) hipLaunchKernelGGL((k_attend_token<D, 2, 4>), grid, four, 0, s, a);
+  if constexpr (D == 64)
+    if (p.block_rows == 64) {
+      hipLaunchKernelGGL((k_attend_token<D, 4, 4>), grid, four, 0, s, a);
+      return;
+    }
+  if (p.block_rows == 32) hipLaunchKernelGGL((k_attend_token<D, 2, 4>), grid, four, 0, s, a);
   else if (!p.shared && groups <= kCUs) hipLaunchKernelGGL((k_attend_token<D, 1, 8>), grid, eight, 0, s, a);
   else hipLaunchKernelGGL((k_attend_token<D, 1, 4>), grid, four, 0, s, a);
 }
 
 }  // namespace
 
-AttendPlan attend_plan(const wz_cache& c, const wz_ragged& r, int q_heads) {
+AttendPlan attend_plan(const wz_cache& c, const wz_ragged& r, int q_heads, int window) {
   const int G = q_heads / c.kv_heads;
   const int64_t rows = int64_t(r.max_tokens) * G;
   AttendPlan p{};
@@ -377,17 +381,24 @@ AttendPlan attend_plan(const wz_cache& c, const wz_ragged& r, int q_heads) {
     const int64_t each = (rows + br - 1) / br;
     return std::min({int64_t(r.batch) * each, int64_t(r.tokens) * G / br + r.batch, int64_t(r.tokens) * G});
   };
-  p.block_rows = rows <= 16 ? 16 : rows <= 32 ? 32 : rows <= 64 ? 64 : 128;
+  // (64 rows of 128 elements would not fit a wave's registers: two blocks of 32
+  // read the keys twice, the second time from L2: 35 rows each of 32 sequences of
+  // 950 tokens 19 us, as blocks of 64 46 and of 128 26)
+  p.block_rows = rows <= 16 ? 16 : rows <= 32 ? 32 : rows <= 64 ? (c.head_dim == 64 ? 64 : 32) : 128;
   p.blocks = int(std::min(blocks(p.block_rows), int64_t(1) << 28));
-  const int64_t tiles = (int64_t(r.max_kv) + kTile - 1) / kTile;
-  // A CU runs two workgroups of four waves at once, or one prompt workgroup of
+  int64_t tiles = (int64_t(r.max_kv) + kTile - 1) / kTile;
+  if (window > 0) tiles = std::min(tiles, (int64_t(window) + (p.block_rows - 1) / G + kTile) / kTile + 1);
+  // A CU runs two workgroups of four waves at once, or one of those whose waves
+  // take more than half the registers (with two planned for, 28 rows each of 10
+  // sequences of 2000 tokens took 30 us instead of 20), or one prompt workgroup of
   // eight, which is faster while blocks are about as many as CUs or fewer
   // (shared, it leaves half as many parts).  Registers would hold four of few
   // rows: more parts, shorter runs, and 74 us instead of 70 for the next tokens of
   // four sequences of 60 000 to 131 000 (three: 72; of 64 of 500 to 8 200: 55 with
   // two, 63, 54).
   p.groups = int64_t(p.blocks) * c.kv_heads <= kCUs * 5 / 4 ? 2 : 1;
-  const int at_once = p.block_rows == 128 && p.groups == 2 ? kCUs : 2 * kCUs;
+  const bool wide = p.block_rows == 64 || (p.block_rows == 32 && c.head_dim == 128);
+  const int at_once = wide || (p.block_rows == 128 && p.groups == 2) ? kCUs : 2 * kCUs;
   p.workers = int(std::max(1, at_once / c.kv_heads));
   // Few rows in few blocks: sharing costs a second launch, which is worth two of
   // the rounds that the waves of the block's only workgroup (eight) or of a
@@ -430,7 +441,7 @@ hipError_t launch_attend(const AttendArgs& a, const AttendPlan& p, hipStream_t s
   switch (p.block_rows) {
     case 16: return D == 128 ? join<128, 16>(a, p, s) : join<64, 16>(a, p, s);
     case 32: return D == 128 ? join<128, 32>(a, p, s) : join<64, 32>(a, p, s);
-    case 64: return D == 128 ? join<128, 64>(a, p, s) : join<64, 64>(a, p, s);
+    case 64: return join<64, 64>(a, p, s);
     default: return D == 128 ? join<128, 128>(a, p, s) : join<64, 128>(a, p, s);
   }
 }

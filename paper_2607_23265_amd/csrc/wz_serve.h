@@ -101,7 +101,7 @@ struct AttendArgs {
   float* part_ml;    // shared: [slots][kv_heads][rows of a block][2] maximum (log2) and sum
 };
 struct AttendPlan {
-  int block_rows;    // rows of a block: 16, 32, 64 (token kernel) or 128 (prompt kernel)
+  int block_rows;    // rows of a block: 16, 32, 64 (token kernel; 64: of 64 elements) or 128 (prompt kernel)
   int groups;        // prompt kernel: of four waves that take a block's tiles in turn
   int blocks;        // upper bound of the batch's blocks, for each key/value head
   int workers;       // shared: workgroups for each key/value head
@@ -109,7 +109,7 @@ struct AttendPlan {
   bool shared;       // several workgroups share a block's tokens
   size_t part_bytes, ml_bytes, bytes;
 };
-AttendPlan attend_plan(const wz_cache& c, const wz_ragged& r, int q_heads);
+AttendPlan attend_plan(const wz_cache& c, const wz_ragged& r, int q_heads, int window);
 hipError_t launch_attend(const AttendArgs& a, const AttendPlan& p, hipStream_t s);
 hipError_t launch_attend_prompt(const AttendArgs& a, const AttendPlan& p, hipStream_t s);
 

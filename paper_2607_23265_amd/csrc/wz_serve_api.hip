@@ -63,7 +63,7 @@ wz_status check_attention(const wz_cache* cache, const wz_ragged* batch, const w
   if ((cfg->causal != 0 && cfg->causal != 1) || cfg->window < 0 || (cfg->window > 0 && !cfg->causal) ||
       !std::isfinite(cfg->scale))
     return WZ_ERR_PARAM;
-  const AttendPlan p = attend_plan(*cache, *batch, cfg->q_heads);
+  const AttendPlan p = attend_plan(*cache, *batch, cfg->q_heads, cfg->window);
   if (int64_t(p.slots) * cache->kv_heads > kMostGroups) return WZ_ERR_SHAPE;
   return WZ_OK;
 }
@@ -121,7 +121,7 @@ wz_status wz_cache_append(const wz_cache* cache, const wz_ragged* batch, const w
 
 size_t wz_attention_workspace_bytes(const wz_cache* cache, const wz_ragged* batch, const wz_attention* cfg) {
   if (check_attention(cache, batch, cfg) != WZ_OK) return 0;
-  return attend_plan(*cache, *batch, cfg->q_heads).bytes;
+  return attend_plan(*cache, *batch, cfg->q_heads, cfg->window).bytes;
 }
 
 wz_status wz_cache_attention(const wz_cache* cache, const wz_ragged* batch, const wz_attention* cfg, const void* q,
@@ -134,7 +134,7 @@ wz_status wz_cache_attention(const wz_cache* cache, const wz_ragged* batch, cons
   WZ_TRY(check_rows(q, q_stride, width));
   WZ_TRY(check_rows(out, out_stride, width));
   if (lse && !aligned(lse, 4)) return WZ_ERR_ALIGN;
-  const AttendPlan p = attend_plan(*cache, *batch, cfg->q_heads);
+  const AttendPlan p = attend_plan(*cache, *batch, cfg->q_heads, cfg->window);
   AttendArgs a{};
   if (p.shared) {
     if (!ws) return WZ_ERR_NULL;

@@ -141,9 +141,9 @@ def cache_append(cache, batch, k, v, rotation=None, positions=None, q=None, q_ou
     return _native.append(cache.c, batch.c, k, v, None if rotation is None else rotation.c, positions, q, q_out)
 
 
-def attention_workspace_bytes(cache, batch, q_heads, tokens):
-    """Bytes of workspace cache_attention() needs for `tokens` rows of q_heads heads."""
-    return _native.workspace(cache.c, batch.c, q_heads, tokens)
+def attention_workspace_bytes(cache, batch, q_heads, tokens, window=0):
+    """Bytes of workspace cache_attention() needs for `tokens` rows of q_heads heads (and that window)."""
+    return _native.workspace(cache.c, batch.c, q_heads, tokens, window)
 
 
 def cache_attention(cache, batch, q, scale=None, causal=True, window=0, out=None, lse=None, ws=None):

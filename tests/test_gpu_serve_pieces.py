@@ -24,6 +24,11 @@ CASES = [
     ([9, 2], [1900, 1100], 1, 7, 64, 32, True, 0, None),  # 63 rows
     ([16], [2100], 1, 4, 128, 16, False, 0, None),
     ([2, 1], [4000, 3000], 2, 4, 64, 64, True, 1500, None),
+    ([9, 5], [1900, 1100], 1, 7, 128, 32, True, 0, None),  # 63 and 35 rows: two blocks of 32 each
+    ([5] * 12, [900 + 60 * i for i in range(12)], 2, 14, 128, 16, True, 0, None),
+    ([5] * 3, [2600, 3000, 90], 2, 14, 128, 64, True, 300, None),
+    ([90], [4000], 2, 8, 128, 64, True, 211, None),       # a prompt whose window is short: not shared
+    ([16], [2100], 1, 4, 64, 16, False, 0, None),
     ([1] * 31, [1600 + 13 * i for i in range(31)], 4, 8, 64, 16, True, 0, None),
     ([1] * 33, [1600 + 13 * i for i in range(33)], 4, 8, 64, 16, True, 0, None),  # a block too many for it
 ]
