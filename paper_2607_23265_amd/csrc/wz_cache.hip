@@ -9,7 +9,7 @@
 // Workgroups behind those rotate the queries.
 //
 // Measured: 52 000 prompt tokens of eight sequences, 28 + 2 * 4 heads of 128, 851 MB
-// in 164 us (5.2 TB/s, as a 1 GiB copy); a token each of 64 sequences in 5.2 us,
+// in 162 us (5.3 TB/s, as a 1 GiB copy); a token each of 64 sequences in 5.0 us,
 // three waits for memory in a row behind the launch.
 #include "wz_serve.h"
 
