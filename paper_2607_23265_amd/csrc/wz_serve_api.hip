@@ -147,7 +147,9 @@ wz_status wz_cache_attention(const wz_cache* cache, const wz_ragged* batch, cons
   // (neither zero nor infinite: a masked score of -inf has to stay what it is)
   const float scale2 = cfg->scale * 1.44269504088896341f;
   a.scale2 = std::copysign(std::min(std::max(std::fabs(scale2), 0x1p-126f), 0x1.fffffep127f), scale2);
-  a.q_heads = cfg->q_heads, a.causal = cfg->causal, a.window = cfg->window;
+  // (no row sees kMostTokens places, so a longer window hides nothing either; places are above -kMostTokens, so a
+  // place less this one stays in 32 bits)
+  a.q_heads = cfg->q_heads, a.causal = cfg->causal, a.window = std::min(cfg->window, kMostTokens);
   a.blocks = p.blocks, a.workers = p.workers, a.shared = p.shared;
   a.block_rows = int(std::min(int64_t(p.block_rows), int64_t(batch->max_tokens) * (cfg->q_heads / cache->kv_heads)));
   return from_hip(launch_attend(a, p, static_cast<hipStream_t>(stream)));
