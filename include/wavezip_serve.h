@@ -94,8 +94,9 @@ typedef struct {
  * v_stride elements apart (multiples of 8, at least kv_heads * head_dim; the
  * pointers 16-byte aligned), so the parts of one fused projection can be
  * passed as they lie.  rotation may be NULL (nothing is rotated); v never is.
- * If q is not NULL its q_heads heads are rotated as well and written to q_out
- * (bf16, rows q_out_stride elements apart; q_out must not overlap q).
+ * If q is not NULL its q_heads heads are rotated as well, in all `tokens` rows,
+ * and written to q_out (bf16, rows q_out_stride elements apart; q_out must not
+ * overlap q).
  *
  * Of every page that receives tokens, keys and values each get the least
  * scale 2^e with |x| <= 448 * 2^e for all its new elements, but no less than
@@ -109,7 +110,8 @@ typedef struct {
  * and zeros for those elements of the value: exactly the output rows that
  * attend to it become NaN.
  *
- * One kernel launch (none when the batch has no tokens).                      */
+ * One kernel launch; none when the batch has no tokens, or when max_tokens is 0
+ * and q NULL.                                                                */
 wz_status wz_cache_append(const wz_cache* cache, const wz_ragged* batch,
                           const wz_rotation* rotation, const void* k,
                           int64_t k_stride, const void* v, int64_t v_stride,

@@ -438,8 +438,9 @@ Grid append_grid(const wz_cache& c, const wz_ragged& r, int q_heads) {
   Grid g{};
   // pages that receive tokens: at most one a token, (n + P - 2) / P + 1 a
   // sequence, and tokens / P and two more a sequence together
-  g.groups = c.kv_heads * std::min({int64_t(r.tokens), int64_t(r.batch) * ((r.max_tokens + P - 2) / P + 1),
-                                    int64_t(r.tokens / P) + 2 * int64_t(r.batch)});
+  if (r.max_tokens > 0)
+    g.groups = c.kv_heads * std::min({int64_t(r.tokens), int64_t(r.batch) * ((r.max_tokens + P - 2) / P + 1),
+                                      int64_t(r.tokens / P) + 2 * int64_t(r.batch)});
   g.heads_at_once = 1;  // a thread has four heads or more where there are as many
   while (g.heads_at_once < 8 && 4 * g.heads_at_once < q_heads) g.heads_at_once *= 2;
   const int per = kThreads / (c.head_dim / 16) / g.heads_at_once;
@@ -455,8 +456,8 @@ int64_t append_groups(const wz_cache& c, const wz_ragged& r, int q_heads) {
 }
 
 hipError_t launch_append(const AppendArgs& a, int in_dtype, hipStream_t s) {
-  if (a.batch.tokens == 0 || a.batch.max_tokens == 0) return hipSuccess;
   const Grid g = append_grid(a.cache, a.batch, a.q_heads);
+  if (g.groups + g.units == 0) return hipSuccess;
   const int groups = int(g.groups), units = int(g.units);
   const bool bf = in_dtype == WZ_BF16;
   if (a.cache.head_dim == 128)

@@ -99,7 +99,8 @@ wz_status wz_cache_append(const wz_cache* cache, const wz_ragged* batch, const w
   }
   if (q && (q_heads < 1 || q_heads > 256 * 64)) return WZ_ERR_SHAPE;
   if (append_groups(*cache, *batch, q ? q_heads : 0) > kMostGroups) return WZ_ERR_SHAPE;
-  if (batch->tokens == 0 || batch->max_tokens == 0) return WZ_OK;
+  // (without a new token to store there may still be queries to rotate)
+  if (batch->tokens == 0 || (batch->max_tokens == 0 && !q)) return WZ_OK;
   WZ_TRY(check_arrays(*cache, *batch));
   if (rotation) {
     WZ_TRY(check_ptr(rotation->table, 16));
