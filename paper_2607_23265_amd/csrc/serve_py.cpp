@@ -224,7 +224,9 @@ PyObject* append(PyObject*, PyObject* const* a, Py_ssize_t n) {
       turn = unpack<wz_rotation>(a[4]);
       if (a[5] == Py_None) refuse("a rotation needs positions");
       const at::Tensor& at_ = dense("positions", a[5], at::kInt, device);
-      if (at_.numel() != turn.x.axes * tokens || turn.device != device)
+      // (the count alone would take [tokens, axes] and turn by other tokens' positions)
+      const int64_t axes = turn.x.axes;
+      if (at_.numel() != axes * tokens || !(axes == 1 || at_.dim() == 1 || at_.size(0) == axes) || turn.device != device)
         refuse("positions must be [axes, tokens], on the device of the table");
       turn.x.positions = static_cast<const int32_t*>(at_.data_ptr());
     }

@@ -1,0 +1,40 @@
+"""Arguments of the serving operators' binding that have the right size but not the right meaning.  Marked gpu."""
+import pytest
+import torch
+
+import libutil
+from paper_2607_23265_amd import serve
+from serve_util import DEV, Case
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _lib():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    libutil.ensure_built()
+
+
+def _new(*shape):
+    return torch.randn(*shape, device=DEV).to(torch.bfloat16)
+
+
+def test_positions_go_by_axis():
+    """[tokens, axes] has as many positions as [axes, tokens], of other tokens."""
+    c = Case([4], [20], 2, 64, 16, seed=1).fill()
+    cache, batch = c.device_cache(), c.batch()
+    k, v = _new(4, 2, 64), _new(4, 2, 64)
+    at = torch.arange(12, dtype=torch.int32, device=DEV).view(3, 4)
+    table = torch.zeros(40, 64, device=DEV)
+    three, one = serve.Rotation(table, (16, 8, 8)), serve.Rotation(table)
+    for good in (at, at.flatten(), at[:, None]):  # axis by axis, however it is shaped
+        serve.cache_append(cache, batch, k, v, three, good)
+    for bad in (at.t().contiguous(), at.view(2, 6), at.view(4, 3), at[:2], at[:, :3].contiguous()):
+        with pytest.raises(ValueError):
+            serve.cache_append(cache, batch, k, v, three, bad)
+    for good in (at[:1], at[0], at[0].view(4, 1)):
+        serve.cache_append(cache, batch, k, v, one, good)
+    with pytest.raises(ValueError):
+        serve.cache_append(cache, batch, k, v, one, at)
+    torch.cuda.synchronize()
