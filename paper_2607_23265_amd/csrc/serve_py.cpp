@@ -91,22 +91,40 @@ at::Tensor empty_on(const at::Tensor& like, at::IntArrayRef shape, at::ScalarTyp
   return at::empty(shape, like.options().dtype(type).requires_grad(false));
 }
 
-// A struct with its device, as bytes.
+// A struct with its kind (several have the same size) and its device, as bytes.
+template <typename T>
+struct Kind;
+template <>
+struct Kind<wz_cache> {
+  static constexpr const char* name = "PagedCache";
+  static constexpr int32_t mark = 0x635a5701;
+};
+template <>
+struct Kind<wz_ragged> {
+  static constexpr const char* name = "Ragged";
+  static constexpr int32_t mark = 0x725a5702;
+};
+template <>
+struct Kind<wz_rotation> {
+  static constexpr const char* name = "Rotation";
+  static constexpr int32_t mark = 0x745a5703;
+};
 template <typename T>
 struct On {
   T x;
-  int32_t device;
+  int32_t mark, device;
 };
 template <typename T>
 PyObject* pack(const T& x, int device) {
-  const On<T> y{x, device};
+  const On<T> y{x, Kind<T>::mark, device};
   return PyBytes_FromStringAndSize(reinterpret_cast<const char*>(&y), sizeof y);
 }
 template <typename T>
 On<T> unpack(PyObject* x) {
   On<T> y;
-  if (!PyBytes_Check(x) || PyBytes_GET_SIZE(x) != Py_ssize_t(sizeof y)) refuse("not a struct of this module");
-  std::memcpy(&y, PyBytes_AS_STRING(x), sizeof y);
+  const bool fits = PyBytes_Check(x) && PyBytes_GET_SIZE(x) == Py_ssize_t(sizeof y);
+  if (fits) std::memcpy(&y, PyBytes_AS_STRING(x), sizeof y);
+  if (!fits || y.mark != Kind<T>::mark) refuse(std::string("a ") + Kind<T>::name + " is expected");
   return y;
 }
 

@@ -38,3 +38,31 @@ def test_positions_go_by_axis():
     with pytest.raises(ValueError):
         serve.cache_append(cache, batch, k, v, one, at)
     torch.cuda.synchronize()
+
+
+def test_arguments_in_the_wrong_order():
+    """A cache, a batch and a rotation are refused in each other's place; what is packed of them is the header's structs."""
+    c = Case([3], [20], 2, 64, 16, seed=2).fill()
+    cache, batch = c.device_cache(), c.batch()
+    turn = serve.Rotation(torch.zeros(40, 64, device=DEV), (16, 8, 8), True)
+    k, q, at = _new(3, 2, 64), _new(3, 4, 64), torch.zeros(3, 3, dtype=torch.int32, device=DEV)
+    for a, b in ((batch, cache), (cache, cache), (batch, batch), (turn, batch), (cache, turn)):
+        with pytest.raises(ValueError):
+            serve.cache_append(a, b, k, k)
+        with pytest.raises(ValueError):
+            serve.cache_attention(a, b, q)
+        with pytest.raises(ValueError):
+            serve.attention_workspace_bytes(a, b, 4, 3)
+    for bad in (cache, batch):
+        with pytest.raises(ValueError):
+            serve.cache_append(cache, batch, k, k, bad, at)
+    mirrors = (
+        (cache, serve._Cache(*(t.data_ptr() for t in (cache.k, cache.v, cache.k_scale, cache.v_scale)), *cache.k.shape)),
+        (batch, serve._Ragged(batch.start.data_ptr(), batch.kv_len.data_ptr(), batch.table.data_ptr(), 1, 0, 3, 20,
+                              batch.table.shape[1])),
+        (turn, serve._Rotation(turn.table.data_ptr(), None, 40, 64, 3, 1, (16, 8, 8))))
+    for x, m in mirrors:
+        used = type(m)
+        last = used._fields_[-1][0]  # (what follows it is padding)
+        size = getattr(used, last).offset + getattr(used, last).size
+        assert x.c[:size] == bytes(m)[:size], used

@@ -21,3 +21,11 @@ def test_queries_without_a_token_to_store(L):
     assert append(L, r=none, q=None) == OK
     assert append(L, r=none, out=None) == NULL and append(L, r=none, out=2 * AT + 8) == ALIGN
     assert append(L, r=none, t=turn(positions=None)) == NULL
+
+
+def test_structs_are_told_apart_by_more_than_their_size(L):
+    """Bytes of a cache's and a batch's size that are neither."""
+    from paper_2607_23265_amd import _serve
+    for size in (48, 52, 56, 60, 64):
+        with pytest.raises(ValueError, match="expected"):
+            _serve.workspace(bytes(size), bytes(size), 4, 1, 0)
