@@ -6,6 +6,7 @@ of their device.  Where a tensor has rows of heads ([tokens, heads, head_dim]) i
 fused projection are passed as they are; everything else is contiguous.
 """
 import ctypes
+import operator
 import struct
 
 import torch
@@ -87,19 +88,29 @@ class _NotLoaded:
 _native = _NotLoaded()
 
 
+def _fixed(*slots):
+    """Properties that read the slots and cannot be assigned: the packed struct beside them holds their addresses and
+    values, and an assignment would leave it with the old ones."""
+    return [property(operator.attrgetter(s)) for s in slots]
+
+
 class PagedCache:
     """The cache of one layer: k [pages, kv_heads, page_size, head_dim] and v [pages, kv_heads, head_dim, page_size]
-    (float8_e4m3fn), k_scale and v_scale [pages, kv_heads] (float32 powers of two)."""
-    __slots__ = ("k", "v", "k_scale", "v_scale", "c")
+    (float8_e4m3fn), k_scale and v_scale [pages, kv_heads] (float32 powers of two).  The fields cannot be assigned."""
+    __slots__ = ("_k", "_v", "_k_scale", "_v_scale", "_c")
+    k, v, k_scale, v_scale, c = _fixed(*__slots__)
 
     def __init__(self, k, v, k_scale, v_scale):
-        self.c = _native.cache(k, v, k_scale, v_scale)
-        self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
+        self._c = _native.cache(k, v, k_scale, v_scale)
+        self._k, self._v, self._k_scale, self._v_scale = k, v, k_scale, v_scale
 
-    device = property(lambda self: self.k.device)
-    kv_heads = property(lambda self: self.k.shape[1])
-    page_size = property(lambda self: self.k.shape[2])
-    head_dim = property(lambda self: self.k.shape[3])
+    def __reduce__(self):  # (a copy packs its own tensors)
+        return type(self), (self._k, self._v, self._k_scale, self._v_scale)
+
+    device = property(lambda self: self._k.device)
+    kv_heads = property(lambda self: self._k.shape[1])
+    page_size = property(lambda self: self._k.shape[2])
+    head_dim = property(lambda self: self._k.shape[3])
 
     @classmethod
     def new(cls, pages, kv_heads, head_dim, page_size=64, device="cuda:0"):
@@ -113,44 +124,53 @@ class PagedCache:
 class Ragged:
     """A ragged batch: sequence b brings rows start[b] .. start[b + 1] - 1 of the call and has kv_len[b] tokens in the
     cache, these counted, in the pages table[b] (all int32).  max_tokens and max_kv bound the new tokens and the
-    tokens of one sequence."""
-    __slots__ = ("start", "kv_len", "table", "max_tokens", "max_kv", "c")
+    tokens of one sequence.  The fields cannot be assigned; the tensors' contents may change between calls, within the
+    bounds."""
+    __slots__ = ("_start", "_kv_len", "_table", "_max_tokens", "_max_kv", "_c")
+    start, kv_len, table, max_tokens, max_kv, c = _fixed(*__slots__)
 
     def __init__(self, start, kv_len, table, max_tokens, max_kv):
-        self.c = _native.ragged(start, kv_len, table, max_tokens, max_kv)
-        self.start, self.kv_len, self.table = start, kv_len, table
-        self.max_tokens, self.max_kv = max_tokens, max_kv
+        self._c = _native.ragged(start, kv_len, table, max_tokens, max_kv)
+        self._start, self._kv_len, self._table = start, kv_len, table
+        self._max_tokens, self._max_kv = max_tokens, max_kv
 
-    device = property(lambda self: self.start.device)
+    def __reduce__(self):
+        return type(self), (self._start, self._kv_len, self._table, self._max_tokens, self._max_kv)
+
+    device = property(lambda self: self._start.device)
 
 
 class Rotation:
     """Rotation by position: table [max_pos, rot_dim] float32 holds cosines, then sines; sections are the numbers of
-    frequencies that go by each row of positions (one section: all by positions[0])."""
-    __slots__ = ("table", "sections", "interleaved", "c")
+    frequencies that go by each row of positions (one section: all by positions[0]).  The fields cannot be assigned."""
+    __slots__ = ("_table", "_sections", "_interleaved", "_c")
+    table, sections, interleaved, c = _fixed(*__slots__)
 
     def __init__(self, table, sections=(), interleaved=False):
-        self.table, self.sections, self.interleaved = table, tuple(sections), bool(interleaved)
-        self.c = _native.rotation(table, self.sections, self.interleaved)
+        self._table, self._sections, self._interleaved = table, tuple(sections), bool(interleaved)
+        self._c = _native.rotation(table, self._sections, self._interleaved)
+
+    def __reduce__(self):
+        return type(self), (self._table, self._sections, self._interleaved)
 
 
 def cache_append(cache, batch, k, v, rotation=None, positions=None, q=None, q_out=None):
     """wz_cache_append: store the batch's new keys and values (k, v [tokens, kv_heads, head_dim] float32 or bfloat16),
     rotated by positions [axes, tokens] int32; returns the rotated queries [tokens, q_heads, head_dim] bfloat16 if q
     is given (into q_out if that is)."""
-    return _native.append(cache.c, batch.c, k, v, None if rotation is None else rotation.c, positions, q, q_out)
+    return _native.append(cache._c, batch._c, k, v, None if rotation is None else rotation._c, positions, q, q_out)
 
 
 def attention_workspace_bytes(cache, batch, q_heads, tokens, window=0):
     """Bytes of workspace cache_attention() needs for `tokens` rows of q_heads heads (and that window)."""
-    return _native.workspace(cache.c, batch.c, q_heads, tokens, window)
+    return _native.workspace(cache._c, batch._c, q_heads, tokens, window)
 
 
 def cache_attention(cache, batch, q, scale=None, causal=True, window=0, out=None, lse=None, ws=None):
     """wz_cache_attention: q [tokens, q_heads, head_dim] bfloat16 over the cache -> out of the same shape.  scale
     defaults to head_dim ** -0.5; lse [tokens, q_heads] float32 receives the rows' log-sum-exp; ws is a uint8 workspace
     (allocated if not given and needed)."""
-    return _native.attention(cache.c, batch.c, q, scale, causal, window, out, lse, ws)
+    return _native.attention(cache._c, batch._c, q, scale, causal, window, out, lse, ws)
 
 
 def quantize_rows(x, out=None, scale=None):

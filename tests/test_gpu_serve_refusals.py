@@ -1,4 +1,6 @@
 """Arguments of the serving operators' binding that have the right size but not the right meaning.  Marked gpu."""
+import copy
+
 import pytest
 import torch
 
@@ -66,3 +68,24 @@ def test_arguments_in_the_wrong_order():
         last = used._fields_[-1][0]  # (what follows it is padding)
         size = getattr(used, last).offset + getattr(used, last).size
         assert x.c[:size] == bytes(m)[:size], used
+
+
+def test_fields_stay_and_copies_have_their_own():
+    c = Case([1], [20], 2, 64, 16, seed=3).fill()
+    cache, batch, q = c.device_cache(), c.batch(), _new(1, 4, 64)
+    want = serve.cache_attention(cache, batch, q)
+    with pytest.raises(AttributeError):
+        batch.kv_len = batch.kv_len - 5
+    with pytest.raises(AttributeError):
+        batch.max_kv = 5
+    assert torch.equal(serve.cache_attention(cache, batch, q), want)
+    batch.kv_len.sub_(5)  # contents may change
+    shorter = serve.cache_attention(cache, batch, q)
+    assert not torch.equal(shorter, want)
+    batch.kv_len.add_(5)
+    twin, alike = copy.deepcopy((cache, batch))
+    cache.k.view(torch.uint8).zero_(), batch.kv_len.zero_()
+    assert torch.equal(serve.cache_attention(twin, alike, q), want)
+    assert twin.k.data_ptr() != cache.k.data_ptr() and (alike.max_tokens, alike.max_kv) == (1, 20)
+    turn = copy.deepcopy(serve.Rotation(torch.zeros(40, 64, device=DEV), (16, 8, 8), True))
+    assert (turn.sections, turn.interleaved) == ((16, 8, 8), True) and turn.c[:8] == turn.table.data_ptr().to_bytes(8, "little")

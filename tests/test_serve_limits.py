@@ -29,3 +29,14 @@ def test_structs_are_told_apart_by_more_than_their_size(L):
     for size in (48, 52, 56, 60, 64):
         with pytest.raises(ValueError, match="expected"):
             _serve.workspace(bytes(size), bytes(size), 4, 1, 0)
+
+
+@pytest.mark.parametrize("kind,fields", [(serve.PagedCache, ("k", "v", "k_scale", "v_scale", "c")),
+                                         (serve.Ragged, ("start", "kv_len", "table", "max_tokens", "max_kv", "c")),
+                                         (serve.Rotation, ("table", "sections", "interleaved", "c"))])
+def test_fields_cannot_be_assigned(kind, fields):
+    """An assigned field would leave the packed struct with the old address or value."""
+    x = kind.__new__(kind)
+    for name in (*fields, "max_pages"):
+        with pytest.raises(AttributeError):
+            setattr(x, name, 1)
