@@ -27,7 +27,12 @@ namespace {
 
 // `count` tiles from spot x on, key/value head h; slot: where their part goes, -1
 // if the block is this workgroup's alone.
-template <int D, int NT, int kWaves>
+//
+// Four waves take a block's tiles: with eight, next tokens of 1 to 64 sequences and
+// four heads, 128 to 1536 tokens, one workgroup to a block, took 6.7 to 23.3 us
+// where four took 6.1 to 21.7 (heads of 64 elements: 5.5 to 13.6 and 5.2 to 12.8).
+constexpr int kWaves = 4;
+template <int D, int NT>
 __device__ __forceinline__ void attend_block(const AttendArgs& a, const Partition<16 * NT>& part, int h, const Spot& x,
                                              int count, int slot, float* so, float (*sm)[16 * NT],
                                              float (*sl)[16 * NT]) {
@@ -255,7 +260,7 @@ __device__ __forceinline__ void attend_block(const AttendArgs& a, const Partitio
   }
 }
 
-template <int D, int NT, int kWaves>
+template <int D, int NT>
 __global__ __launch_bounds__(kWaves* kWave, NT == 1 ? 2 : 1) void k_attend_token(AttendArgs a) {
   constexpr int BR = 16 * NT;
   __shared__ __align__(16) float so[kWaves * BR * (D + 4)];
@@ -263,7 +268,7 @@ __global__ __launch_bounds__(kWaves* kWave, NT == 1 ? 2 : 1) void k_attend_token
   const int Hkv = a.cache.kv_heads, h = blockIdx.x % Hkv, me = blockIdx.x / Hkv;
   const Partition<BR> part(a);
   part.each_piece(me, [&](const Spot& x, int count, int slot) {
-    attend_block<D, NT, kWaves>(a, part, h, x, count, slot, so, sm, sl);
+    attend_block<D, NT>(a, part, h, x, count, slot, so, sm, sl);
   });
 }
 
@@ -360,15 +365,14 @@ hipError_t join(const AttendArgs& a, const AttendPlan& p, hipStream_t s) {
 
 template <int D>
 void launch_token(const AttendArgs& a, const AttendPlan& p, int64_t groups, hipStream_t s) {
-  const dim3 grid{uint32_t(groups)}, four{4 * kWave}, eight{8 * kWave};
+  const dim3 grid{uint32_t(groups)}, block{kWaves * kWave};
   if constexpr (D == 64)
     if (p.block_rows == 64) {
-      hipLaunchKernelGGL((k_attend_token<D, 4, 4>), grid, four, 0, s, a);
+      hipLaunchKernelGGL((k_attend_token<D, 4>), grid, block, 0, s, a);
       return;
     }
-  if (p.block_rows == 32) hipLaunchKernelGGL((k_attend_token<D, 2, 4>), grid, four, 0, s, a);
-  else if (!p.shared && groups <= kCUs) hipLaunchKernelGGL((k_attend_token<D, 1, 8>), grid, eight, 0, s, a);
-  else hipLaunchKernelGGL((k_attend_token<D, 1, 4>), grid, four, 0, s, a);
+  if (p.block_rows == 32) hipLaunchKernelGGL((k_attend_token<D, 2>), grid, block, 0, s, a);
+  else hipLaunchKernelGGL((k_attend_token<D, 1>), grid, block, 0, s, a);
 }
 
 }  // namespace
@@ -400,16 +404,18 @@ AttendPlan attend_plan(const wz_cache& c, const wz_ragged& r, int q_heads, int w
   const bool wide = p.block_rows == 64 || (p.block_rows == 32 && c.head_dim == 128);
   const int at_once = wide || (p.block_rows == 128 && p.groups == 2) ? kCUs : 2 * kCUs;
   p.workers = int(std::max(1, at_once / c.kv_heads));
-  // Few rows in few blocks: sharing costs a second launch, which is worth two of
-  // the rounds that the waves of the block's only workgroup (eight) or of a
-  // shared run (four) make over its tiles (single tokens of one sequence and four
-  // heads, 1286 tokens: 14.6 us alone, three rounds, and 11.9 shared, one; 800
-  // tokens: 12.0 and 11.5).
+  // Few rows in few blocks: sharing costs a second launch, which is worth four of
+  // the rounds that four waves make over a block's tiles where it has 16 rows (as
+  // the rule counts them, two of eight tiles), and two where it has more.  Not
+  // shared and shared, one to four sequences of four heads of 128:
+  //   7 rows    1024 tokens 11.2 and 12.2 us, 1280 12.5 and 12.3, 1536 13.9 and 12.7
+  //   25 rows   512 tokens 12.5 and 15.7, 768 14.6 and 15.9, 1024 16.4 and 15.9
+  // (heads of 64 cross later: 7.8 and 10.6 at 1024 tokens, 10.7 and 10.8 at 2048.)
   bool long_enough = tiles > 24;
   if (p.block_rows <= 64 && lone_pieces(p.blocks, p.workers)) {
     const int64_t run = lone_run(p.blocks * tiles, p.blocks, p.workers);
-    const int waves = p.block_rows == 16 ? 8 : 4;
-    long_enough = (tiles + waves - 1) / waves >= (run + 3) / 4 + 2;
+    const int round = p.block_rows == 16 ? 8 : 4;
+    long_enough = (tiles + round - 1) / round >= (run + 3) / 4 + 2;
   }
   // (every sequence at its bounds, so that no array's contents make the tiles pass 32 bits)
   const int64_t most = int64_t(r.batch) * ((rows + p.block_rows - 1) / p.block_rows) * (tiles + 1 + kStartTiles);
