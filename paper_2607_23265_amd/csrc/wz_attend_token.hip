@@ -411,7 +411,13 @@ AttendPlan attend_plan(const wz_cache& c, const wz_ragged& r, int q_heads, int w
   //   7 rows    1024 tokens 11.2 and 12.2 us, 1280 12.5 and 12.3, 1536 13.9 and 12.7
   //   25 rows   512 tokens 12.5 and 15.7, 768 14.6 and 15.9, 1024 16.4 and 15.9
   // (heads of 64 cross later: 7.8 and 10.6 at 1024 tokens, 10.7 and 10.8 at 2048.)
-  bool long_enough = tiles > 24;
+  // Prompts: a block alone takes as many turns as it has tiles, a shared run its
+  // share of all tiles, and the parts, their join and what begins a piece come to
+  // 24 turns (28 heads of 128 over 4, not shared and shared: 100 rows over 1500
+  // tokens 32 and 36 us, over 2000 40 and 37, over 5000 78 and 42; a prompt of 1600
+  // 41 and 89, of 2200 56 and 113; 1000 rows over 4000 tokens 81 and 100; 300 over
+  // 6000 94 and 56; 400 over 16000 226 and 119).
+  bool long_enough = tiles > 24 + (p.block_rows > 64 ? p.blocks * tiles / p.workers : 0);
   if (p.block_rows <= 64 && lone_pieces(p.blocks, p.workers)) {
     const int64_t run = lone_run(p.blocks * tiles, p.blocks, p.workers);
     const int round = p.block_rows == 16 ? 8 : 4;

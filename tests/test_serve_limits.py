@@ -2,11 +2,13 @@
 
 Every call here fails validation or has nothing to do, which returns before any HIP call is made.
 """
+import ctypes
+
 import pytest
 
 import libutil
 from paper_2607_23265_amd import serve
-from test_serve_capi import ALIGN, AT, NULL, OK, append, ragged, turn
+from test_serve_capi import ALIGN, AT, NULL, OK, append, cache, ragged, turn
 
 
 @pytest.fixture(scope="module")
@@ -40,3 +42,14 @@ def test_fields_cannot_be_assigned(kind, fields):
     for name in (*fields, "max_pages"):
         with pytest.raises(AttributeError):
             setattr(x, name, 1)
+
+
+@pytest.mark.parametrize("n,kv,shared", [
+    (1286, 1323, False), (1600, 1600, False), (2200, 2200, False), (1000, 5000, False), (100, 1600, False),
+    (100, 3100, True), (300, 6300, True), (400, 16400, True)])
+def test_prompts_are_shared_where_that_is_faster(L, n, kv, shared):
+    """28 query heads of 128 over 4: the measured side of each (a workspace is needed where blocks are shared)."""
+    r = ragged(batch=1, tokens=n, max_tokens=n, max_kv=kv, table_stride=kv)
+    f = serve._Attention(28, 1, 0, 0.1)
+    need = L.wz_attention_workspace_bytes(ctypes.byref(cache()), ctypes.byref(r), ctypes.byref(f))
+    assert (need > 0) == shared
