@@ -18,7 +18,8 @@
 // sixteen lanes that read sixteen rows hit all 64 banks.
 //
 // Measured: 1.19 TFLOP of two causal prompts of 8 300 to 9 459 tokens, 28 heads of
-// 128 over 4, in 1129 us (1.05 PFLOP/s; the library's 8192^3 bf16 product 1.53).
+// 128 over 4, in 1129 to 1161 us on different cards (1.05 to 1.03 PFLOP/s; the
+// library's 8192^3 bf16 product 1.53).
 // A wave of 32 rows fills the registers of two waves a SIMD (output 64, scores
 // 32, queries 32, fragments 64), and those two must overlap vector work, 60 % of
 // the cycles, with products, 50 %; LDS is at 38 %, without conflicts.  128 rows
@@ -263,7 +264,10 @@ __device__ __forceinline__ void attend_block(const AttendArgs& a, const Partitio
     }
     const float use = m == -INFINITY ? 0.f : m;
     // Products with the values, 16 tokens at a time, the probabilities of the
-    // next 16 between them.
+    // next 16 between them.  Each is rounded to bf16 once, for products at bf16's
+    // rate with values that it holds exactly; the sum takes it unrounded (error
+    // against 64 bits, of results in bf16: 0.0017 to 0.0018, with fp32
+    // probabilities 0.0017).
     bf16x8 p[2], v[2][DT];
     auto read_values = [&](int u) {
 #pragma unroll

@@ -19,7 +19,7 @@
 //
 // Measured: next tokens of four sequences of 60 000 to 131 000 tokens, 28 heads of
 // 128 over 4, 349 MB in 64.6 us and 5 us for the join (a 1 GiB copy's 5.2 TB/s
-// would take 66.8); of 64 sequences of 500 to 8 200, 212 MB in 47 and 5.
+// would take 66.8); of 64 sequences of 500 to 8 200, 212 MB in 46 and 5.
 #include "wz_attend.h"
 
 namespace wz {
@@ -174,7 +174,9 @@ __device__ __forceinline__ void attend_block(const AttendArgs& a, const Partitio
       }
       m[n] = mx;
       // each probability is rounded to bf16 once, for the product with values
-      // that bf16 holds exactly; the sum takes it unrounded
+      // that bf16 holds exactly, on the matrix cores' rate for bf16; the sum takes
+      // it unrounded, so a row's weights add up to one within 2^-9 (error against
+      // 64 bits, of results in bf16: 0.0016 to 0.0017, with fp32 probabilities 0.0016)
 #pragma unroll
       for (int t = 0; t < 4; ++t)
 #pragma unroll
@@ -353,7 +355,10 @@ __global__ __launch_bounds__(256) void k_attend_join(AttendArgs a) {
 
 template <int D, int BR>
 hipError_t join(const AttendArgs& a, const AttendPlan& p, hipStream_t s) {
-  // groups share rows where blocks have eight parts or more on average
+  // groups share rows where blocks have eight parts or more on average (next
+  // tokens of four heads over 30 000 tokens, shared and not: one sequence 19 and 34
+  // us, four 31 and 34, twelve 78 and 78, 24 143 and 141; 36 rows over 8000 33 and
+  // 36, 150 rows 55 and 45)
   constexpr int kGroups = 1024 / D;
   const bool many = p.workers >= 8 * p.blocks;
   const int rows = many ? 1 : kGroups;  // of a workgroup
@@ -395,11 +400,15 @@ AttendPlan attend_plan(const wz_cache& c, const wz_ragged& r, int q_heads, int w
   // A CU runs two workgroups of four waves at once, or one of those whose waves
   // take more than half the registers (with two planned for, 28 rows each of 10
   // sequences of 2000 tokens took 30 us instead of 20), or one prompt workgroup of
-  // eight, which is faster while blocks are about as many as CUs or fewer
-  // (shared, it leaves half as many parts).  Registers would hold four of few
-  // rows: more parts, shorter runs, and 74 us instead of 70 for the next tokens of
-  // four sequences of 60 000 to 131 000 (three: 72; of 64 of 500 to 8 200: 55 with
-  // two, 63, 54).
+  // eight.  Registers would hold four of few rows: more parts, shorter runs, and
+  // 74 us instead of 70 for the next tokens of four sequences of 60 000 to 131 000
+  // (three: 72; of 64 of 500 to 8 200: 55 with two, 63, 54).
+  // Eight waves to a prompt's workgroup: a prompt of 28 heads over 4, with four
+  // waves and with eight, of 100 rows (24 blocks times heads) 11.6 and 13.1 us, 800
+  // (176) 24.4 and 23.0, 1286 (284) 35.2 and 31.4, 1400 (308) 37.4 and 33.1, 2000
+  // (440) 51 and 50, 2600 (572) 70 and 78.  Equal blocks lose as soon as they need
+  // a second round: 128 rows each of 60 sequences, 500 tokens before them, 4 heads
+  // (240) 29.3 and 28.6, of 80 (320) 33.5 and 43.2, of 100 (400) 36.7 and 48.2.
   p.groups = int64_t(p.blocks) * c.kv_heads <= kCUs * 5 / 4 ? 2 : 1;
   const bool wide = p.block_rows == 64 || (p.block_rows == 32 && c.head_dim == 128);
   const int at_once = wide || (p.block_rows == 128 && p.groups == 2) ? kCUs : 2 * kCUs;
@@ -417,12 +426,21 @@ AttendPlan attend_plan(const wz_cache& c, const wz_ragged& r, int q_heads, int w
   // tokens 32 and 36 us, over 2000 40 and 37, over 5000 78 and 42; a prompt of 1600
   // 41 and 89, of 2200 56 and 113; 1000 rows over 4000 tokens 81 and 100; 300 over
   // 6000 94 and 56; 400 over 16000 226 and 119).
+  // Few rows in more blocks: sharing makes up for unequal lengths, which the
+  // bounds do not tell.  64 sequences of four heads, not shared and shared: 1536
+  // tokens each 21.7 and 28.3 us, 4096 each 53 and 63, 64 to 4096 31 and 34; one of
+  // 1280 beside others of 191 14.5 and 17.1, one of 2048 19.2 and 17.9, one of 4096
+  // 29 and 19; 128 sequences of 100 to 8000 102 and 75.
   bool long_enough = tiles > 24 + (p.block_rows > 64 ? p.blocks * tiles / p.workers : 0);
   if (p.block_rows <= 64 && lone_pieces(p.blocks, p.workers)) {
     const int64_t run = lone_run(p.blocks * tiles, p.blocks, p.workers);
     const int round = p.block_rows == 16 ? 8 : 4;
     long_enough = (tiles + round - 1) / round >= (run + 3) / 4 + 2;
   }
+  // Many blocks level out by themselves unless one is far longer than the others
+  // (next tokens of four heads, not shared and shared; 256 sequences: 2000 tokens
+  // each 101 and 112 us, 100 to 8000 126 and 121, one of 60 000 beside others of
+  // 200 324 and 53; 512 sequences: 189 and 219, 198 and 226, 339 and 94).
   // (every sequence at its bounds, so that no array's contents make the tiles pass 32 bits)
   const int64_t most = int64_t(r.batch) * ((rows + p.block_rows - 1) / p.block_rows) * (tiles + 1 + kStartTiles);
   p.shared = long_enough && most < (int64_t(1) << 30) &&

@@ -8,7 +8,7 @@
 // writes codes.  Values are turned to [head_dim][page_size] through LDS.
 // Workgroups behind those rotate the queries.
 //
-// Measured: 52 000 prompt tokens of eight sequences, 28 + 2 * 4 heads of 128, 851 MB
+// Measured: 48 869 prompt tokens of eight sequences, 28 + 2 * 4 heads of 128, 851 MB
 // in 162 us (5.3 TB/s, as a 1 GiB copy); a token each of 64 sequences in 5.0 us,
 // three waits for memory in a row behind the launch.
 #include "wz_serve.h"

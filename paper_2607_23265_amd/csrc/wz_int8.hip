@@ -90,6 +90,10 @@ __global__ __launch_bounds__(256) void k_quantize(const In* x, int64_t x_stride,
 template <typename In>
 hipError_t quantize(const In* x, int64_t x_stride, int rows, int cols, int8_t* q, int64_t q_stride, float* scale,
                     hipStream_t s) {
+  // A wave to a row, or a workgroup: 9459 rows of 512, 1024, 2048 and 2560 columns
+  // of bf16 5.4, 8.6, 13.0 and 16.2 us against 8.9, 10.8, 13.2 and 14.7 (64 rows of
+  // 2048 4.3 and 3.5).  Two chunks a thread hold 4096 columns, eight 16 384: 1286
+  // rows of 3584 columns 5.1 and 5.4 us, 9459 of 8192 45 and 40.
   const dim3 block(256);
   if (cols <= 2048)
     hipLaunchKernelGGL((k_quantize<In, kWave, 4>), dim3((rows + 3) / 4), block, 0, s, x, x_stride, rows, cols, q,

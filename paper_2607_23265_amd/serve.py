@@ -18,7 +18,8 @@ EXPORTS = ("wz_cache_append", "wz_cache_attention", "wz_attention_workspace_byte
 E4M3 = torch.float8_e4m3fn
 _P, _I, _L, _S = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_size_t
 
-# For calls of the library by ctypes (lib()): the header's structs as bytes, and below as ctypes.Structure.
+# For calls of the C entry points by ctypes (lib()): the header's structs as bytes, and below as ctypes.Structure.  The
+# functions at the end of this module go through the native half, which packs structs of its own.
 _CACHE = struct.Struct("@4P4i").pack      # wz_cache
 _RAGGED = struct.Struct("@3P5i4x").pack   # wz_ragged
 _ROTATION = struct.Struct("@2P7i4x").pack  # wz_rotation
