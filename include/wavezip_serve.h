@@ -1,14 +1,21 @@
 /*
  * wavezip_serve.h -- C ABI of the operators that serve condensed tokens on
  * AMD Instinct MI355X (gfx950): one language-model layer's traffic with a
- * paged key/value cache held in 8 bits, and matrix products in 8-bit
- * integers.
+ * paged key/value cache held in 8 bits, or with states of a fixed size, and
+ * matrix products in 8-bit integers.
  *
- *   wz_cache_append     rotates new keys (and queries) by their positions and
- *                       stores keys and values in the cache;
- *   wz_cache_attention  attention of a ragged batch of queries over the cache;
- *   wz_quantize_rows    rows to 8-bit integers with one scale each;
- *   wz_matmul_int       their product with weights held the same way.
+ *   wz_cache_append         rotates new keys (and queries) by their positions
+ *                           and stores keys and values in the cache;
+ *   wz_cache_attention      attention of a ragged batch over the cache;
+ *   wz_decay_attention      linear attention with a decay for each head, over
+ *                           states of a fixed size;
+ *   wz_quantize_rows        rows to 8-bit integers with one scale each;
+ *   wz_norm_quantize        the same of the root-mean-square norm of rows, or
+ *                           of the sum of two;
+ *   wz_matmul_int           their product with weights held the same way;
+ *   wz_matmul_int_epilogue  the same with an activation and a residual;
+ *   wz_gated_int            both projections of a gated feed-forward block,
+ *                           the activation and the product.
  *
  * The conventions of wavezip.h hold here too: device pointers owned by the
  * caller, nothing allocated or kept by the library, all work enqueued on
@@ -189,6 +196,117 @@ wz_status wz_matmul_int(const int8_t* a, int64_t a_stride,
                         const float* bias, int32_t M, int32_t N, int32_t K,
                         void* out, int64_t out_stride, int32_t out_dtype,
                         void* stream);
+
+/* What becomes of a product's elements, in fp32.                             */
+typedef enum {
+  WZ_ACT_NONE = 0,
+  WZ_ACT_RELU = 1,      /* max(x, 0)                                          */
+  WZ_ACT_SILU = 2,      /* x / (1 + exp(-x))                                  */
+  WZ_ACT_GELU = 3,      /* x (1 + erf(x / sqrt 2)) / 2                        */
+  WZ_ACT_GELU_TANH = 4  /* x (1 + tanh(sqrt(2/pi) (x + 0.044715 x^3))) / 2    */
+} wz_activation;
+
+/* The product of wz_matmul_int with an epilogue:
+ *   out[m][n] = residual[m][n] +
+ *               act((sum_k a[m][k] w[n][k]) * a_scale[m] * w_scale[n] + bias[n])
+ * in fp32, rounded to out_dtype once.  residual (optional, may be NULL): rows of
+ * out_dtype, residual_stride elements apart (>= N, any; aligned to its element);
+ * it may be `out` itself, with its stride, and must not overlap it otherwise.
+ * Everything else as in wz_matmul_int, whose results it gives without both.  */
+wz_status wz_matmul_int_epilogue(const int8_t* a, int64_t a_stride,
+                                 const float* a_scale, const int8_t* w,
+                                 int64_t w_stride, const float* w_scale,
+                                 const float* bias, int32_t activation,
+                                 const void* residual, int64_t residual_stride,
+                                 int32_t M, int32_t N, int32_t K, void* out,
+                                 int64_t out_stride, int32_t out_dtype,
+                                 void* stream);
+
+/* A gated feed-forward block's first half:
+ *   out[m][n] = act(g[m][n]) * u[m][n]
+ *   g = (sum_k a[m][k] gate[n][k]) * a_scale[m] * gate_scale[n] + gate_bias[n]
+ *   u = (sum_k a[m][k] up[n][k]) * a_scale[m] * up_scale[n] + up_bias[n]
+ * with both sums exact in 32-bit integers and the rest in fp32, rounded to
+ * out_dtype once; neither g nor u goes to memory.  gate and up: int8 [N][K], rows
+ * gate_stride and up_stride bytes apart (the halves of one tensor, for example);
+ * the biases fp32 [N] or NULL, each by itself; activation: any of wz_activation.
+ * The limits are those of wz_matmul_int with 2 N <= 2^24 - 1.  One kernel launch,
+ * or two.                                                                    */
+wz_status wz_gated_int(const int8_t* a, int64_t a_stride, const float* a_scale,
+                       const int8_t* gate, int64_t gate_stride,
+                       const float* gate_scale, const float* gate_bias,
+                       const int8_t* up, int64_t up_stride,
+                       const float* up_scale, const float* up_bias,
+                       int32_t activation, int32_t M, int32_t N, int32_t K,
+                       void* out, int64_t out_stride, int32_t out_dtype,
+                       void* stream);
+
+/* Rows of a residual stream to 8-bit integers behind their root-mean-square norm:
+ *   h = x + residual        in fp32, rounded to dtype (h = x where residual is NULL)
+ *   y = h * weight / sqrt(mean(h^2) + eps)
+ *   scale[m] = max|y| / 127,  q = y / scale[m] rounded to the nearest integer
+ * The norm's factor is one number a row and cancels in the codes, so they go by
+ * t = h * weight (fp32) alone: q = t * (127 / max(max|t|, 2^-100)), each operation
+ * rounded to fp32, ties to even; scale = (max(max|t|, 2^-100) / 127) / sqrt(...).
+ * The squares are summed in fp32 in an order that the row's length alone decides (and
+ * scaled before where the sum would pass fp32).  A row with a NaN or an infinity in t
+ * gets the scale NaN and zeros.  total (with a residual: required; without one: not
+ * looked at) receives h; it may be x or residual itself, with its stride, and must
+ * not overlap them otherwise.  x, residual, total: [rows][cols] of dtype (fp32 or
+ * bf16), rows a multiple of 8 elements apart; weight: fp32 [cols], 16-byte aligned;
+ * q: int8, rows q_stride bytes apart; eps: positive and finite.  Limits on sizes and
+ * strides as in wz_quantize_rows.  One kernel launch.                        */
+wz_status wz_norm_quantize(const void* x, int64_t x_stride, const void* residual,
+                           int64_t residual_stride, const float* weight,
+                           float eps, int32_t rows, int32_t cols, int32_t dtype,
+                           void* total, int64_t total_stride, int8_t* q,
+                           int64_t q_stride, float* scale, void* stream);
+
+/* The states of one layer with linear attention: a matrix for each sequence and
+ * head, in a slot of its own.  Supported: head_dim 64 or 128; 1 <= heads <= 256;
+ * 1 <= slots (their elements may pass 2^32).  state 16-byte aligned.  Nothing
+ * needs initialising.                                                        */
+typedef struct {
+  float* state;  /* [slots][heads][head_dim of keys][head_dim of values] fp32 */
+  int32_t slots, heads, head_dim;
+} wz_states;
+
+/* Bytes of workspace wz_decay_attention needs (0 if the arguments are invalid or
+ * none is needed), at most 256 MiB: what segments of long sequences add to the
+ * state.  Depends on batch, max_tokens, heads and head_dim alone.            */
+size_t wz_decay_workspace_bytes(const wz_states* states, const wz_ragged* batch);
+
+/* Linear attention with a decay for each head.  For each new token t of a sequence,
+ * in order, and each head h:
+ *   S <- exp(log_decay[h]) * S + k_t v_t^T,   out_t = scale * q_t S
+ * S (fp32) is the sequence's state in slot[b]: where the sequence has tokens before
+ * the call (kv_len[b] > n_b) it goes on from what the slot holds, otherwise from
+ * zeros; behind the last token it is stored there.  A sequence that brings no token
+ * leaves its slot alone.  Where slot[b] is outside [0, slots) the sequence begins
+ * with zeros and its state is not stored.  Distinct sequences that bring tokens need
+ * distinct slots.  The batch's table and table_stride are not looked at; the
+ * other limits and cuts of wz_ragged hold.
+ *
+ * log_decay: fp32 [heads], 0 (nothing is forgotten) or less, to -infinity (only the
+ * token itself is seen); above 0 it counts as 0, and a NaN makes the head's rows and
+ * states NaN.  q and out: bf16 rows of `heads` heads; k and v of kv_heads heads,
+ * which divide heads: head h reads key head h / (heads / kv_heads).  Strides are
+ * multiples of 8 elements, pointers 16-byte aligned; out must not overlap q, k or v.
+ * scale: finite.  Sums and states are fp32; a state's sum takes the products exact
+ * in fp32, the outputs of prompts take the state and the decayed scores with 16
+ * significant bits and more.  A NaN or an infinity in a token's key, value or query
+ * reaches those elements of rows and states that depend on it by the formula (as
+ * one or the other), and no others.  Rows of tokens that no sequence has are not
+ * written.  slot: int32 [batch].  ws: 256-byte aligned, at least
+ * wz_decay_workspace_bytes() bytes; contents on entry are ignored.  One to three
+ * kernel launches.                                                           */
+wz_status wz_decay_attention(const wz_states* states, const wz_ragged* batch,
+                             const int32_t* slot, const float* log_decay,
+                             const void* q, int64_t q_stride, const void* k,
+                             int64_t k_stride, const void* v, int64_t v_stride,
+                             int32_t kv_heads, float scale, void* out,
+                             int64_t out_stride, void* ws, size_t ws_bytes,
+                             void* stream);
 
 #ifdef __cplusplus
 }

@@ -2,6 +2,8 @@
 
 Written from the header's definitions with loops over sequences, pages and heads; it shares no code with the library.
 """
+import math
+
 import numpy as np
 
 
@@ -156,3 +158,60 @@ def matmul_int(a, a_scale, w, w_scale, bias=None):
     acc = a.astype(np.float64) @ w.astype(np.float64).T  # whole numbers below 2^53: exact
     y = acc * a_scale.astype(np.float64)[:, None] * w_scale.astype(np.float64)
     return (y, np.abs(y)) if bias is None else (y + bias.astype(np.float64), np.abs(y) + np.abs(bias))
+
+
+def norm_quantize(h, weight, eps):
+    """h [rows, cols] float32 (the stream as it is stored) -> (int8, scale float64): codes from h * weight, each operation
+    in float32; the norm in float64."""
+    h, weight = np.asarray(h, dtype=np.float32), np.asarray(weight, dtype=np.float32)
+    with np.errstate(all="ignore"):
+        t = h * weight
+    q, scale = quantize_rows(t)
+    top = np.maximum(np.abs(np.nan_to_num(t)).max(1), np.float32(2.0 ** -100)).astype(np.float64)
+    with np.errstate(all="ignore"):
+        norm = np.sqrt(np.square(h.astype(np.float64)).mean(1) + eps)
+        return q, np.where(np.isfinite(scale), top / 127 / norm, np.nan)
+
+
+def activation(x, name):
+    """(activation of x, a bound of its slope) in float64."""
+    x = np.asarray(x, dtype=np.float64)
+    if name in (None, "none"):
+        return x, 1.0
+    if name == "relu":
+        return np.maximum(x, 0), 1.0
+    with np.errstate(over="ignore"):
+        if name == "silu":
+            return x / (1 + np.exp(-x)), 1.1
+        if name == "gelu":
+            return 0.5 * x * np.vectorize(math.erfc)(-x / math.sqrt(2)), 1.13
+        return x / (1 + np.exp(-2 * math.sqrt(2 / math.pi) * (x + 0.044715 * x ** 3))), 1.13  # (1 + tanh(z)) / 2
+
+
+def decay_attention(state, start, held, slot, q, k, v, log_decay, scale):
+    """The recurrence token by token in float64.  state [slots, heads, D, D] (not changed), held[b]: whether the sequence
+    goes on from its slot; q [tokens, heads, D], k and v [tokens, kv_heads, D].  Returns (out, the sum of its terms'
+    magnitudes, states, theirs); rows of no sequence are NaN."""
+    T, H, D = q.shape
+    G = H // k.shape[1]
+    out, mag = np.full((T, H, D), np.nan), np.full((T, H, D), np.nan)
+    state = state.astype(np.float64)
+    size = np.abs(state)
+    with np.errstate(all="ignore"):
+        decay = np.exp(np.minimum(np.asarray(log_decay, dtype=np.float64), 0.0))
+        for b in range(len(slot)):
+            kept = 0 <= slot[b] < state.shape[0]
+            if start[b + 1] <= start[b]:
+                continue
+            for h in range(H):
+                S, M = np.zeros((D, D)), np.zeros((D, D))
+                if kept and held[b]:
+                    S, M = state[slot[b], h].copy(), size[slot[b], h].copy()
+                for t in range(start[b], start[b + 1]):
+                    x = np.outer(k[t, h // G].astype(np.float64), v[t, h // G].astype(np.float64))
+                    S, M = decay[h] * S + x, decay[h] * M + np.abs(x)
+                    y = q[t, h].astype(np.float64)
+                    out[t, h], mag[t, h] = scale * (y @ S), abs(scale) * (np.abs(y) @ M)
+                if kept:
+                    state[slot[b], h], size[slot[b], h] = S, M
+    return out, mag, state, size

@@ -15,6 +15,7 @@
 #include <cstring>
 #include <stdexcept>
 #include <string>
+#include <utility>
 
 #include "wavezip_serve.h"
 
@@ -108,6 +109,11 @@ template <>
 struct Kind<wz_rotation> {
   static constexpr const char* name = "Rotation";
   static constexpr int32_t mark = 0x745a5703;
+};
+template <>
+struct Kind<wz_states> {
+  static constexpr const char* name = "States";
+  static constexpr int32_t mark = 0x735a5704;
 };
 template <typename T>
 struct On {
@@ -209,6 +215,15 @@ PyObject* rotation(PyObject*, PyObject* const* a, Py_ssize_t n) {
       r.sections[i] = int32_t(integer("a section", PyTuple_GET_ITEM(a[1], i)));
     if (sections == 1 && 2 * int64_t(r.sections[0]) != table.size(1)) refuse("the sections must sum to rot_dim / 2");
     return pack(r, table.get_device());
+  });
+}
+
+PyObject* states(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded(n, 1, [&] {
+    const at::Tensor& s = dense("state", a[0], at::kFloat);
+    if (s.dim() != 4 || s.size(2) != s.size(3)) refuse("state must be [slots, heads, head_dim, head_dim]");
+    return pack(wz_states{static_cast<float*>(s.data_ptr()), count("slots", s.size(0)), count("heads", s.size(1)),
+                          count("head_dim", s.size(2))}, s.get_device());
   });
 }
 
@@ -329,42 +344,204 @@ PyObject* quantize_rows(PyObject*, PyObject* const* a, Py_ssize_t n) {
   });
 }
 
-// (a, a_scale, w, w_scale, bias, out, out_dtype) -> out
+// An activation's name, or None.
+int32_t activation(PyObject* x) {
+  static const std::pair<const char*, int32_t> names[] = {{"relu", WZ_ACT_RELU}, {"silu", WZ_ACT_SILU},
+                                                          {"gelu", WZ_ACT_GELU}, {"gelu_tanh", WZ_ACT_GELU_TANH}};
+  if (x == Py_None) return WZ_ACT_NONE;
+  if (PyUnicode_Check(x))
+    for (const auto& [name, value] : names)
+      if (PyUnicode_CompareWithASCIIString(x, name) == 0) return value;
+  refuse("activation must be None, 'relu', 'silu', 'gelu' or 'gelu_tanh'");
+}
+// Weights [N, K] with a scale, and perhaps a bias, for each row.
+struct Weights {
+  const int8_t* w;
+  int64_t stride, rows;
+  const float *scale, *bias;
+};
+Weights weights(const char* name, PyObject* w, PyObject* scale, PyObject* bias, int64_t K, int device) {
+  const at::Tensor& t = tensor(name, w);
+  Weights r{};
+  r.stride = matrix(name, t, false, device), r.rows = t.size(0);
+  if (t.size(1) != K) refuse(std::string("a and ") + name + " must have the same columns");
+  const at::Tensor& s = dense("a scale of weights", scale, at::kFloat, device);
+  bool fits = s.numel() == r.rows;
+  if (bias != Py_None) {
+    const at::Tensor& b = dense("a bias", bias, at::kFloat, device);
+    fits = fits && b.numel() == r.rows, r.bias = static_cast<const float*>(b.data_ptr());
+  }
+  if (!fits) refuse(std::string("the scale and the bias of ") + name + " must be [N]");
+  r.w = static_cast<const int8_t*>(t.data_ptr()), r.scale = static_cast<const float*>(s.data_ptr());
+  return r;
+}
+// The activations of a product, and its result (made where it is not given).
+struct Rows {
+  const int8_t* a;
+  int64_t stride, M, K;
+  int device;
+  const float* scale;
+};
+Rows rows_in(PyObject* a, PyObject* a_scale) {
+  const at::Tensor& x = tensor("a", a);
+  Rows r{};
+  r.stride = matrix("a", x, false), r.M = x.size(0), r.K = x.size(1), r.device = x.get_device();
+  const at::Tensor& s = dense("a_scale", a_scale, at::kFloat, r.device);
+  if (s.numel() != r.M) refuse("a_scale must be [M]");
+  r.a = static_cast<const int8_t*>(x.data_ptr()), r.scale = static_cast<const float*>(s.data_ptr());
+  return r;
+}
+at::Tensor product_out(const Rows& r, PyObject* a, int64_t N, PyObject* out, PyObject* out_dtype) {
+  if (out != Py_None) return tensor("out", out);
+  if (!THPDtype_Check(out_dtype)) refuse("out_dtype must be a dtype");
+  const at::ScalarType type = reinterpret_cast<THPDtype*>(out_dtype)->scalar_type;
+  if (!numbers(type)) refuse("out must be [M, N] float32 or bfloat16");
+  return empty_on(tensor("a", a), {r.M, N}, type);
+}
+
+// (a, a_scale, w, w_scale, bias, out, out_dtype, activation, residual) -> out
 PyObject* matmul_int(PyObject*, PyObject* const* a, Py_ssize_t n) {
-  return guarded(n, 7, [&]() -> PyObject* {
-    const at::Tensor &x = tensor("a", a[0]), &w = tensor("w", a[2]);
-    const int64_t as = matrix("a", x, false);
-    const int device = x.get_device();
-    const int64_t ws = matrix("w", w, false, device);
-    const int64_t M = x.size(0), K = x.size(1), N = w.size(0);
-    if (w.size(1) != K) refuse("a and w must have the same columns");
-    const at::Tensor &a_scale = dense("a_scale", a[1], at::kFloat, device),
-                     &w_scale = dense("w_scale", a[3], at::kFloat, device);
-    const float* bias = nullptr;
-    bool fits = a_scale.numel() == M && w_scale.numel() == N;
-    if (a[4] != Py_None) {
-      const at::Tensor& b = dense("bias", a[4], at::kFloat, device);
-      fits = fits && b.numel() == N, bias = static_cast<const float*>(b.data_ptr());
+  return guarded(n, 9, [&]() -> PyObject* {
+    const Rows r = rows_in(a[0], a[1]);
+    const Weights w = weights("w", a[2], a[3], a[4], r.K, r.device);
+    const int32_t act = activation(a[7]);
+    at::Tensor out = product_out(r, a[0], w.rows, a[5], a[6]);
+    const int64_t os = matrix("out", out, true, r.device);
+    if (!is(out, {r.M, w.rows})) refuse("out must be [M, N] float32 or bfloat16");
+    const void* residual = nullptr;
+    int64_t rs = 0;
+    if (a[8] != Py_None) {
+      const at::Tensor& t = tensor("residual", a[8]);
+      rs = matrix("residual", t, true, r.device), residual = t.data_ptr();
+      if (!is(t, {r.M, w.rows}) || t.scalar_type() != out.scalar_type())
+        refuse("residual must be [M, N] of the type of out");
     }
-    if (!fits) refuse("a_scale must be [M], w_scale and bias [N]");
-    at::Tensor out;
-    if (a[5] == Py_None) {
-      if (!THPDtype_Check(a[6])) refuse("out_dtype must be a dtype");
-      const at::ScalarType type = reinterpret_cast<THPDtype*>(a[6])->scalar_type;
-      if (!numbers(type)) refuse("out must be [M, N] float32 or bfloat16");
-      out = empty_on(x, {M, N}, type);
-    } else {
-      out = tensor("out", a[5]);
-    }
-    const int64_t os = matrix("out", out, true, device);
-    if (!is(out, {M, N})) refuse("out must be [M, N] float32 or bfloat16");
-    call("wz_matmul_int", device, [&](void* s) {
-      return wz_matmul_int(static_cast<const int8_t*>(x.data_ptr()), as, static_cast<const float*>(a_scale.data_ptr()),
-                           static_cast<const int8_t*>(w.data_ptr()), ws, static_cast<const float*>(w_scale.data_ptr()),
-                           bias, count("M", M), count("N", N), count("K", K), out.data_ptr(), os,
-                           code(out.scalar_type()), s);
-    });
+    const int32_t M = count("M", r.M), N = count("N", w.rows), K = count("K", r.K), type = code(out.scalar_type());
+    if (act == WZ_ACT_NONE && a[8] == Py_None)
+      call("wz_matmul_int", r.device, [&](void* s) {
+        return wz_matmul_int(r.a, r.stride, r.scale, w.w, w.stride, w.scale, w.bias, M, N, K, out.data_ptr(), os, type,
+                             s);
+      });
+    else
+      call("wz_matmul_int_epilogue", r.device, [&](void* s) {
+        return wz_matmul_int_epilogue(r.a, r.stride, r.scale, w.w, w.stride, w.scale, w.bias, act, residual, rs, M, N,
+                                      K, out.data_ptr(), os, type, s);
+      });
     return a[5] == Py_None ? THPVariable_Wrap(std::move(out)) : Py_NewRef(a[5]);
+  });
+}
+
+// (a, a_scale, gate, gate_scale, up, up_scale, activation, gate_bias, up_bias, out, out_dtype) -> out
+PyObject* gated_int(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded(n, 11, [&]() -> PyObject* {
+    const Rows r = rows_in(a[0], a[1]);
+    const Weights gate = weights("gate", a[2], a[3], a[7], r.K, r.device), up = weights("up", a[4], a[5], a[8], r.K, r.device);
+    if (gate.rows != up.rows) refuse("gate and up must have the same rows");
+    const int32_t act = activation(a[6]);
+    at::Tensor out = product_out(r, a[0], up.rows, a[9], a[10]);
+    const int64_t os = matrix("out", out, true, r.device);
+    if (!is(out, {r.M, up.rows})) refuse("out must be [M, N] float32 or bfloat16");
+    call("wz_gated_int", r.device, [&](void* s) {
+      return wz_gated_int(r.a, r.stride, r.scale, gate.w, gate.stride, gate.scale, gate.bias, up.w, up.stride,
+                          up.scale, up.bias, act, count("M", r.M), count("N", up.rows), count("K", r.K), out.data_ptr(),
+                          os, code(out.scalar_type()), s);
+    });
+    return a[9] == Py_None ? THPVariable_Wrap(std::move(out)) : Py_NewRef(a[9]);
+  });
+}
+
+// (x, weight, eps, residual, total, out, scale) -> (out, scale) or (out, scale, total)
+PyObject* norm_quantize(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded(n, 7, [&]() -> PyObject* {
+    const at::Tensor& x = tensor("x", a[0]);
+    const int64_t xs = matrix("x", x, true), rows = x.size(0), cols = x.size(1);
+    const int device = x.get_device();
+    const at::Tensor& weight = dense("weight", a[1], at::kFloat, device);
+    if (weight.numel() != cols) refuse("weight must be [cols]");
+    const double eps = PyFloat_AsDouble(a[2]);
+    if (eps == -1.0 && PyErr_Occurred()) throw Raised{};
+    const bool sum = a[3] != Py_None;
+    const void* residual = nullptr;
+    int64_t rs = 0, ts = 0;
+    at::Tensor total;
+    auto stream = [&](const char* name, const at::Tensor& t) {
+      const int64_t stride = matrix(name, t, true, device);
+      if (!is(t, {rows, cols}) || t.scalar_type() != x.scalar_type())
+        refuse(std::string(name) + " must have the shape and the type of x");
+      return stride;
+    };
+    if (sum) {
+      const at::Tensor& t = tensor("residual", a[3]);
+      rs = stream("residual", t), residual = t.data_ptr();
+      total = a[4] == Py_None ? empty_on(x, {rows, cols}, x.scalar_type()) : tensor("total", a[4]);
+      ts = stream("total", total);
+    } else if (a[4] != Py_None) {
+      refuse("a total needs a residual");
+    }
+    const at::Tensor out = a[5] == Py_None ? empty_on(x, {rows, cols}, at::kChar) : tensor("out", a[5]);
+    const at::Tensor scale =
+        a[6] == Py_None ? empty_on(x, {rows}, at::kFloat) : dense("scale", a[6], at::kFloat, device);
+    const int64_t qs = matrix("out", out, false, device);
+    if (!is(out, {rows, cols}) || !is(scale, {rows})) refuse("out must have the shape of x, and scale [rows]");
+    call("wz_norm_quantize", device, [&](void* s) {
+      return wz_norm_quantize(x.data_ptr(), xs, residual, rs, static_cast<const float*>(weight.data_ptr()), float(eps),
+                              count("rows", rows), count("cols", cols), code(x.scalar_type()),
+                              sum ? total.data_ptr() : nullptr, ts, static_cast<int8_t*>(out.data_ptr()), qs,
+                              static_cast<float*>(scale.data_ptr()), s);
+    });
+    PyObject* const all = PyTuple_New(sum ? 3 : 2);
+    if (!all) throw Raised{};
+    PyTuple_SET_ITEM(all, 0, a[5] == Py_None ? THPVariable_Wrap(out) : Py_NewRef(a[5]));
+    PyTuple_SET_ITEM(all, 1, a[6] == Py_None ? THPVariable_Wrap(scale) : Py_NewRef(a[6]));
+    if (sum) PyTuple_SET_ITEM(all, 2, a[4] == Py_None ? THPVariable_Wrap(total) : Py_NewRef(a[4]));
+    return all;
+  });
+}
+
+// (states, batch) -> bytes of workspace
+PyObject* decay_workspace(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded(n, 2, [&] {
+    const auto z = unpack<wz_states>(a[0]);
+    const auto r = unpack<wz_ragged>(a[1]);
+    return PyLong_FromSize_t(wz_decay_workspace_bytes(&z.x, &r.x));
+  });
+}
+
+// (states, batch, slot, q, k, v, log_decay, scale, out, ws) -> out
+PyObject* decay_attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded(n, 10, [&]() -> PyObject* {
+    const auto z = unpack<wz_states>(a[0]);
+    auto r = unpack<wz_ragged>(a[1]);
+    const int device = z.device;
+    if (r.device != device) refuse("the batch must be on the states' device");
+    const at::Tensor& slot = dense("slot", a[2], at::kInt, device);
+    if (!is(slot, {r.x.batch})) refuse("slot must be [batch]");
+    const int64_t dim = z.x.head_dim, heads = z.x.heads;
+    const at::Tensor &q = tensor("q", a[3]), &k = tensor("k", a[4]), &v = tensor("v", a[5]);
+    const int64_t qs = rows_of("q", q, -1, heads, dim, device, at::kBFloat16), tokens = q.size(0);
+    const int64_t ks = rows_of("k", k, tokens, -1, dim, device, at::kBFloat16);
+    const int64_t vs = rows_of("v", v, tokens, k.size(1), dim, device, at::kBFloat16);
+    r.x.tokens = count("tokens", tokens);
+    const at::Tensor& decay = dense("log_decay", a[6], at::kFloat, device);
+    if (!is(decay, {heads})) refuse("log_decay must be [heads]");
+    const double scale = a[7] == Py_None ? 1 / std::sqrt(double(dim)) : PyFloat_AsDouble(a[7]);
+    if (scale == -1.0 && PyErr_Occurred()) throw Raised{};
+    const at::Tensor out = a[8] == Py_None ? empty_on(q, {tokens, heads, dim}, at::kBFloat16) : tensor("out", a[8]);
+    const int64_t os = rows_of("out", out, tokens, heads, dim, device, at::kBFloat16);
+    at::Tensor ws;
+    if (a[9] == Py_None) {
+      const size_t need = wz_decay_workspace_bytes(&z.x, &r.x);
+      if (need) ws = empty_on(q, {int64_t(need)}, at::kByte);
+    } else {
+      ws = dense("ws", a[9], at::kByte, device);
+    }
+    call("wz_decay_attention", device, [&](void* s) {
+      return wz_decay_attention(&z.x, &r.x, static_cast<const int32_t*>(slot.data_ptr()),
+                                static_cast<const float*>(decay.data_ptr()), q.data_ptr(), qs, k.data_ptr(), ks,
+                                v.data_ptr(), vs, count("kv_heads", k.size(1)), float(scale), out.data_ptr(), os,
+                                ws.defined() ? ws.data_ptr() : nullptr, ws.defined() ? size_t(ws.numel()) : 0, s);
+    });
+    return a[8] == Py_None ? THPVariable_Wrap(out) : Py_NewRef(a[8]);
   });
 }
 
@@ -375,7 +552,8 @@ PyObject* raise_as(PyObject*, PyObject* error) {
 
 #define FAST(f) {#f, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(f)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {FAST(cache), FAST(ragged), FAST(rotation), FAST(append), FAST(workspace), FAST(attention),
-                         FAST(quantize_rows), FAST(matmul_int), {"raise_as", raise_as, METH_O, nullptr}, {}};
+                         FAST(quantize_rows), FAST(matmul_int), FAST(gated_int), FAST(norm_quantize), FAST(states), FAST(decay_workspace),
+                         FAST(decay_attention), {"raise_as", raise_as, METH_O, nullptr}, {}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_serve", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

@@ -122,7 +122,42 @@ struct MatmulArgs {
   void* out;
   int64_t a_stride, w_stride, out_stride;
   int M, N, K;
+  // the epilogue's: an activation and a residual
+  int activation;
+  const void* residual;
+  int64_t residual_stride;
+  // the gated block's: the projection that is not activated (w is the gate)
+  const int8_t* w2;
+  const float *w2_scale, *bias2;
+  int64_t w2_stride;
 };
 hipError_t launch_matmul(const MatmulArgs& p, int out_dtype, hipStream_t s);
+hipError_t launch_matmul_epilogue(const MatmulArgs& p, int out_dtype, hipStream_t s);
+hipError_t launch_gated(const MatmulArgs& p, int out_dtype, hipStream_t s);
+
+struct NormArgs {
+  const void *x, *residual;  // residual NULL: none, and no total
+  const float* weight;
+  void* total;
+  int8_t* q;
+  float* scale;
+  int64_t x_stride, residual_stride, total_stride, q_stride;
+  float eps;
+  int rows, cols;
+};
+hipError_t launch_norm(const NormArgs& p, int dtype, hipStream_t s);
+
+struct DecayArgs {
+  wz_states states;
+  wz_ragged batch;  // (without its table)
+  const int32_t* slot;
+  const float* log_decay;
+  const void *q, *k, *v;
+  void* out;
+  int64_t q_stride, k_stride, v_stride, out_stride;
+  float scale;
+  int group;  // heads that share a key head
+};
+hipError_t launch_decay_token(const DecayArgs& p, hipStream_t s);
 
 }  // namespace wz

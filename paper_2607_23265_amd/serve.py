@@ -1,7 +1,7 @@
 """Python binding of the serving operators (include/wavezip_serve.h): argument marshalling only, in csrc/serve_py.cpp.
 
-A paged key/value cache held in 8 bits, attention over it, and products in 8-bit integers, for a language model that
-reads the tokens wavezip.condense() keeps.  Tensors are torch GPU tensors; every call goes to the current HIP stream
+A paged key/value cache held in 8 bits and attention over it, linear attention over states of a fixed size, norms to 8
+bits and products in 8-bit integers, for a language model that reads the tokens wavezip.condense() keeps.  Tensors are torch GPU tensors; every call goes to the current HIP stream
 of their device.  Where a tensor has rows of heads ([tokens, heads, head_dim]) its rows may lie apart, so parts of one
 fused projection are passed as they are; everything else is contiguous.
 """
@@ -14,9 +14,11 @@ import torch
 from . import wavezip as wz
 
 EXPORTS = ("wz_cache_append", "wz_cache_attention", "wz_attention_workspace_bytes", "wz_quantize_rows",
-           "wz_matmul_int")
+           "wz_matmul_int", "wz_matmul_int_epilogue", "wz_gated_int", "wz_norm_quantize", "wz_decay_attention",
+           "wz_decay_workspace_bytes")
+SIZES = ("wz_attention_workspace_bytes", "wz_decay_workspace_bytes")  # (the others return a wz_status)
 E4M3 = torch.float8_e4m3fn
-_P, _I, _L, _S = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_size_t
+_P, _I, _L, _S, _F = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_size_t, ctypes.c_float
 
 # For calls of the C entry points by ctypes (lib()): the header's structs as bytes, and below as ctypes.Structure.  The
 # functions at the end of this module go through the native half, which packs structs of its own.
@@ -49,6 +51,11 @@ class _Attention(ctypes.Structure):
     _fields_ = [("q_heads", _I), ("causal", _I), ("window", _I), ("scale", ctypes.c_float)]
 
 
+class _States(ctypes.Structure):
+    """Mirror of wz_states."""
+    _fields_ = [("state", _P), ("slots", _I), ("heads", _I), ("head_dim", _I)]
+
+
 _lib = None
 
 
@@ -60,13 +67,16 @@ def lib():
         L.wz_cache_append.argtypes = [_P, _P, _P, _P, _L, _P, _L, _P, _L, _I, _P, _L,
                                       _I, _P]
         L.wz_attention_workspace_bytes.argtypes = [_P, _P, _P]
-        L.wz_attention_workspace_bytes.restype = _S
         L.wz_cache_attention.argtypes = [_P, _P, _P, _P, _L, _P, _L, _P, _P, _S, _P]
         L.wz_quantize_rows.argtypes = [_P, _L, _I, _I, _I, _P, _L, _P, _P]
         L.wz_matmul_int.argtypes = [_P, _L, _P, _P, _L, _P, _P, _I, _I, _I, _P, _L, _I, _P]
+        L.wz_matmul_int_epilogue.argtypes = [_P, _L, _P, _P, _L, _P, _P, _I, _P, _L, _I, _I, _I, _P, _L, _I, _P]
+        L.wz_gated_int.argtypes = [_P, _L, _P, _P, _L, _P, _P, _P, _L, _P, _P, _I, _I, _I, _I, _P, _L, _I, _P]
+        L.wz_norm_quantize.argtypes = [_P, _L, _P, _L, _P, _F, _I, _I, _I, _P, _L, _P, _L, _P, _P]
+        L.wz_decay_workspace_bytes.argtypes = [_P, _P]
+        L.wz_decay_attention.argtypes = [_P, _P, _P, _P, _P, _L, _P, _L, _P, _L, _I, _F, _P, _L, _P, _S, _P]
         for f in EXPORTS:
-            if f != "wz_attention_workspace_bytes":
-                getattr(L, f).restype = ctypes.c_int
+            getattr(L, f).restype = _S if f in SIZES else ctypes.c_int
         _lib = L
     return _lib
 
@@ -155,6 +165,30 @@ class Rotation:
         return type(self), (self._table, self._sections, self._interleaved)
 
 
+class States:
+    """The states of one layer with linear attention: [slots, heads, head_dim, head_dim] float32, keys' elements before
+    values'.  The field cannot be assigned; the tensor's contents are the layer's memory."""
+    __slots__ = ("_state", "_c")
+    state, c = _fixed(*__slots__)
+
+    def __init__(self, state):
+        self._c = _native.states(state)
+        self._state = state
+
+    def __reduce__(self):  # (a copy packs its own tensor)
+        return type(self), (self._state,)
+
+    device = property(lambda self: self._state.device)
+    slots = property(lambda self: self._state.shape[0])
+    heads = property(lambda self: self._state.shape[1])
+    head_dim = property(lambda self: self._state.shape[2])
+
+    @classmethod
+    def new(cls, slots, heads, head_dim, device="cuda:0"):
+        """Empty states (nothing in them needs initialising)."""
+        return cls(torch.empty(slots, heads, head_dim, head_dim, dtype=torch.float32, device=device))
+
+
 def cache_append(cache, batch, k, v, rotation=None, positions=None, q=None, q_out=None):
     """wz_cache_append: store the batch's new keys and values (k, v [tokens, kv_heads, head_dim] float32 or bfloat16),
     rotated by positions [axes, tokens] int32; returns the rotated queries [tokens, q_heads, head_dim] bfloat16 if q
@@ -179,7 +213,36 @@ def quantize_rows(x, out=None, scale=None):
     return _native.quantize_rows(x, out, scale)
 
 
-def matmul_int(a, a_scale, w, w_scale, bias=None, out=None, out_dtype=torch.bfloat16):
+def matmul_int(a, a_scale, w, w_scale, bias=None, out=None, out_dtype=torch.bfloat16, activation=None, residual=None):
     """wz_matmul_int: a [M, K] and w [N, K] int8 with scales [M] and [N] -> a w^T, scaled, + bias [N], as out_dtype
-    [M, N] (or the type of out)."""
-    return _native.matmul_int(a, a_scale, w, w_scale, bias, out, out_dtype)
+    [M, N] (or the type of out).  With an activation ("relu", "silu", "gelu" or "gelu_tanh") or a residual [M, N] of
+    the type of out (which may be out itself), wz_matmul_int_epilogue: residual + activation(product + bias)."""
+    return _native.matmul_int(a, a_scale, w, w_scale, bias, out, out_dtype, activation, residual)
+
+
+def gated_int(a, a_scale, gate, gate_scale, up, up_scale, activation="silu", gate_bias=None, up_bias=None, out=None,
+              out_dtype=torch.bfloat16):
+    """wz_gated_int: activation(a gate^T + gate_bias) * (a up^T + up_bias), the products scaled as matmul_int's; gate
+    and up [N, K] int8 with scales [N], as out_dtype [M, N] (or the type of out)."""
+    return _native.gated_int(a, a_scale, gate, gate_scale, up, up_scale, activation, gate_bias, up_bias, out, out_dtype)
+
+
+def norm_quantize(x, weight, eps=1e-6, residual=None, total=None, out=None, scale=None):
+    """wz_norm_quantize: the root-mean-square norm of x [rows, cols] float32 or bfloat16, times weight [cols] float32 ->
+    (int8 [rows, cols], scale [rows] float32).  With a residual like x the norm is of their sum, which is the third result
+    (total, which may be x or residual itself)."""
+    return _native.norm_quantize(x, weight, eps, residual, total, out, scale)
+
+
+def decay_workspace_bytes(states, batch):
+    """Bytes of workspace decay_attention() needs."""
+    return _native.decay_workspace(states._c, batch._c)
+
+
+def decay_attention(states, batch, slot, q, k, v, log_decay, scale=None, out=None, ws=None):
+    """wz_decay_attention: linear attention with a decay for each head, S <- exp(log_decay) S + k v^T and out = scale q S
+    token after token, from and to the states of slot [batch] int32 (which hold what is before the batch's new tokens; the
+    batch's table is not looked at).  q [tokens, heads, head_dim], k and v [tokens, kv_heads, head_dim] bfloat16, log_decay
+    [heads] float32 -> out like q.  scale defaults to head_dim ** -0.5; ws is a uint8 workspace (allocated if not given
+    and needed)."""
+    return _native.decay_attention(states._c, batch._c, slot, q, k, v, log_decay, scale, out, ws)
