@@ -27,7 +27,10 @@ __global__ __launch_bounds__(kWave) void k_decay_token(DecayArgs p) {
 #pragma unroll
     for (int i = 0; i < kRows; ++i) S[i] = *reinterpret_cast<const f32x4*>(state + i * D);
   }
-  const float l = exp2f(log2_decay(p, h));
+  // The factor in two parts: rounded to one, it would be off the same way for
+  // every token of a long answer (by 2^-25 each).
+  const double factor = exp2(double(log2_decay(p, h)));
+  const float l = float(factor), l2 = float(factor - l);
   const uint16_t* q = static_cast<const uint16_t*>(p.q) + s.start * p.q_stride + h * D + part * kRows;
   const uint16_t* k = static_cast<const uint16_t*>(p.k) + s.start * p.k_stride + kh * D + part * kRows;
   const uint16_t* v = static_cast<const uint16_t*>(p.v) + s.start * p.v_stride + kh * D + slice * 32 + 4 * col;
@@ -48,7 +51,7 @@ __global__ __launch_bounds__(kWave) void k_decay_token(DecayArgs p) {
       const float qe = i % 2 ? bf16_hi(qw) : bf16_lo(qw), ke = i % 2 ? bf16_hi(kw) : bf16_lo(kw);
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        S[i][e] = fmaf(S[i][e], l, ke * ve[e]);
+        S[i][e] = fmaf(S[i][e], l, fmaf(S[i][e], l2, ke * ve[e]));
         o[e] = fmaf(qe, S[i][e], o[e]);
       }
     }

@@ -156,8 +156,18 @@ struct DecayArgs {
   void* out;
   int64_t q_stride, k_stride, v_stride, out_stride;
   float scale;
-  int group;  // heads that share a key head
+  int group;     // heads that share a key head
+  int segments;  // the plan's: of a sequence at most, each of `segment` tokens (a multiple of 64) but its last
+  int segment;
+  float* part;   // segments > 1: [batch][segments][heads][head_dim][head_dim], the state that each begins with
 };
+struct DecayPlan {
+  bool token;  // token after token; otherwise in chunks
+  int segments, segment;
+  size_t bytes;
+};
+DecayPlan decay_plan(const wz_states& z, const wz_ragged& r);
 hipError_t launch_decay_token(const DecayArgs& p, hipStream_t s);
+hipError_t launch_decay_prompt(const DecayArgs& p, hipStream_t s);
 
 }  // namespace wz

@@ -279,7 +279,7 @@ wz_status wz_norm_quantize(const void* x, int64_t x_stride, const void* residual
 
 size_t wz_decay_workspace_bytes(const wz_states* states, const wz_ragged* batch) {
   if (check_states(states, batch) != WZ_OK) return 0;
-  return 0;
+  return decay_plan(*states, *batch).bytes;
 }
 
 wz_status wz_decay_attention(const wz_states* states, const wz_ragged* batch, const int32_t* slot,
@@ -303,7 +303,15 @@ wz_status wz_decay_attention(const wz_states* states, const wz_ragged* batch, co
   if (out == q || out == k || out == v) return WZ_ERR_PARAM;
   DecayArgs p{*states, *batch, slot, log_decay, q, k, v, out, q_stride, k_stride, v_stride, out_stride, scale,
               heads / kv_heads};
-  return from_hip(launch_decay_token(p, static_cast<hipStream_t>(stream)));
+  const DecayPlan plan = decay_plan(*states, *batch);
+  p.segments = plan.segments, p.segment = plan.segment;
+  if (plan.bytes) {
+    if (!ws) return WZ_ERR_NULL;
+    if (!aligned(ws, 256) || ws_bytes < plan.bytes) return WZ_ERR_WORKSPACE;
+    p.part = static_cast<float*>(ws);
+  }
+  const auto s = static_cast<hipStream_t>(stream);
+  return from_hip(plan.token ? launch_decay_token(p, s) : launch_decay_prompt(p, s));
 }
 
 }  // extern "C"

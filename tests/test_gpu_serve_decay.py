@@ -204,10 +204,12 @@ def test_bounds_above_the_lengths_and_below():
     c = Layer([5, 20], [1, 1], 2, 2, 64, seed=4)
     for most in (20, 64, 700, 5000):
         c.check(*c.run(batch=c.batch(most)), f"max_tokens {most}")
-    got, states = c.run(batch=c.batch(3))
-    cut = Layer([5, 20], [1, 1], 2, 2, 64, seed=4)
-    first, _ = Layer.run(c)
-    assert torch.equal(got[:3], first[:3]) and torch.equal(got[5:8], first[5:8])
+    got, _ = c.run(batch=c.batch(3))  # (another plan: the same rows to within the bounds of both)
+    out, mag, _, _ = c.want()
+    g = got.float().cpu().numpy().astype(np.float64)
+    for rows in (slice(0, 3), slice(5, 8)):
+        tol = (2.0 ** -14 + U * (4 * 21 + 160)) * mag[rows]
+        assert (np.abs(g[rows] - out[rows]) <= tol + 2.0 ** -8 * (np.abs(out[rows]) + tol)).all()
     assert (got[3:5] == 9).all() and (got[8:25] == 9).all()
 
 
