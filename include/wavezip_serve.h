@@ -272,8 +272,8 @@ typedef struct {
 } wz_states;
 
 /* Bytes of workspace wz_decay_attention needs (0 if the arguments are invalid or
- * none is needed), at most 256 MiB: what segments of long sequences add to the
- * state.  Depends on batch, max_tokens, heads and head_dim alone.            */
+ * none is needed), at most 128 MiB: what parts of long sequences add to their
+ * states.  Depends on batch, tokens, max_tokens, heads and head_dim alone. */
 size_t wz_decay_workspace_bytes(const wz_states* states, const wz_ragged* batch);
 
 /* Linear attention with a decay for each head.  For each new token t of a sequence,
@@ -291,10 +291,10 @@ size_t wz_decay_workspace_bytes(const wz_states* states, const wz_ragged* batch)
  * token itself is seen); above 0 it counts as 0, and a NaN makes the head's rows and
  * states NaN.  q and out: bf16 rows of `heads` heads; k and v of kv_heads heads,
  * which divide heads: head h reads key head h / (heads / kv_heads).  Strides are
- * multiples of 8 elements, pointers 16-byte aligned; out must not overlap q, k or v.
- * scale: finite.  Sums and states are fp32; a state's sum takes the products exact
- * in fp32, the outputs of prompts take the state and the decayed scores with 16
- * significant bits and more.  A NaN or an infinity in a token's key, value or query
+ * multiples of 8 elements, at most 2^22 (out's any), pointers 16-byte aligned; out
+ * must not overlap q, k or v.  scale: finite.  Sums and states are fp32 (elements of
+ * values and of states up to 2^110); a state's sum takes a decayed value with all of
+ * its 24 bits, the outputs of prompts take the state and the decayed scores with 15.  A NaN or an infinity in a token's key, value or query
  * reaches those elements of rows and states that depend on it by the formula (as
  * one or the other), and no others.  Rows of tokens that no sequence has are not
  * written.  slot: int32 [batch].  ws: 256-byte aligned, at least

@@ -498,11 +498,12 @@ PyObject* norm_quantize(PyObject*, PyObject* const* a, Py_ssize_t n) {
   });
 }
 
-// (states, batch) -> bytes of workspace
+// (states, batch, tokens) -> bytes of workspace
 PyObject* decay_workspace(PyObject*, PyObject* const* a, Py_ssize_t n) {
-  return guarded(n, 2, [&] {
+  return guarded(n, 3, [&] {
     const auto z = unpack<wz_states>(a[0]);
-    const auto r = unpack<wz_ragged>(a[1]);
+    auto r = unpack<wz_ragged>(a[1]);
+    r.x.tokens = int32_t(integer("tokens", a[2]));
     return PyLong_FromSize_t(wz_decay_workspace_bytes(&z.x, &r.x));
   });
 }

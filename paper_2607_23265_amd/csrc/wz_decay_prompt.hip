@@ -14,6 +14,8 @@
 // Factors that are not bf16 already are taken apart: the state's sums take the
 // decayed values in three parts, which is all of their 24 bits; the outputs, which
 // are rounded to bf16 themselves, take the state and the decayed scores in two.
+#include <cmath>
+
 #include "wz_decay.h"
 
 namespace wz {
@@ -22,386 +24,491 @@ namespace {
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 
 constexpr int kChunk = 64;
+constexpr float kRaised = 16.f;  // log2 of what a state is raised by at most
 
 __device__ __forceinline__ f32x16 mfma(u32x4 a, u32x4 b, f32x16 c) {
-  return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+  return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0,
+                                                 0);
 }
-// The upper halves of two numbers: both cut to bf16.
-__device__ __forceinline__ uint32_t upper(float lo, float hi) {
-  return __builtin_amdgcn_perm(__float_as_uint(hi), __float_as_uint(lo), 0x07060302);
-}
-// 2^x; below fp32's normal numbers zero.
-__device__ __forceinline__ float power(float x) { return __builtin_amdgcn_exp2f(x); }
-__device__ __forceinline__ float rest(float x) { return x - __uint_as_float(__float_as_uint(x) & 0xffff0000u); }
 __device__ __forceinline__ uint32_t pair(float lo, float hi) {
-  typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
   return __builtin_bit_cast(uint32_t, bf16x2{__bf16(lo), __bf16(hi)});
 }
+// c and the products of two pairs of bf16.
+__device__ __forceinline__ float dot2(uint32_t a, uint32_t b, float c) {
+  return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, a), __builtin_bit_cast(bf16x2, b), c, false);
+}
+// Two numbers cut to bf16 (their upper halves), and what that leaves of them: a
+// product with -1 and a sum in one instruction.  The constants have to lie in
+// vector registers.
+struct Cut {
+  uint32_t low, high;  // (-1, 0) and (0, -1)
+  __device__ __forceinline__ uint32_t operator()(float& x, float& y) const {
+    const uint32_t u = __builtin_amdgcn_perm(__float_as_uint(y), __float_as_uint(x), 0x07060302);
+    x = dot2(u, low, x), y = dot2(u, high, y);
+    return u;
+  }
+};
+// 2^x; below fp32's normal numbers zero.
+__device__ __forceinline__ float power(float x) { return __builtin_amdgcn_exp2f(x); }
 
-// Where a sequence's segment begins: its state in the workspace, in the order of
-// the accumulators ([wave][rows of 32][16 rows of those in four][lane], four
-// numbers each).
-template <int D>
-__device__ __forceinline__ f32x4* begins(const DecayArgs& p, int b, int seg, int h, int wave) {
-  return reinterpret_cast<f32x4*>(p.part + ((int64_t(b) * p.segments + seg) * p.states.heads + h) * (D * D)) +
-         wave * (D / 32) * 4 * kWave + __lane_id();
+// A state in the workspace, in the order of the accumulators ([wave][rows of 32]
+// [16 rows of those in four][lane], four numbers each).
+__device__ __forceinline__ float* stored(const DecayArgs& p, int kind, int run, int h) {
+  return p.part + ((int64_t(kind) * p.runs + run) * p.states.heads + h) * (p.states.head_dim * p.states.head_dim);
+}
+constexpr int kBegins = 0;  // what a run's first sequence has before the run, if that goes on from another run
+constexpr int kFirst = 1;   // what a run's last sequence has before the call, if that begins in the run and goes on
+constexpr int kHalf = 2;    // what the first half of a run's last sequence adds, if that goes on
+
+// Chunks from one sequence to the next: a run's are [lo, hi) of all.
+__device__ __forceinline__ int chunks_of(const Seq& s) { return (s.n + kChunk - 1) / kChunk; }
+struct Run {
+  int seq, at;  // its first chunk's sequence, and the chunk's number there
+  int chunks;
+};
+// LAST: of the run, what belongs to its last sequence.
+template <bool LAST>
+__device__ __forceinline__ Run run_of(const DecayArgs& p, int run) {
+  if (p.runs == 0) return Run{run, 0, chunks_of(sequence(p.batch, run))};  // a sequence each
+  int all = 0;
+  for (int b = 0; b < p.batch.batch; b += kWave) {
+    const int mine = b + __lane_id();
+    const int n = mine < p.batch.batch ? chunks_of(sequence(p.batch, mine)) : 0;
+    all += __builtin_amdgcn_readlane(wave_incl_scan_i32(n), kWave - 1);
+  }
+  const int lo = int(int64_t(run) * all / p.runs), hi = int(int64_t(run + 1) * all / p.runs);
+  if (lo >= hi) return Run{0, 0, 0};
+  const Found f = find_item(p.batch, LAST ? hi - 1 : lo, [](const Seq& s) { return chunks_of(s); });
+  if (f.seq < 0) return Run{0, 0, 0};  // (rows that overlap against the contract, past 32 bits)
+  if (!LAST) return Run{f.seq, f.local, hi - lo};
+  const int at = max(f.local - (hi - 1 - lo), 0);
+  return Run{f.seq, at, f.local - at + 1};
 }
 
-// OUT: outputs and the last state; otherwise what a segment adds to the state.
+// A workgroup goes through a run of chunks.  OUT: outputs, and the sequences' last
+// states.  Otherwise, where the run's last sequence goes on in the next run, what
+// its chunks here add to the state.
 template <int D, bool OUT>
 __global__ __launch_bounds__(2 * D, 2) void k_decay_prompt(DecayArgs p) {
   constexpr int W = D / 32, NA = D / 32, kUnits = D / 8;  // waves; tiles of the state's rows; 16-byte units of a row
-  // (scores are written where the keys lay, once every wave is done with those)
-  constexpr int kScores = 2 * kChunk * kChunk;
-  __shared__ __align__(256) uint16_t lds[OUT ? 3 * kChunk * D + (kChunk * D > kScores ? kChunk * D : kScores) : 2 * kChunk * D];
-  __shared__ __align__(16) float weight[kChunk];
-  __shared__ uint32_t odd[2][2];  // tokens with a number that is none, of this chunk and of the next
   // [D][64 tokens] keys, values; [64][D] queries, keys, in the order of the accumulators' rows; [2 parts][64][64
-  // tokens] scores: bytes from the beginning
-  constexpr uint32_t kt = 0, vt = 2 * kChunk * D, qs = 2 * vt, ks = 3 * vt, sc = ks;
-  constexpr uint32_t kRow = 2 * D, kCol = 2 * kChunk;  // bytes of a row
-  auto at16 = [&](uint32_t to) -> u32x4& { return *reinterpret_cast<u32x4*>(reinterpret_cast<char*>(lds) + to); };
-  auto at8 = [&](uint32_t to) -> u32x2& { return *reinterpret_cast<u32x2*>(reinterpret_cast<char*>(lds) + to); };
-  auto at2 = [&](uint32_t to) -> uint16_t& { return *reinterpret_cast<uint16_t*>(reinterpret_cast<char*>(lds) + to); };
+  // tokens] scores, where the keys lay, once every wave is done with those
+  constexpr int kt = 0, vt = 2 * kChunk * D, qs = 2 * vt, ks = 3 * vt, sc = ks;
+  constexpr int kRow = 2 * D, kCol = 2 * kChunk;  // bytes of a row
+  __shared__ __align__(256) char lds[OUT ? ks + (vt > 2 * 64 * kCol ? vt : 2 * 64 * kCol) : qs];
+  __shared__ __align__(16) float weight[kChunk];
+  __shared__ int strange[OUT ? D : 1];  // of each element of the values, the first token where it is no number
 
-  const int lane = __lane_id(), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), c = lane & 31, g = lane >> 5;
-  const int h = blockIdx.x % p.states.heads, rest_id = blockIdx.x / p.states.heads;
-  const int segs = OUT ? p.segments : p.segments - 1;
-  const int seg = rest_id % segs, b = rest_id / segs;
-  const Seq s = sequence(p.batch, b);
-  const int first = p.segments > 1 ? seg * p.segment : 0;
-  const int last = p.segments > 1 ? min(s.n, first + p.segment) : s.n;
-  // (a segment that is its sequence's last adds to no other's beginning)
-  if (first >= s.n || (!OUT && last >= s.n)) return;
-  const int slot = p.slot[b];
-  const bool kept = uint32_t(slot) < uint32_t(p.states.slots);
-  float* const state = p.states.state + (int64_t(kept ? slot : 0) * p.states.heads + h) * (D * D) + wave * 32 + c;
+  const int lane = __lane_id(), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+  const int c = lane & 31, g = lane >> 5;
+  // Workgroups go to the XCDs in turn: heads that share a key head to the same
+  // one, whose L2 they read it from.
+  const int x = blockIdx.x % kXcds, y = blockIdx.x / kXcds, kv_heads = p.states.heads / p.group;
+  const int runs = p.runs ? p.runs : p.batch.batch, set = y / p.group * kXcds + x, halves = OUT ? 1 : 2;
+  if (set >= runs * kv_heads * halves) return;
+  const int kh = set % kv_heads, h = kh * p.group + y % p.group, run = set / kv_heads / halves;
+  const int half = OUT ? 0 : set / kv_heads % 2;
+  const Run all = run_of<!OUT>(p, run);
+  int goes_on = 0;
   float ld = log2_decay(p, h);
   const int b0 = wave * 32;
 
-  f32x16 S[NA] = {};
-  if constexpr (OUT) {
-    if (p.segments > 1) {
-      const f32x4* from = begins<D>(p, b, seg, h, wave);
-#pragma unroll
-      for (int i = 0; i < NA * 4; ++i) {
-        const f32x4 x = from[i * kWave];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) S[i / 4][i % 4 * 4 + e] = x[e];
-      }
-    } else if (kept && s.place0 > 0) {
-#pragma unroll
-      for (int a = 0; a < NA; ++a)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) S[a][r] = state[(32 * a + 8 * (r / 4) + 4 * g + r % 4) * D];
-    }
-  }
-
-  // A thread moves four tokens' 16 bytes of queries, keys and values.
+  Seq s;
+  int last;  // behind the last token of the sequence in this run
+  // A thread moves four tokens' 16 bytes of queries, keys and values.  Tokens behind
+  // the last one lie behind the buffer's end and read as zeros.
   int unit = threadIdx.x % kUnits, quad = threadIdx.x / kUnits;
-  const int kh = h / p.group;
-  const uint16_t* const qp = static_cast<const uint16_t*>(p.q) + s.start * p.q_stride + h * D + 8 * unit;
-  const uint16_t* const kp = static_cast<const uint16_t*>(p.k) + s.start * p.k_stride + kh * D + 8 * unit;
-  const uint16_t* const vp = static_cast<const uint16_t*>(p.v) + s.start * p.v_stride + kh * D + 8 * unit;
   u32x4 nq[4], nk[4], nv[4];
-  auto fetch = [&](int t0) {
+  auto get = [&](const void* base, int64_t stride, int head, int t0, u32x4 (&to)[4]) {
+    const int rows = min(kChunk, last - t0);
+    const auto r = make_rsrc_uniform(static_cast<const uint16_t*>(base) + (s.start + t0) * stride + head * D,
+                                     uint32_t((rows - 1) * int(stride) + D) * 2);
+    int at = 4 * quad * int(2 * stride) + 16 * unit;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int t = min(t0 + 4 * quad + i, last - 1);
-      if constexpr (OUT) nq[i] = *reinterpret_cast<const u32x4*>(qp + t * p.q_stride);
-      nk[i] = *reinterpret_cast<const u32x4*>(kp + t * p.k_stride);
-      nv[i] = *reinterpret_cast<const u32x4*>(vp + t * p.v_stride);
-    }
+    for (int i = 0; i < 4; ++i, at += int(2 * stride)) to[i] = buf_load_u32x4(r, at);
   };
+  auto fetch = [&](int t0) {
+    get(p.k, p.k_stride, kh, t0, nk);
+    get(p.v, p.v_stride, kh, t0, nv);
+    if constexpr (OUT) get(p.q, p.q_stride, h, t0, nq);
+  };
+  // (barriers order LDS alone: the next chunk's loads stay under way)
+  //
   // The 16-byte units of a row are exchanged by the row's number, so that 16 lanes
   // that read one unit of 16 rows hit all banks, and writes of four tokens half of
-  // them.  The number is the unit's xor some bits of the row's: a lane's reads differ by
-  // an xor with constants.
+  // them.  A unit's place is its number xor some bits of the row's: a lane's reads
+  // differ by an xor with constants.
   auto row_x = [](int row) { return kUnits == 16 ? row & 15 : row >> 1 & 7; };
   auto col_x = [](int row) { return (row >> 1 ^ row >> 4) & 7; };
-  auto row_at = [&](uint32_t base, int row, int u) { return base + row * kRow + 16 * (u ^ row_x(row)); };
-  auto col_at = [&](uint32_t base, int row, int u) { return base + row * kCol + 16 * (u ^ col_x(row)); };
-  // this lane's unit g of rows c (the others: rows 32 i + c, units 2 k + g)
-  uint32_t my_row = row_at(0, c, g), my_col = col_at(0, c, g), my_sc = c * kCol + 16 * (g ^ (c >> 1 & 7));
-  auto read_row = [&](uint32_t base, int i, int k) -> u32x4 { return at16(base + 32 * i * kRow + (my_row ^ 32 * k)); };
-  auto read_col = [&](uint32_t base, int i, int k) -> u32x4 { return at16(base + 32 * i * kCol + (my_col ^ 32 * (k ^ i))); };
-  auto read_sc = [&](int part, int i, int k) -> u32x4 { return at16(sc + (64 * part + 32 * i) * kCol + (my_sc ^ 32 * k)); };
-  auto store_rows = [&](uint32_t base, const u32x4 (&x)[4]) {
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-#pragma unroll
-      for (int half = 0; half < 2; ++half)
-        at8(row_at(base, 4 * quad + i, unit / 2 * 2 + half) + 8 * (unit & 1)) =
-            u32x2{x[i][2 * half], x[i][2 * half + 1]};
+  // this lane's unit g of rows c (its others: rows 32 i + c, units 2 k + g)
+  int my_row = c * kRow + 16 * (g ^ row_x(c)), my_col = c * kCol + 16 * (g ^ col_x(c));
+  int my_sc = c * kCol + 16 * (g ^ (c >> 1 & 7));
+  auto read = [&](int to, int more) { return *reinterpret_cast<const u32x4*>(lds + to + more); };
+  auto read_row = [&](int base, int i, int k) { return read(my_row ^ 32 * k, base + 32 * i * kRow); };
+  auto read_col = [&](int base, int i, int k) { return read(my_col ^ 32 * (k ^ i), base + 32 * i * kCol); };
+  auto read_sc = [&](int part, int i, int k) { return read(my_sc ^ 32 * k, sc + (64 * part + 32 * i) * kCol); };
+  auto write8 = [&](int to, int more, uint32_t lo, uint32_t hi) {
+    *reinterpret_cast<u32x2*>(lds + to + more) = u32x2{lo, hi};
   };
-  auto store_columns = [&](uint32_t base, const u32x4 (&x)[4]) {
+  auto store_rows = [&](int base, const u32x4 (&v)[4]) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int row = 4 * quad + i, to = row * kRow + 16 * ((unit & ~1) ^ row_x(row)) + 8 * (unit & 1);
+      write8(to, base, v[i][0], v[i][1]);
+      write8(to ^ 16, base, v[i][2], v[i][3]);
+    }
+  };
+  auto store_columns = [&](int base, const u32x4 (&v)[4]) {
+    const int to = 8 * unit * kCol + 16 * (quad / 2 ^ col_x(8 * unit)) + 8 * (quad & 1);
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
       const uint32_t pick = e % 2 ? 0x07060302 : 0x05040100;
-      at8(col_at(base, 8 * unit + e, quad / 2) + 8 * (quad & 1)) =
-          u32x2{__builtin_amdgcn_perm(x[1][e / 2], x[0][e / 2], pick), __builtin_amdgcn_perm(x[3][e / 2], x[2][e / 2], pick)};
+      write8(to ^ 16 * (e >> 1), base + e * kCol, __builtin_amdgcn_perm(v[1][e / 2], v[0][e / 2], pick),
+             __builtin_amdgcn_perm(v[3][e / 2], v[2][e / 2], pick));
     }
   };
+  Cut cut{0x0000bf80u, 0xbf800000u};
+  uint32_t zero = 0;
+  asm volatile("" : "+v"(cut.low), "+v"(cut.high), "+v"(zero));
 
-  if (threadIdx.x < 4) odd[threadIdx.x / 2][threadIdx.x % 2] = 0;
-  __syncthreads();
-  fetch(first);
-  int parity = 0;
-  for (int t0 = first; t0 < last; t0 += kChunk, parity ^= 1) {
-    const int len = min(kChunk, last - t0);
-    asm volatile("" : "+v"(unit), "+v"(quad));
-    // a key or a value that is no number, by its exponent
-    uint32_t strange = 0;
+  // the decays from a score's token to its query, and the scale
+  constexpr int kMine = OUT ? (3 + W - 1) / W : 1;  // of the three tiles of scores
+  f32x16 by_gap[kMine];
+  if constexpr (OUT) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const bool in = 4 * quad + i < len;
-      typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
-      u16x2 top = {};
+    for (int m = 0; m < kMine; ++m)
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        nk[i][e] = in ? nk[i][e] : 0u, nv[i][e] = in ? nv[i][e] : 0u;
-        if constexpr (OUT) nq[i][e] = in ? nq[i][e] : 0u;
-        top = __builtin_elementwise_max(top, __builtin_bit_cast(u16x2, nk[i][e] & 0x7fff7fffu));
-        top = __builtin_elementwise_max(top, __builtin_bit_cast(u16x2, nv[i][e] & 0x7fff7fffu));
-      }
-      strange |= top[0] >= 0x7f80 || top[1] >= 0x7f80 ? 1u << i : 0u;
+      for (int r = 0; r < 16; ++r)
+        by_gap[m][r] =
+            power(float(max((wave + m * W == 2 ? 32 : 0) + c - 4 * g - 8 * (r / 4) - r % 4, 0)) * ld) * p.scale;
+  }
+  int b = all.seq, at = all.at, left = all.chunks;
+  while (left > 0 && b < p.batch.batch) {
+    s = sequence(p.batch, b);
+    int chunks = min(chunks_of(s) - at, left), first = at * kChunk;
+    if (OUT && chunks <= 0) {  // (a sequence without tokens)
+      ++b, at = 0;
+      continue;
     }
-    if (strange) atomicOr(&odd[parity][quad / 8], strange << (4 * quad & 31));
-    auto weigh = [&](int end) {  // a token's decay up to the one before `end`
-      if (threadIdx.x < kChunk) weight[threadIdx.x] = power(float(max(end - 1 - int(threadIdx.x), 0)) * ld);
-    };
-    if (t0 == first || len < kChunk) weigh(len);
-    store_columns(kt, nk);
-    store_columns(vt, nv);
-    if constexpr (OUT) {
-      store_rows(qs, nq);
-      store_rows(ks, nk);
+    left -= chunks;
+    last = min(s.n, first + chunks * kChunk);
+    const bool on = last < s.n;  // in the next run
+    if constexpr (!OUT) {
+      if (!on) break;
+      goes_on = first == 0 ? -chunks : chunks;
+      if (half) first += chunks / 2 * kChunk;
+      else last = first + chunks / 2 * kChunk;
     }
-    __syncthreads();
-    if (threadIdx.x < 2) odd[parity ^ 1][threadIdx.x] = 0;  // (read by none before the next chunk's barrier)
-    const uint64_t marked = uint64_t(__builtin_amdgcn_readfirstlane(odd[parity][1])) << 32 |
-                            uint32_t(__builtin_amdgcn_readfirstlane(odd[parity][0]));
-    if (!marked && t0 + kChunk < last) fetch(t0 + kChunk);
-    uint16_t* const out = OUT ? static_cast<uint16_t*>(p.out) + (s.start + t0) * p.out_stride + h * D + b0 : nullptr;
-    // In a product with zeros what is no number would reach rows that do not see it:
-    // a chunk is worked on in pieces, a token with such a number and those between two
-    // of them, the others' keys and values being zeros.  (All but always: one piece.)
-    for (int u0 = 0, u1; u0 < len; u0 = u1) {
-    // (what is worked out from these is not worth a register from chunk to chunk)
-    int row = c, four = 4 * g;
-    asm volatile("" : "+v"(my_row), "+v"(my_col), "+v"(my_sc), "+v"(ld), "+v"(row), "+v"(four));
-    const uint64_t ahead = marked >> u0;
-    u1 = ahead & 1 ? u0 + 1 : ahead ? u0 + __builtin_ctzll(ahead) : len;
-    if (marked) {
-      __syncthreads();
-      weigh(u1);
-      if constexpr (OUT) store_rows(ks, nk);  // (where the last piece's scores were)
-      __syncthreads();
-    }
-    auto piece = [&](int k, u32x4& x) {
-      if (marked) {
+    const int slot = p.slot[b];
+    const bool kept = uint32_t(slot) < uint32_t(p.states.slots);
+    const auto state =
+        make_rsrc_uniform(p.states.state + (int64_t(kept ? slot : 0) * p.states.heads + h) * (D * D), D * D * 4);
+    auto row_of = [](int a, int r) { return 4 * D * (32 * a + 8 * (r / 4) + r % 4); };  // bytes from the lane's first
+    // this lane's element of a state's first row of four, and its first four in the accumulators' order
+    int in_state = 4 * (4 * g * D + wave * 32 + c), in_order = 16 * (wave * NA * 4 * kWave + lane);
+    asm volatile("" : "+v"(in_state), "+v"(in_order));
+    f32x16 S[NA] = {};
+    auto from = [&](const float* base) {
+      const auto r = make_rsrc_uniform(base, D * D * 4);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const int t = 16 * k + 2 * four + 2 * e;
-          x[e] &= (t >= u0 && t < u1 ? 0xffffu : 0u) | (t + 1 >= u0 && t + 1 < u1 ? 0xffff0000u : 0u);
-        }
+      for (int i = 0; i < NA * 4; ++i) {
+        const f32x4 v =
+            __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(r, in_order, i * 16 * kWave, 0));
+#pragma unroll
+        for (int e = 0; e < 4; ++e) S[i / 4][i % 4 * 4 + e] = v[e];
       }
     };
-    u32x4 vf[4];
-    auto read_values = [&] {
+    auto into = [&](float* base) {
+      const auto r = make_rsrc_uniform(base, D * D * 4);
 #pragma unroll
-      for (int k = 0; k < 4; ++k) vf[k] = read_col(vt, wave, k), piece(k, vf[k]);
+      for (int i = 0; i < NA * 4; ++i) {
+        const f32x16& x = S[i / 4];
+        const f32x4 v = {x[i % 4 * 4], x[i % 4 * 4 + 1], x[i % 4 * 4 + 2], x[i % 4 * 4 + 3]};
+        __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, v), r, in_order, i * 16 * kWave, 0);
+      }
     };
-    if constexpr (OUT) {
-      // Scores of 32 x 32 (tokens down, queries across), three of the chunk's four: (0, 0), (32, 32), and (0, 32).
-      constexpr int kMine = (3 + W - 1) / W;
-      f32x16 X[kMine] = {};
-#pragma unroll
-      for (int m = 0; m < kMine; ++m) {
-        const int tile = wave + m * W;
-        if (tile < 3) {
-          const int kr = tile == 1, qr = tile != 0;
-#pragma unroll
-          for (int k = 0; k < D / 16; ++k) {
-            X[m] = mfma(read_row(ks, kr, k), read_row(qs, qr, k), X[m]);
-            if (k % 2) __builtin_amdgcn_sched_barrier(0);
-          }
-        }
-      }
-      __syncthreads();
-#pragma unroll
-      for (int m = 0; m < kMine; ++m) {
-        const int tile = wave + m * W;
-        if (tile < 3) {
-          const int kr = tile == 1, qr = tile != 0;
-#pragma unroll
-          for (int q = 0; q < 4; ++q) {
-            float y[4];
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              const int t = 8 * q + four + e, gap = 32 * (qr - kr) + row - t;
-              const float x = X[m][4 * q + e] * power(float(max(gap, 0)) * ld);
-              y[e] = min(gap, 32 * kr + t - u0) >= 0 ? x : 0.f;
-            }
-            const uint32_t to = sc + 32 * qr * kCol + ((my_sc ^ 4 * four) ^ 16 * (4 * kr + q)) + 2 * four;
-            at8(to) = u32x2{upper(y[0], y[1]), upper(y[2], y[3])};
-            at8(to + 64 * kCol) = u32x2{pair(rest(y[0]), rest(y[1])), pair(rest(y[2]), rest(y[3]))};
-            __builtin_amdgcn_sched_barrier(0);
-          }
-        }
-      }
-      f32x16 O[2] = {};
+    if (OUT && first > 0) {
+      from(stored(p, kBegins, run, h));
+    } else if (OUT && on) {
+      from(stored(p, kFirst, run, h));
+    } else if (kept && s.place0 > 0 && first == 0 && !half) {
 #pragma unroll
       for (int a = 0; a < NA; ++a)
 #pragma unroll
-        for (int kk = 0; kk < 2; ++kk) {
-          u32x4 hi, lo;
+        for (int r = 0; r < 16; ++r)
+          S[a][r] = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(state, in_state, row_of(a, r), 0));
+    }
+    // (the run that stores the sequence's last state may do so before another looks at what the slot holds)
+    if (!OUT && goes_on < 0 && !half) into(stored(p, kFirst, run, h));
+    if (first < last) fetch(first);
+    int age = 0;
+    for (int t0 = first; t0 < last; t0 += kChunk) {
+      const int len = min(kChunk, last - t0);
+      // S, whatever the text says of it, is kept as of `age` tokens ago (without their decay), so that it is not
+      // multiplied with every chunk's; what is added to it is raised by as much.
+      const bool renew = float(age + len) * ld < -kRaised;
+      const int from_age = renew ? -len : age;
+      if (threadIdx.x < kChunk)
+        weight[threadIdx.x] = power(float(-(from_age + 1 + min(int(threadIdx.x), len - 1))) * ld);
+      store_columns(kt, nk);
+      store_columns(vt, nv);
+      if constexpr (OUT) {
+        store_rows(ks, nk);
+        store_rows(qs, nq);
+      }
+      lds_barrier();
+      if (t0 + kChunk < last) fetch(t0 + kChunk);
+      // (what is worked out from these is not worth a register from chunk to chunk)
+      int row = c, four = 4 * g;
+      asm volatile("" : "+v"(my_row), "+v"(my_col), "+v"(my_sc), "+v"(ld), "+v"(row), "+v"(four));
+      uint16_t* const out = OUT ? static_cast<uint16_t*>(p.out) + (s.start + t0) * p.out_stride + h * D + b0 : nullptr;
+      u32x4 vf[4];
+      auto read_values = [&] {
 #pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const float x = S[a][8 * kk + 2 * e], y = S[a][8 * kk + 2 * e + 1];
-            hi[e] = upper(x, y), lo[e] = pair(rest(x), rest(y));
+        for (int k = 0; k < 4; ++k) vf[k] = read_col(vt, wave, k);
+      };
+      if constexpr (OUT) {
+        // Scores of 32 x 32 (tokens down, queries across), three of the chunk's four:
+        // (0, 0), (32, 32), and (0, 32).
+        f32x16 X[kMine];
+#pragma unroll
+        for (int m = 0; m < kMine; ++m) {
+          const int tile = wave + m * W;
+          if (tile < 3) {
+            X[m] = f32x16{};
+            const int kr = my_row + (tile == 1 ? 32 * kRow : 0), qr = my_row + (tile != 0 ? 32 * kRow : 0);
+#pragma unroll
+            for (int k = 0; k < D / 16; ++k) X[m] = mfma(read(kr ^ 32 * k, ks), read(qr ^ 32 * k, qs), X[m]);
           }
-          const u32x4 q0 = read_row(qs, 0, 2 * a + kk), q1 = read_row(qs, 1, 2 * a + kk);
-          O[0] = mfma(hi, q0, O[0]);
-          O[1] = mfma(hi, q1, O[1]);
-          O[0] = mfma(lo, q0, O[0]);
-          O[1] = mfma(lo, q1, O[1]);
-          if (kk) __builtin_amdgcn_sched_barrier(0);
+        }
+        lds_barrier();
+#pragma unroll
+        for (int m = 0; m < kMine; ++m) {
+          const int tile = wave + m * W;
+          if (tile < 3) {
+            const int kr = tile == 1, qr = tile != 0;
+            const int gap = 32 * (qr - kr) + row - four;  // to the token of element 8 q + e: 8 q + e less
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+              float v[4];
+#pragma unroll
+              for (int e = 0; e < 4; ++e) v[e] = gap >= 8 * q + e ? X[m][4 * q + e] * by_gap[m][4 * q + e] : 0.f;
+              const int to = (my_sc ^ 4 * four ^ 16 * (4 * kr + q)) + 2 * four + 32 * qr * kCol;
+              const uint32_t lo = cut(v[0], v[1]), hi = cut(v[2], v[3]);
+              write8(to, sc, lo, hi);
+              write8(to, sc + 64 * kCol, pair(v[0], v[1]), pair(v[2], v[3]));
+            }
+          }
+        }
+        f32x16 O[2] = {};
+#pragma unroll
+        for (int a = 0; a < NA; ++a)
+#pragma unroll
+          for (int kk = 0; kk < 2; ++kk) {
+            u32x4 hi, lo;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const uint32_t v = __float_as_uint(S[a][8 * kk + 2 * e]), w = __float_as_uint(S[a][8 * kk + 2 * e + 1]);
+              hi[e] = __builtin_amdgcn_perm(w, v, 0x07060302);
+              lo[e] = pair(__uint_as_float(v) - __uint_as_float(v & 0xffff0000u),
+                           __uint_as_float(w) - __uint_as_float(w & 0xffff0000u));
+            }
+            const u32x4 q0 = read_row(qs, 0, 2 * a + kk), q1 = read_row(qs, 1, 2 * a + kk);
+            O[0] = mfma(hi, q0, O[0]);
+            O[1] = mfma(hi, q1, O[1]);
+            O[0] = mfma(lo, q0, O[0]);
+            O[1] = mfma(lo, q1, O[1]);
+          }
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          const float f = power(float(age + 32 * i + row + 1) * ld) * p.scale;
+#pragma unroll
+          for (int r = 0; r < 16; ++r) O[i][r] *= f;
+        }
+        lds_barrier();
+        read_values();
+        // A value that is no number (its product with zero is not zero) must not reach the
+        // rows before its token through their scores of zero: it is left out of the
+        // product, and put into the rows from its token on.
+        float none = 0.f;
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            none = dot2(vf[k][e], zero, none);
+        const bool odd = __ballot(none != 0.f) != 0;
+        if (odd) {
+          int token = kChunk;
+#pragma unroll
+          for (int k = 0; k < 4; ++k)
+#pragma unroll
+            for (int e = 7; e >= 0; --e) {
+              const uint32_t half = e % 2 ? 0x7f800000u : 0x7f80u;
+              if ((vf[k][e / 2] & half) == half) {
+                token = min(token, 16 * k + 2 * four + e);
+                vf[k][e / 2] &= e % 2 ? 0xffffu : 0xffff0000u;
+              }
+            }
+          strange[b0 + c] = kChunk;
+          __builtin_amdgcn_wave_barrier();
+          atomicMin(&strange[b0 + c], token);
         }
 #pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        const float f = power(float(max(32 * i + row + 1 - u0, 0)) * ld);
+        for (int k = 0; k < 4; ++k) {
 #pragma unroll
-        for (int r = 0; r < 16; ++r) O[i][r] *= f;
+          for (int part = 0; part < 2; ++part) {
+            if (k < 2) O[0] = mfma(vf[k], read_sc(part, 0, k), O[0]);
+            O[1] = mfma(vf[k], read_sc(part, 1, k), O[1]);
+          }
+        }
+        if (odd) {
+          __builtin_amdgcn_wave_barrier();
+#pragma unroll
+          for (int r = 0; r < 16; ++r) {
+            const int token = strange[b0 + 8 * (r / 4) + four + r % 4];
+#pragma unroll
+            for (int i = 0; i < 2; ++i) O[i][r] = 32 * i + row >= token ? __uint_as_float(0x7fc00000u) : O[i][r];
+          }
+          read_values();
+        }
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+          if (32 * i + row < len) {
+#pragma unroll
+            for (int q = 0; q < 4; ++q)
+              *reinterpret_cast<u32x2*>(out + (32 * i + row) * p.out_stride + 8 * q + four) =
+                  u32x2{pair(O[i][4 * q], O[i][4 * q + 1]), pair(O[i][4 * q + 2], O[i][4 * q + 3])};
+          }
+      } else {
+        read_values();
       }
-      __syncthreads();
-      read_values();
+      if (renew) {
+        const float fade = power(float(age + len) * ld);
+#pragma unroll
+        for (int a = 0; a < NA; ++a)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) S[a][r] *= fade;
+      }
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
+        u32x4 part[3];
+        f32x4 w[2];
 #pragma unroll
-        for (int part = 0; part < 2; ++part) {
-          if (k < 2) O[0] = mfma(vf[k], read_sc(part, 0, k), O[0]);
-          O[1] = mfma(vf[k], read_sc(part, 1, k), O[1]);
+        for (int e = 0; e < 2; ++e) w[e] = *reinterpret_cast<const f32x4*>(weight + 16 * k + 2 * four + 4 * e);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          float lo = bf16_lo(vf[k][e]) * w[e / 2][e % 2 * 2], hi = bf16_hi(vf[k][e]) * w[e / 2][e % 2 * 2 + 1];
+          part[0][e] = cut(lo, hi), part[1][e] = cut(lo, hi);
+          part[2][e] = __builtin_amdgcn_perm(__float_as_uint(hi), __float_as_uint(lo), 0x07060302);
         }
-        __builtin_amdgcn_sched_barrier(0);
+        u32x4 kf[NA];
+#pragma unroll
+        for (int a = 0; a < NA; ++a) kf[a] = read_col(kt, a, k);
+#pragma unroll
+        for (int i = 0; i < 3; ++i)
+#pragma unroll
+          for (int a = 0; a < NA; ++a) S[a] = mfma(kf[a], part[i], S[a]);
+        
       }
-#pragma unroll
-      for (int i = 0; i < 2; ++i)
-        if (32 * i + row >= u0 && 32 * i + row < u1) {
-#pragma unroll
-          for (int q = 0; q < 4; ++q)
-            *reinterpret_cast<u32x2*>(out + (32 * i + row) * p.out_stride + 8 * q + four) =
-                u32x2{pair(O[i][4 * q] * p.scale, O[i][4 * q + 1] * p.scale),
-                      pair(O[i][4 * q + 2] * p.scale, O[i][4 * q + 3] * p.scale)};
-        }
-    } else {
-      read_values();
+      lds_barrier();
+      age = from_age + len;
     }
-    const float fade = power(float(u1 - u0) * ld);
+    if (age > 0) {
+      const float fade = power(float(age) * ld);
 #pragma unroll
-    for (int a = 0; a < NA; ++a)
+      for (int a = 0; a < NA; ++a)
 #pragma unroll
-      for (int r = 0; r < 16; ++r) S[a][r] *= fade;
-#pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      u32x4 part[3];
-      f32x4 w[2];
-#pragma unroll
-      for (int e = 0; e < 2; ++e) w[e] = *reinterpret_cast<const f32x4*>(weight + 16 * k + 2 * four + 4 * e);
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const float x = bf16_lo(vf[k][e]) * w[e / 2][e % 2 * 2], y = bf16_hi(vf[k][e]) * w[e / 2][e % 2 * 2 + 1];
-        const float x1 = rest(x), y1 = rest(y);
-        part[0][e] = upper(x, y), part[1][e] = upper(x1, y1), part[2][e] = upper(rest(x1), rest(y1));
-      }
-      u32x4 kf[NA];
-#pragma unroll
-      for (int a = 0; a < NA; ++a) kf[a] = read_col(kt, a, k), piece(k, kf[a]);
-#pragma unroll
-      for (int i = 0; i < 3; ++i)
-#pragma unroll
-        for (int a = 0; a < NA; ++a) S[a] = mfma(kf[a], part[i], S[a]);
-      __builtin_amdgcn_sched_barrier(0);
+        for (int r = 0; r < 16; ++r) S[a][r] *= fade;
     }
-    }
-    __syncthreads();
-    if (marked && t0 + kChunk < last) {
-      fetch(t0 + kChunk);
-      weigh(kChunk);
-    }
-  }
 
-  if constexpr (!OUT) {
-    f32x4* to = begins<D>(p, b, seg + 1, h, wave);
+    if constexpr (!OUT) {
+      into(half ? stored(p, kBegins, run + 1, h) : stored(p, kHalf, run, h));
+    } else if (kept && !on) {
 #pragma unroll
-    for (int i = 0; i < NA * 4; ++i)
-      to[i * kWave] = f32x4{S[i / 4][i % 4 * 4], S[i / 4][i % 4 * 4 + 1], S[i / 4][i % 4 * 4 + 2], S[i / 4][i % 4 * 4 + 3]};
-  } else if (kept && last == s.n) {
+      for (int a = 0; a < NA; ++a)
 #pragma unroll
-    for (int a = 0; a < NA; ++a)
-#pragma unroll
-      for (int r = 0; r < 16; ++r) state[(32 * a + 8 * (r / 4) + 4 * g + r % 4) * D] = S[a][r];
+        for (int r = 0; r < 16; ++r)
+          __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(S[a][r]), state, in_state, row_of(a, r), 0);
+    }
+    if (!OUT) break;
+    ++b, at = 0;
   }
+  if (!OUT && h == 0 && !half && threadIdx.x == 0) p.goes_on[run] = goes_on;
 }
 
-// The state that each segment of a sequence begins with, from what those before
-// it add: four numbers a thread.
+// The states that runs begin with, from what the runs before them add: four
+// numbers a thread.
 template <int D>
 __global__ __launch_bounds__(256) void k_decay_join(DecayArgs p) {
-  constexpr int kParts = D * D / 4 / 256;  // workgroups of a sequence and head
-  const int part = blockIdx.x % kParts, h = blockIdx.x / kParts % p.states.heads, b = blockIdx.x / kParts / p.states.heads;
-  const Seq s = sequence(p.batch, b);
-  if (s.n <= 0) return;
-  const int slot = p.slot[b], lane = __lane_id();
-  const int at = (part * 256 + threadIdx.x) / kWave, wave = at / (D / 8), i = at % (D / 8);  // in the accumulators' order
-  f32x4 S = {};
-  if (uint32_t(slot) < uint32_t(p.states.slots) && s.place0 > 0) {
-    const float* state = p.states.state + (int64_t(slot) * p.states.heads + h) * (D * D) + wave * 32 + (lane & 31);
-#pragma unroll
-    for (int e = 0; e < 4; ++e) S[e] = state[(32 * (i / 4) + 8 * (i % 4) + 4 * (lane >> 5) + e) * D];
-  }
-  const float fade = power(float(p.segment) * log2_decay(p, h));
-  const int segs = (s.n + p.segment - 1) / p.segment;
-  f32x4* to = begins<D>(p, b, 0, h, wave) + i * kWave;
+  constexpr int kParts = D * D / 4 / 256;  // workgroups of a head
+  const int part = blockIdx.x % kParts, h = blockIdx.x / kParts;
+  const float fade = log2_decay(p, h) * kChunk;
+  f32x4* to = reinterpret_cast<f32x4*>(stored(p, kBegins, 1, h)) + part * 256 + threadIdx.x;
+  const f32x4* half = reinterpret_cast<const f32x4*>(stored(p, kHalf, 0, h)) + part * 256 + threadIdx.x;
   const int64_t next = int64_t(p.states.heads) * (D * D / 4);
-  for (int j = 0; j < segs; ++j, to += next) {
-    if (j > 0) {
-      const f32x4 x = *to;
+  f32x4 S = {};
+  constexpr int kAtOnce = 8;  // runs whose sums are asked for together
+  for (int run = 0; run + 1 < p.runs; run += kAtOnce, to += kAtOnce * next, half += kAtOnce * next) {
+    f32x4 x[kAtOnce], y[kAtOnce];
 #pragma unroll
-      for (int e = 0; e < 4; ++e) S[e] = fmaf(S[e], fade, x[e]);
+    for (int i = 0; i < kAtOnce; ++i)
+      if (run + i + 1 < p.runs) x[i] = half[i * next], y[i] = to[i * next];  // (whatever is there, if there is none)
+#pragma unroll
+    for (int i = 0; i < kAtOnce; ++i) {
+      const int chunks = run + i + 1 < p.runs ? p.goes_on[run + i] : 0, n = abs(chunks);
+      if (chunks == 0) continue;
+      // (a sequence that begins in the run has what it began with in its first half)
+      const float f = exp2f(float(n / 2) * fade), f2 = exp2f(float(n - n / 2) * fade);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) S[e] = fmaf(chunks < 0 ? x[i][e] : fmaf(S[e], f, x[i][e]), f2, y[i][e]);
+      to[i * next] = S;
     }
-    *to = S;
   }
 }
 
 template <int D>
 hipError_t prompt(const DecayArgs& p, hipStream_t s) {
-  const uint32_t pairs = uint32_t(p.batch.batch) * p.states.heads;
-  if (p.segments > 1) {
-    hipLaunchKernelGGL((k_decay_prompt<D, false>), dim3(pairs * (p.segments - 1)), dim3(2 * D), 0, s, p);
-    hipLaunchKernelGGL((k_decay_join<D>), dim3(pairs * (D * D / 1024)), dim3(256), 0, s, p);
+  auto grid = [&](int runs) {  // (whole turns of the XCDs, each of heads that share a key head)
+    return dim3((uint32_t(runs) * (p.states.heads / p.group) + kXcds - 1) / kXcds * kXcds * p.group);
+  };
+  if (p.runs > 1) {
+    hipLaunchKernelGGL((k_decay_prompt<D, false>), grid(2 * p.runs), dim3(2 * D), 0, s, p);
+    hipLaunchKernelGGL((k_decay_join<D>), dim3(p.states.heads * (D * D / 1024)), dim3(256), 0, s, p);
   }
-  hipLaunchKernelGGL((k_decay_prompt<D, true>), dim3(pairs * p.segments), dim3(2 * D), 0, s, p);
+  hipLaunchKernelGGL((k_decay_prompt<D, true>), grid(p.runs ? p.runs : p.batch.batch), dim3(2 * D), 0, s, p);
   return hipGetLastError();
 }
 
 }  // namespace
 
-// A workgroup to a sequence and head, or to a segment of it where those are fewer
-// than the CUs hold.
+// Token after token up to 8 of a sequence: 5 and 16 tokens (28 heads of 128 elements) 6.5
+// and 14.9 us, in a chunk 8.9; of 64 sequences 42 and 70, in chunks 52 and 54.
+//
+// Then a workgroup to a sequence and head, or to a run of chunks of all sequences.
+// What a chunk takes was measured (us): 5.4 where a CU has one workgroup, 8.4 where
+// it has two.  Runs cost two more launches, the join of what they begin with, and
+// the keys' and values' chunks of every sequence that goes on in another run a second
+// time (0.4 of a chunk).  A sequence and head each (16 x 600 tokens, 28 heads: 95 us,
+// in runs 139; 8 x 200: 27 and 54) waits for the longest (a prompt of 9459: 650
+// and 134; eight of 3531 to 9459: 740 and 579).
 DecayPlan decay_plan(const wz_states& z, const wz_ragged& r) {
   DecayPlan p{};
-  p.token = r.max_tokens <= 16;
-  p.segments = 1, p.segment = r.max_tokens;
+  p.token = r.max_tokens <= 8;
   if (p.token) return p;
-  const int64_t pairs = int64_t(r.batch) * z.heads, room = 2 * kCUs;
-  const int chunks = (r.max_tokens + kChunk - 1) / kChunk;
-  const int64_t want = std::min<int64_t>(room / pairs, chunks / 2);
-  if (want > 1) {
-    p.segment = int((chunks + want - 1) / want) * kChunk;
-    p.segments = (r.max_tokens + p.segment - 1) / p.segment;
+  const double most = (r.max_tokens + kChunk - 1) / kChunk;
+  // chunks of all sequences at most
+  const double all = std::min(r.batch * most, double(r.tokens / kChunk + r.batch));
+  double best = 5 + std::max(most * 4.9, all * z.heads / kCUs * 3.9);
+  int most_runs = std::min(2 * kCUs / z.heads, int(all / 2));
+  for (int i = 0; i < 4 && most_runs > 1; ++i, most_runs /= 2) {
+    const double each = std::ceil(all / most_runs), again = std::max(0., 1 - each * r.batch / (2 * all));
+    const int runs = int(std::ceil(all / each));
+    const double time = 17 + 0.15 * runs + each * (runs * z.heads > kCUs ? 8.4 : 5.4) * (1 + 0.4 * again);
+    if (time < best) best = time, p.runs = runs;
   }
-  if (p.segments > 1) p.bytes = size_t(pairs) * p.segments * z.head_dim * z.head_dim * 4;
+  if (p.runs == 0) return p;
+  p.state_bytes = size_t(3) * p.runs * z.heads * z.head_dim * z.head_dim * 4;
+  p.bytes = p.state_bytes + (size_t(p.runs) * 4 + 255) / 256 * 256;
   return p;
 }
 

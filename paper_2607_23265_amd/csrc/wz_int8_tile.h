@@ -229,14 +229,16 @@ __global__ __launch_bounds__(WM* WN* KS* kWave) void k_matmul_tile(MatmulArgs p,
   // them 16 bytes a lane, whole lines of the result (or halves or quarters).
   constexpr int kWaveCols = EPI == kGated ? BN / WN / 2 : BN / WN;
   constexpr int kMostBytes = kWaveCols * int(sizeof(Out));
-  constexpr int kUnitBytes = kWaves * 32 * 128 <= (BM + BN) * KB && kMostBytes >= 128 ? 128 : kMostBytes >= 64 ? 64 : 32;
+  constexpr int kUnitBytes =
+      kWaves * 32 * 128 <= (BM + BN) * KB && kMostBytes >= 128 ? 128 : kMostBytes >= 64 ? 64 : 32;
   constexpr int kUnit = kUnitBytes / sizeof(Out);  // columns of a unit
   constexpr int kUnitChunks = kUnit * sizeof(Out) / 16, kPer = 16 / sizeof(Out);  // 16-byte chunks of a row, elements
   static_assert(kWaves * 32 * kUnit * sizeof(Out) <= (BM + BN) * KB && kWaveCols % kUnit == 0, "");
   Out* const out = static_cast<Out*>(p.out);
   Out* const unit = reinterpret_cast<Out*>(lds) + w * 32 * kUnit;
   auto place = [&](int row, int chunk) {
-    return unit + row * kUnit + kPer * (chunk ^ (kUnitChunks == 8 ? row >> 1 & 7 : kUnitChunks == 4 ? row >> 2 & 3 : row >> 3 & 1));
+    const int x = kUnitChunks == 8 ? row >> 1 & 7 : kUnitChunks == 4 ? row >> 2 & 3 : row >> 3 & 1;
+    return unit + row * kUnit + kPer * (chunk ^ x);
   };
   float* const wsc = reinterpret_cast<float*>(lds + KS * kStage);  // [BN] scales, [BN] biases
   const int mw = m0 + (w / WN) * (BM / WM), nt = (w % WN) * kWaveCols;
@@ -323,7 +325,8 @@ __global__ __launch_bounds__(WM* WN* KS* kWave) void k_matmul_tile(MatmulArgs p,
           Out* const to = place(c, (col + 4 * g) / kPer) + (col + 4 * g) % kPer;
           if constexpr (EPI == kGated) {
             const int j = (u + col) / 16, q = (u + col) % 16 / 8, at = wt + 32 * j + 8 * q + 4 * g;
-            const f32x4 sg = *reinterpret_cast<const f32x4*>(wsc + at), su = *reinterpret_cast<const f32x4*>(wsc + at + 16);
+            const f32x4 sg = *reinterpret_cast<const f32x4*>(wsc + at);
+            const f32x4 su = *reinterpret_cast<const f32x4*>(wsc + at + 16);
             const f32x4 bg = *reinterpret_cast<const f32x4*>(wsc + BN + at);
             const f32x4 bu = *reinterpret_cast<const f32x4*>(wsc + BN + at + 16);
 #pragma unroll
@@ -379,8 +382,8 @@ hipError_t tiles(const MatmulArgs& p, hipStream_t s) {
   const int64_t tm = (p.M + BM - 1) / BM, tn = (weight_rows<EPI>(p) + BN - 1) / BN;
   const int64_t groups = (tm * tn + kXcds - 1) / kXcds * kXcds;
   if (groups > 0x7fffffff) return hipErrorInvalidValue;
-  hipLaunchKernelGGL((k_matmul_tile<Out, BM, BN, WM, WN, ST, KS, EPI>), dim3(uint32_t(groups)), dim3(WM * WN * KS * kWave),
-                     0, s, p, int(tm), int(tn));
+  hipLaunchKernelGGL((k_matmul_tile<Out, BM, BN, WM, WN, ST, KS, EPI>), dim3(uint32_t(groups)),
+                     dim3(WM * WN * KS * kWave), 0, s, p, int(tm), int(tn));
   return hipGetLastError();
 }
 

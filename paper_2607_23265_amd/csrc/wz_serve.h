@@ -157,14 +157,15 @@ struct DecayArgs {
   int64_t q_stride, k_stride, v_stride, out_stride;
   float scale;
   int group;     // heads that share a key head
-  int segments;  // the plan's: of a sequence at most, each of `segment` tokens (a multiple of 64) but its last
-  int segment;
-  float* part;   // segments > 1: [batch][segments][heads][head_dim][head_dim], the state that each begins with
+  int runs;      // the plan's
+  float* part;   // runs > 1: [3][runs][heads][head_dim][head_dim], states
+  int* goes_on;  // runs > 1: [runs] chunks of the run's last sequence, if that goes on in the next run (negative
+                 // where it begins in this one); 0: it does not
 };
 struct DecayPlan {
   bool token;  // token after token; otherwise in chunks
-  int segments, segment;
-  size_t bytes;
+  int runs;    // workgroups that share a head's chunks; 0: one to a sequence and head
+  size_t state_bytes, bytes;
 };
 DecayPlan decay_plan(const wz_states& z, const wz_ragged& r);
 hipError_t launch_decay_token(const DecayArgs& p, hipStream_t s);

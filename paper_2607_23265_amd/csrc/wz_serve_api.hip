@@ -300,15 +300,18 @@ wz_status wz_decay_attention(const wz_states* states, const wz_ragged* batch, co
   WZ_TRY(check_rows(k, k_stride, int64_t(kv_heads) * dim));
   WZ_TRY(check_rows(v, v_stride, int64_t(kv_heads) * dim));
   WZ_TRY(check_rows(out, out_stride, int64_t(heads) * dim));
+  // (64 rows are addressed with 32 bits)
+  if (std::max({q_stride, k_stride, v_stride}) > (1 << 22)) return WZ_ERR_SHAPE;
   if (out == q || out == k || out == v) return WZ_ERR_PARAM;
   DecayArgs p{*states, *batch, slot, log_decay, q, k, v, out, q_stride, k_stride, v_stride, out_stride, scale,
               heads / kv_heads};
   const DecayPlan plan = decay_plan(*states, *batch);
-  p.segments = plan.segments, p.segment = plan.segment;
+  p.runs = plan.runs;
   if (plan.bytes) {
     if (!ws) return WZ_ERR_NULL;
     if (!aligned(ws, 256) || ws_bytes < plan.bytes) return WZ_ERR_WORKSPACE;
     p.part = static_cast<float*>(ws);
+    p.goes_on = reinterpret_cast<int*>(static_cast<char*>(ws) + plan.state_bytes);
   }
   const auto s = static_cast<hipStream_t>(stream);
   return from_hip(plan.token ? launch_decay_token(p, s) : launch_decay_prompt(p, s));

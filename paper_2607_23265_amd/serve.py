@@ -234,9 +234,9 @@ def norm_quantize(x, weight, eps=1e-6, residual=None, total=None, out=None, scal
     return _native.norm_quantize(x, weight, eps, residual, total, out, scale)
 
 
-def decay_workspace_bytes(states, batch):
-    """Bytes of workspace decay_attention() needs."""
-    return _native.decay_workspace(states._c, batch._c)
+def decay_workspace_bytes(states, batch, tokens):
+    """Bytes of workspace decay_attention() needs for `tokens` rows."""
+    return _native.decay_workspace(states._c, batch._c, tokens)
 
 
 def decay_attention(states, batch, slot, q, k, v, log_decay, scale=None, out=None, ws=None):

@@ -220,7 +220,7 @@ def test_runs_agree_bit_for_bit(new, dim):
     want, states = c.run()
     batch = c.batch()
     z = serve.States(torch.from_numpy(c.state).to(DEV))
-    need = serve.decay_workspace_bytes(z, batch)
+    need = serve.decay_workspace_bytes(z, batch, c.q.shape[0])
     ws = torch.full((max(need, 256),), 0xFF, dtype=torch.uint8, device=DEV)
     got, again = c.run(ws=ws)
     assert torch.equal(got, want) and torch.equal(again.state, states.state)
@@ -253,7 +253,7 @@ def test_runs_agree_bit_for_bit(new, dim):
 def test_nothing_behind_the_workspace_is_written():
     c = Layer([1500, 900], [1, 0], 4, 2, 64, seed=6)
     z, batch = serve.States(torch.from_numpy(c.state).to(DEV)), c.batch()
-    need = serve.decay_workspace_bytes(z, batch)
+    need = serve.decay_workspace_bytes(z, batch, c.q.shape[0])
     space = torch.full((need + (1 << 20),), 0x5A, dtype=torch.uint8, device=DEV)
     got, _ = c.run(ws=space[:need] if need else None)
     assert bool((space[need:] == 0x5A).all())
@@ -264,7 +264,7 @@ def test_overlapping_rows_stay_in_the_workspace():
     c = Layer([400, 400], [1, 1], 2, 2, 64, seed=7)
     batch = serve.Ragged(ints([700, -5, 900]), ints([400, 1 << 20]), torch.zeros(2, 0, dtype=torch.int32, device=DEV), 400, 500)
     z = serve.States(torch.from_numpy(c.state).to(DEV))
-    need = serve.decay_workspace_bytes(z, batch)
+    need = serve.decay_workspace_bytes(z, batch, c.q.shape[0])
     space = torch.full((need + (1 << 20),), 0x5A, dtype=torch.uint8, device=DEV)
     c.run(states=z, batch=batch, ws=space[:need] if need else None)
     assert bool((space[need:] == 0x5A).all())
