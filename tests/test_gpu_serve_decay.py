@@ -104,6 +104,17 @@ def test_lengths(new, held, heads, kv, dim):
     c.check(*c.run(), f"{new} {heads}/{kv} x {dim}")
 
 
+@pytest.mark.parametrize("new,held,heads,kv,dim", [
+    # runs of chunks that begin and end inside sequences, at their ends, and over several of them
+    ([300, 0, 64, 1000, 9, 129, 640], [1, 1, 0, 1, 0, 0, 1], 3, 1, 64), ([128] * 9, [0, 1] * 4 + [1], 2, 2, 128),
+    ([1500], [1], 1, 1, 64), ([64, 1200, 64], [1, 1, 1], 2, 2, 64), ([700, 1] * 3, [0] * 6, 40, 20, 64),
+    # the most heads
+    ([3, 1], [1, 0], 256, 64, 64), ([70], [1], 256, 256, 64)])
+def test_runs(new, held, heads, kv, dim):
+    c = Layer(new, held, heads, kv, dim, seed=sum(new) + dim)
+    c.check(*c.run(), f"runs {new} {heads}/{kv} x {dim}")
+
+
 @pytest.mark.parametrize("dim", [64, 128])
 @pytest.mark.parametrize("n", [1, 3, 300])
 def test_decays_at_the_ends(n, dim):
@@ -156,6 +167,15 @@ def test_large_and_small_numbers(n):
     c.k.mul_(2.0 ** 60), c.v.mul_(2.0 ** 30), c.q.mul_(2.0 ** -60)
     c.state *= np.float32(2.0 ** 90)
     c.check(*c.run(), "large keys")
+
+
+@pytest.mark.parametrize("n", [20, 400])
+def test_the_largest_states(n):
+    """A state's elements of 2^110 keep their precision where they are kept raised for some chunks, and fade."""
+    c = Layer([n], [1], 3, 1, 64, seed=n, log_decay=[-0.003, -0.05, -0.6])
+    c.state = np.sign(c.state) * np.float32(2.0 ** 109)
+    c.q.mul_(2.0 ** -60)
+    c.check(*c.run(), f"the largest states, {n}")
 
 
 @pytest.mark.parametrize("new", [[1, 1, 1], [5, 70, 300]])
