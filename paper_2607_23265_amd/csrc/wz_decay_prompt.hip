@@ -58,7 +58,6 @@ __device__ __forceinline__ float* stored(const DecayArgs& p, int kind, int run, 
 }
 constexpr int kBegins = 0;  // what a run's first sequence has before the run, if that goes on from another run
 constexpr int kFirst = 1;   // what a run's last sequence has before the call, if that begins in the run and goes on
-constexpr int kHalf = 2;    // what the first half of a run's last sequence adds, if that goes on
 
 // Chunks from one sequence to the next: a run's are [lo, hi) of all.
 __device__ __forceinline__ int chunks_of(const Seq& s) { return (s.n + kChunk - 1) / kChunk; }
@@ -70,19 +69,28 @@ struct Run {
 template <bool LAST>
 __device__ __forceinline__ Run run_of(const DecayArgs& p, int run) {
   if (p.runs == 0) return Run{run, 0, chunks_of(sequence(p.batch, run))};  // a sequence each
-  int all = 0;
+  const int lane = __lane_id();
+  int all = 0, mine = 0, incl = 0;  // (of 64 sequences at a time: this lane's, and those up to it)
   for (int b = 0; b < p.batch.batch; b += kWave) {
-    const int mine = b + __lane_id();
-    const int n = mine < p.batch.batch ? chunks_of(sequence(p.batch, mine)) : 0;
-    all += __builtin_amdgcn_readlane(wave_incl_scan_i32(n), kWave - 1);
+    mine = b + lane < p.batch.batch ? chunks_of(sequence(p.batch, b + lane)) : 0;
+    incl = wave_incl_scan_i32(mine);
+    all += __builtin_amdgcn_readlane(incl, kWave - 1);
   }
   const int lo = int(int64_t(run) * all / p.runs), hi = int(int64_t(run + 1) * all / p.runs);
   if (lo >= hi) return Run{0, 0, 0};
-  const Found f = find_item(p.batch, LAST ? hi - 1 : lo, [](const Seq& s) { return chunks_of(s); });
-  if (f.seq < 0) return Run{0, 0, 0};  // (rows that overlap against the contract, past 32 bits)
-  if (!LAST) return Run{f.seq, f.local, hi - lo};
-  const int at = max(f.local - (hi - 1 - lo), 0);
-  return Run{f.seq, at, f.local - at + 1};
+  const int item = LAST ? hi - 1 : lo;
+  int seq, at;
+  if (p.batch.batch <= kWave) {
+    seq = __builtin_ctzll(__ballot(incl > item));
+    at = item - __builtin_amdgcn_readlane(incl, seq) + __builtin_amdgcn_readlane(mine, seq);
+  } else {
+    const Found f = find_item(p.batch, item, [](const Seq& s) { return chunks_of(s); });
+    if (f.seq < 0) return Run{0, 0, 0};  // (rows that overlap against the contract, past 32 bits)
+    seq = f.seq, at = f.local;
+  }
+  if (!LAST) return Run{seq, at, hi - lo};
+  const int first = max(at - (hi - 1 - lo), 0);
+  return Run{seq, first, at - first + 1};
 }
 
 // A workgroup goes through a run of chunks.  OUT: outputs, and the sequences' last
@@ -104,10 +112,9 @@ __global__ __launch_bounds__(2 * D, 2) void k_decay_prompt(DecayArgs p) {
   // Workgroups go to the XCDs in turn: heads that share a key head to the same
   // one, whose L2 they read it from.
   const int x = blockIdx.x % kXcds, y = blockIdx.x / kXcds, kv_heads = p.states.heads / p.group;
-  const int runs = p.runs ? p.runs : p.batch.batch, set = y / p.group * kXcds + x, halves = OUT ? 1 : 2;
-  if (set >= runs * kv_heads * halves) return;
-  const int kh = set % kv_heads, h = kh * p.group + y % p.group, run = set / kv_heads / halves;
-  const int half = OUT ? 0 : set / kv_heads % 2;
+  const int runs = p.runs ? p.runs : p.batch.batch, set = y / p.group * kXcds + x;
+  if (set >= runs * kv_heads) return;
+  const int kh = set % kv_heads, h = kh * p.group + y % p.group, run = set / kv_heads;
   const Run all = run_of<!OUT>(p, run);
   int goes_on = 0;
   float ld = log2_decay(p, h);
@@ -185,7 +192,7 @@ __global__ __launch_bounds__(2 * D, 2) void k_decay_prompt(DecayArgs p) {
   int b = all.seq, at = all.at, left = all.chunks;
   while (left > 0 && b < p.batch.batch) {
     s = sequence(p.batch, b);
-    int chunks = min(chunks_of(s) - at, left), first = at * kChunk;
+    const int chunks = min(chunks_of(s) - at, left), first = at * kChunk;
     if (OUT && chunks <= 0) {  // (a sequence without tokens)
       ++b, at = 0;
       continue;
@@ -193,12 +200,7 @@ __global__ __launch_bounds__(2 * D, 2) void k_decay_prompt(DecayArgs p) {
     left -= chunks;
     last = min(s.n, first + chunks * kChunk);
     const bool on = last < s.n;  // in the next run
-    if constexpr (!OUT) {
-      if (!on) break;
-      goes_on = first == 0 ? -chunks : chunks;
-      if (half) first += chunks / 2 * kChunk;
-      else last = first + chunks / 2 * kChunk;
-    }
+    if (!OUT && !on) break;
     const int slot = p.slot[b];
     const bool kept = uint32_t(slot) < uint32_t(p.states.slots);
     const auto state =
@@ -231,7 +233,7 @@ __global__ __launch_bounds__(2 * D, 2) void k_decay_prompt(DecayArgs p) {
       from(stored(p, kBegins, run, h));
     } else if (OUT && on) {
       from(stored(p, kFirst, run, h));
-    } else if (kept && s.place0 > 0 && first == 0 && !half) {
+    } else if (kept && s.place0 > 0 && first == 0) {
 #pragma unroll
       for (int a = 0; a < NA; ++a)
 #pragma unroll
@@ -239,8 +241,8 @@ __global__ __launch_bounds__(2 * D, 2) void k_decay_prompt(DecayArgs p) {
           S[a][r] = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(state, in_state, row_of(a, r), 0));
     }
     // (the run that stores the sequence's last state may do so before another looks at what the slot holds)
-    if (!OUT && goes_on < 0 && !half) into(stored(p, kFirst, run, h));
-    if (first < last) fetch(first);
+    if (!OUT && first == 0) into(stored(p, kFirst, run, h));
+    fetch(first);
     int age = 0;
     for (int t0 = first; t0 < last; t0 += kChunk) {
       const int len = min(kChunk, last - t0);
@@ -422,7 +424,8 @@ __global__ __launch_bounds__(2 * D, 2) void k_decay_prompt(DecayArgs p) {
     }
 
     if constexpr (!OUT) {
-      into(half ? stored(p, kBegins, run + 1, h) : stored(p, kHalf, run, h));
+      into(stored(p, kBegins, run + 1, h));
+      goes_on = first == 0 ? -chunks : chunks;
     } else if (kept && !on) {
 #pragma unroll
       for (int a = 0; a < NA; ++a)
@@ -433,7 +436,7 @@ __global__ __launch_bounds__(2 * D, 2) void k_decay_prompt(DecayArgs p) {
     if (!OUT) break;
     ++b, at = 0;
   }
-  if (!OUT && h == 0 && !half && threadIdx.x == 0) p.goes_on[run] = goes_on;
+  if (!OUT && h == 0 && threadIdx.x == 0) p.goes_on[run] = goes_on;
 }
 
 // The states that runs begin with, from what the runs before them add: four
@@ -444,24 +447,24 @@ __global__ __launch_bounds__(256) void k_decay_join(DecayArgs p) {
   const int part = blockIdx.x % kParts, h = blockIdx.x / kParts;
   const float fade = log2_decay(p, h) * kChunk;
   f32x4* to = reinterpret_cast<f32x4*>(stored(p, kBegins, 1, h)) + part * 256 + threadIdx.x;
-  const f32x4* half = reinterpret_cast<const f32x4*>(stored(p, kHalf, 0, h)) + part * 256 + threadIdx.x;
   const int64_t next = int64_t(p.states.heads) * (D * D / 4);
   f32x4 S = {};
   constexpr int kAtOnce = 8;  // runs whose sums are asked for together
-  for (int run = 0; run + 1 < p.runs; run += kAtOnce, to += kAtOnce * next, half += kAtOnce * next) {
-    f32x4 x[kAtOnce], y[kAtOnce];
+  for (int run = 0; run + 1 < p.runs; run += kAtOnce, to += kAtOnce * next) {
+    f32x4 x[kAtOnce];
 #pragma unroll
     for (int i = 0; i < kAtOnce; ++i)
-      if (run + i + 1 < p.runs) x[i] = half[i * next], y[i] = to[i * next];  // (whatever is there, if there is none)
+      if (run + i + 1 < p.runs) x[i] = to[i * next];  // (whatever is there, if there is none)
 #pragma unroll
     for (int i = 0; i < kAtOnce; ++i) {
-      const int chunks = run + i + 1 < p.runs ? p.goes_on[run + i] : 0, n = abs(chunks);
-      if (chunks == 0) continue;
-      // (a sequence that begins in the run has what it began with in its first half)
-      const float f = exp2f(float(n / 2) * fade), f2 = exp2f(float(n - n / 2) * fade);
+      const int chunks = run + i + 1 < p.runs ? p.goes_on[run + i] : 0;
+      if (chunks > 0) {  // (a sequence that begins in the run has what it began with in the sum)
+        const float f = exp2f(float(chunks) * fade);
 #pragma unroll
-      for (int e = 0; e < 4; ++e) S[e] = fmaf(chunks < 0 ? x[i][e] : fmaf(S[e], f, x[i][e]), f2, y[i][e]);
-      to[i * next] = S;
+        for (int e = 0; e < 4; ++e) x[i][e] = fmaf(S[e], f, x[i][e]);
+        to[i * next] = x[i];
+      }
+      S = x[i];
     }
   }
 }
@@ -472,7 +475,7 @@ hipError_t prompt(const DecayArgs& p, hipStream_t s) {
     return dim3((uint32_t(runs) * (p.states.heads / p.group) + kXcds - 1) / kXcds * kXcds * p.group);
   };
   if (p.runs > 1) {
-    hipLaunchKernelGGL((k_decay_prompt<D, false>), grid(2 * p.runs), dim3(2 * D), 0, s, p);
+    hipLaunchKernelGGL((k_decay_prompt<D, false>), grid(p.runs), dim3(2 * D), 0, s, p);
     hipLaunchKernelGGL((k_decay_join<D>), dim3(p.states.heads * (D * D / 1024)), dim3(256), 0, s, p);
   }
   hipLaunchKernelGGL((k_decay_prompt<D, true>), grid(p.runs ? p.runs : p.batch.batch), dim3(2 * D), 0, s, p);
@@ -486,11 +489,12 @@ hipError_t prompt(const DecayArgs& p, hipStream_t s) {
 //
 // Then a workgroup to a sequence and head, or to a run of chunks of all sequences.
 // What a chunk takes was measured (us): 5.4 where a CU has one workgroup, 8.4 where
-// it has two.  Runs cost two more launches, the join of what they begin with, and
-// the keys' and values' chunks of every sequence that goes on in another run a second
-// time (0.4 of a chunk).  A sequence and head each (16 x 600 tokens, 28 heads: 95 us,
-// in runs 139; 8 x 200: 27 and 54) waits for the longest (a prompt of 9459: 650
-// and 134; eight of 3531 to 9459: 740 and 579).
+// it has two.  Runs cost two more launches, the states that they begin with (64 KiB
+// a run and head, four times), and the keys' and values' chunks of every sequence that
+// goes on in another run a second time (0.4 of a chunk).  Measured on the side that
+// the rule takes and on the other (28 heads of 128 elements): 200 tokens 22 and 26 us,
+// 8 x 200 27 and 54, 16 x 600 87 and 142, 8 x 6562 506 and 560; in runs, 1286 tokens
+// 43 and 105, 9459 126 and 650, eight sequences of 3531 to 9459 570 and 740.
 DecayPlan decay_plan(const wz_states& z, const wz_ragged& r) {
   DecayPlan p{};
   p.token = r.max_tokens <= 8;
@@ -507,7 +511,7 @@ DecayPlan decay_plan(const wz_states& z, const wz_ragged& r) {
     if (time < best) best = time, p.runs = runs;
   }
   if (p.runs == 0) return p;
-  p.state_bytes = size_t(3) * p.runs * z.heads * z.head_dim * z.head_dim * 4;
+  p.state_bytes = size_t(2) * p.runs * z.heads * z.head_dim * z.head_dim * 4;
   p.bytes = p.state_bytes + (size_t(p.runs) * 4 + 255) / 256 * 256;
   return p;
 }
