@@ -76,8 +76,11 @@ __device__ __forceinline__ Run run_of(const DecayArgs& p, int run) {
     incl = wave_incl_scan_i32(mine);
     all += __builtin_amdgcn_readlane(incl, kWave - 1);
   }
-  const int lo = int(int64_t(run) * all / p.runs), hi = int(int64_t(run + 1) * all / p.runs);
-  if (lo >= hi) return Run{0, 0, 0};
+  // (fewer chunks than the bounds promise: a run each, and none behind, since what a sequence has before a run is
+  // handed on by the run before it)
+  const int runs = min(p.runs, all);
+  if (run >= runs) return Run{0, 0, 0};
+  const int lo = int(int64_t(run) * all / runs), hi = int(int64_t(run + 1) * all / runs);
   const int item = LAST ? hi - 1 : lo;
   int seq, at;
   if (p.batch.batch <= kWave) {
@@ -336,8 +339,7 @@ __global__ __launch_bounds__(2 * D, 2) void k_decay_prompt(DecayArgs p) {
 #pragma unroll
         for (int k = 0; k < 4; ++k)
 #pragma unroll
-          for (int e = 0; e < 4; ++e)
-            none = dot2(vf[k][e], zero, none);
+          for (int e = 0; e < 4; ++e) none = dot2(vf[k][e], zero, none);
         const bool odd = __ballot(none != 0.f) != 0;
         if (odd) {
           int token = kChunk;
@@ -410,7 +412,6 @@ __global__ __launch_bounds__(2 * D, 2) void k_decay_prompt(DecayArgs p) {
         for (int i = 0; i < 3; ++i)
 #pragma unroll
           for (int a = 0; a < NA; ++a) S[a] = mfma(kf[a], part[i], S[a]);
-        
       }
       lds_barrier();
       age = from_age + len;

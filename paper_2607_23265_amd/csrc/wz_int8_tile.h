@@ -37,7 +37,8 @@ struct ActLinear {
 struct ActSigmoid {
   float c1, c3;  // of -z log2(e)
   __device__ __forceinline__ float operator()(float x) const {
-    return x * __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(x * fmaf(c3 * x, x, c1)));
+    // (an infinite square times silu's c3 of zero would be no number)
+    return x * __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(x * fmaf(c3, fminf(x * x, 1e30f), c1)));
   }
 };
 // x (1 + erf(x / sqrt 2)) / 2 = max(x, 0) - |x| erfc(|x| / sqrt 2) / 2, with erfc(y) =

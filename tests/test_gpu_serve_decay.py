@@ -233,6 +233,19 @@ def test_bounds_above_the_lengths_and_below():
     assert (got[3:5] == 9).all() and (got[8:25] == 9).all()
 
 
+@pytest.mark.parametrize("new", [[200], [129, 0, 65], [63], [0, 0, 0], [64, 320] + [0] * 70 + [130]])
+@pytest.mark.parametrize("dim", [64, 128])
+def test_fewer_tokens_than_rows(new, dim):
+    """A padded batch: rows, and max_tokens, far above what the sequences bring, so that the plan has more runs than
+    there are chunks."""
+    c = Layer(new, [1, 0, 1] if len(new) == 3 else [1] * len(new), 4, 2, dim, seed=sum(new), behind=6000)
+    z = serve.States(torch.from_numpy(c.state).to(DEV))
+    for most in (6000, 330):
+        batch = c.batch(most)
+        ws = torch.full((serve.decay_workspace_bytes(z, batch, c.q.shape[0]) + 256,), 0xFF, dtype=torch.uint8, device=DEV)
+        c.check(*c.run(batch=batch, ws=ws), f"{new} of 6000, {most} at most")
+
+
 @pytest.mark.parametrize("new,dim", [([1] * 5, 128), ([900, 40], 64), ([2000], 128)])
 def test_runs_agree_bit_for_bit(new, dim):
     """The same call again, with whatever lies in its workspace, on a stream of its own, and captured and replayed."""

@@ -167,6 +167,18 @@ def test_numbers_at_the_ends():
         assert torch.equal(y[[0, 2]], x[[0, 2]]) and not y[[1, 3, 5]].any() and torch.isnan(y[4]).all(), act
 
 
+def test_infinite_sums():
+    """Infinities go through an activation as through its formula: the upper one stays."""
+    inf = float("inf")
+    a, w = torch.ones(2, 16, dtype=torch.int8, device=DEV), torch.ones(40, 16, dtype=torch.int8, device=DEV)
+    one, bias = torch.ones(2, device=DEV), torch.zeros(40, device=DEV)
+    bias[3] = inf
+    for act in (None, "relu", "silu", "gelu", "gelu_tanh"):
+        y = serve.matmul_int(a, one, w, torch.ones(40, device=DEV), bias, out_dtype=F32, activation=act)
+        torch.cuda.synchronize()
+        assert (y[:, 3] == inf).all() and torch.isfinite(y[:, :3]).all() and torch.isfinite(y[:, 4:]).all(), act
+
+
 def test_no_rows():
     a, s = torch.empty(0, 64, dtype=torch.int8, device=DEV), torch.empty(0, device=DEV)
     w, sw = torch.zeros(5, 64, dtype=torch.int8, device=DEV), torch.ones(5, device=DEV)
