@@ -56,7 +56,8 @@ __device__ __forceinline__ float power(float x) { return __builtin_amdgcn_exp2f(
 __device__ __forceinline__ float* stored(const DecayArgs& p, int kind, int run, int h) {
   return p.part + ((int64_t(kind) * p.runs + run) * p.states.heads + h) * (p.states.head_dim * p.states.head_dim);
 }
-constexpr int kBegins = 0;  // what a run's first sequence has before the run, if that goes on from another run
+constexpr int kBegins = 0;  // of a run's first sequence, if that goes on from another run: what the run before this
+                            // one adds (to zeros, or to kFirst), and then, if the sums are joined, what it begins with
 constexpr int kFirst = 1;   // what a run's last sequence has before the call, if that begins in the run and goes on
 
 // Chunks from one sequence to the next: a run's are [lo, hi) of all.
@@ -64,11 +65,17 @@ __device__ __forceinline__ int chunks_of(const Seq& s) { return (s.n + kChunk - 
 struct Run {
   int seq, at;  // its first chunk's sequence, and the chunk's number there
   int chunks;
+  int all, runs;  // of the call: chunks, and runs that have any
 };
+// The first of `all` chunks that a run has: the first runs have one more than the others.
+__device__ __forceinline__ int first_of(int run, int all, int runs) {
+  const int each = uint32_t(all) / uint32_t(runs);
+  return run * each + min(run, all - each * runs);
+}
 // LAST: of the run, what belongs to its last sequence.
 template <bool LAST>
 __device__ __forceinline__ Run run_of(const DecayArgs& p, int run) {
-  if (p.runs == 0) return Run{run, 0, chunks_of(sequence(p.batch, run))};  // a sequence each
+  if (p.runs == 0) return Run{run, 0, chunks_of(sequence(p.batch, run)), 0, 0};  // a sequence each
   const int lane = __lane_id();
   int all = 0, mine = 0, incl = 0;  // (of 64 sequences at a time: this lane's, and those up to it)
   for (int b = 0; b < p.batch.batch; b += kWave) {
@@ -79,8 +86,8 @@ __device__ __forceinline__ Run run_of(const DecayArgs& p, int run) {
   // (fewer chunks than the bounds promise: a run each, and none behind, since what a sequence has before a run is
   // handed on by the run before it)
   const int runs = min(p.runs, all);
-  if (run >= runs) return Run{0, 0, 0};
-  const int lo = int(int64_t(run) * all / runs), hi = int(int64_t(run + 1) * all / runs);
+  if (run >= runs) return Run{};
+  const int lo = first_of(run, all, runs), hi = first_of(run + 1, all, runs);
   const int item = LAST ? hi - 1 : lo;
   int seq, at;
   if (p.batch.batch <= kWave) {
@@ -88,12 +95,12 @@ __device__ __forceinline__ Run run_of(const DecayArgs& p, int run) {
     at = item - __builtin_amdgcn_readlane(incl, seq) + __builtin_amdgcn_readlane(mine, seq);
   } else {
     const Found f = find_item(p.batch, item, [](const Seq& s) { return chunks_of(s); });
-    if (f.seq < 0) return Run{0, 0, 0};  // (rows that overlap against the contract, past 32 bits)
+    if (f.seq < 0) return Run{};  // (rows that overlap against the contract, past 32 bits)
     seq = f.seq, at = f.local;
   }
-  if (!LAST) return Run{seq, at, hi - lo};
+  if (!LAST) return Run{seq, at, hi - lo, all, runs};
   const int first = max(at - (hi - 1 - lo), 0);
-  return Run{seq, first, at - first + 1};
+  return Run{seq, first, at - first + 1, all, runs};
 }
 
 // A workgroup goes through a run of chunks.  OUT: outputs, and the sequences' last
@@ -213,15 +220,16 @@ __global__ __launch_bounds__(2 * D, 2) void k_decay_prompt(DecayArgs p) {
     int in_state = 4 * (4 * g * D + wave * 32 + c), in_order = 16 * (wave * NA * 4 * kWave + lane);
     asm volatile("" : "+v"(in_state), "+v"(in_order));
     f32x16 S[NA] = {};
-    auto from = [&](const float* base) {
+    auto from = [&](const float* base, float f) {  // (added)
       const auto r = make_rsrc_uniform(base, D * D * 4);
+      f32x4 v[NA * 4];
 #pragma unroll
-      for (int i = 0; i < NA * 4; ++i) {
-        const f32x4 v =
-            __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(r, in_order, i * 16 * kWave, 0));
+      for (int i = 0; i < NA * 4; ++i)
+        v[i] = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(r, in_order, i * 16 * kWave, 0));
 #pragma unroll
-        for (int e = 0; e < 4; ++e) S[i / 4][i % 4 * 4 + e] = v[e];
-      }
+      for (int i = 0; i < NA * 4; ++i)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) S[i / 4][i % 4 * 4 + e] = fmaf(v[i][e], f, S[i / 4][i % 4 * 4 + e]);
     };
     auto into = [&](float* base) {
       const auto r = make_rsrc_uniform(base, D * D * 4);
@@ -232,10 +240,17 @@ __global__ __launch_bounds__(2 * D, 2) void k_decay_prompt(DecayArgs p) {
         __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, v), r, in_order, i * 16 * kWave, 0);
       }
     };
-    if (OUT && first > 0) {
-      from(stored(p, kBegins, run, h));
+    if (OUT && first > 0 && !p.join) {
+      const int here = first_of(run, all.all, all.runs), begins = here - first / kChunk;
+      for (int r = run; r > 0; --r) {
+        const int before = first_of(r, all.all, all.runs);
+        if (before <= begins) break;
+        from(stored(p, kBegins, r, h), power(float((here - before) * kChunk) * ld));
+      }
+    } else if (OUT && first > 0) {
+      from(stored(p, kBegins, run, h), 1.f);
     } else if (OUT && on) {
-      from(stored(p, kFirst, run, h));
+      from(stored(p, kFirst, run, h), 1.f);
     } else if (kept && s.place0 > 0 && first == 0) {
 #pragma unroll
       for (int a = 0; a < NA; ++a)
@@ -477,7 +492,7 @@ hipError_t prompt(const DecayArgs& p, hipStream_t s) {
   };
   if (p.runs > 1) {
     hipLaunchKernelGGL((k_decay_prompt<D, false>), grid(p.runs), dim3(2 * D), 0, s, p);
-    hipLaunchKernelGGL((k_decay_join<D>), dim3(p.states.heads * (D * D / 1024)), dim3(256), 0, s, p);
+    if (p.join) hipLaunchKernelGGL((k_decay_join<D>), dim3(p.states.heads * (D * D / 1024)), dim3(256), 0, s, p);
   }
   hipLaunchKernelGGL((k_decay_prompt<D, true>), grid(p.runs ? p.runs : p.batch.batch), dim3(2 * D), 0, s, p);
   return hipGetLastError();
@@ -508,8 +523,11 @@ DecayPlan decay_plan(const wz_states& z, const wz_ragged& r) {
   for (int i = 0; i < 4 && most_runs > 1; ++i, most_runs /= 2) {
     const double each = std::ceil(all / most_runs), again = std::max(0., 1 - each * r.batch / (2 * all));
     const int runs = int(std::ceil(all / each));
-    const double time = 17 + 0.15 * runs + each * (runs * z.heads > kCUs ? 8.4 : 5.4) * (1 + 0.4 * again);
-    if (time < best) best = time, p.runs = runs;
+    const bool two = runs * z.heads > kCUs;
+    const double chunks = each * (two ? 8.4 : 5.4) * (1 + 0.4 * again);
+    const double join = 6 + 0.2 * runs, adds = (two ? 0.9 : 0.5) * std::min(std::ceil(most / each), runs - 1.);
+    const double time = 12.5 + std::min(join, adds) + chunks;
+    if (time < best) best = time, p.runs = runs, p.join = join < adds;
   }
   if (p.runs == 0) return p;
   p.state_bytes = size_t(2) * p.runs * z.heads * z.head_dim * z.head_dim * 4;

@@ -158,6 +158,7 @@ struct DecayArgs {
   float scale;
   int group;     // heads that share a key head
   int runs;      // the plan's
+  bool join;
   float* part;   // runs > 1: [2][runs][heads][head_dim][head_dim], states
   int* goes_on;  // runs > 1: [runs] chunks of the run's last sequence, if that goes on in the next run (negative
                  // where it begins in this one); 0: it does not
@@ -165,6 +166,7 @@ struct DecayArgs {
 struct DecayPlan {
   bool token;  // token after token; otherwise in chunks
   int runs;    // workgroups that share a head's chunks; 0: one to a sequence and head
+  bool join;   // a launch of its own adds up what runs begin with; otherwise each run does
   size_t state_bytes, bytes;
 };
 DecayPlan decay_plan(const wz_states& z, const wz_ragged& r);

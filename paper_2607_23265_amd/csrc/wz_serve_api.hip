@@ -306,7 +306,7 @@ wz_status wz_decay_attention(const wz_states* states, const wz_ragged* batch, co
   DecayArgs p{*states, *batch, slot, log_decay, q, k, v, out, q_stride, k_stride, v_stride, out_stride, scale,
               heads / kv_heads};
   const DecayPlan plan = decay_plan(*states, *batch);
-  p.runs = plan.runs;
+  p.runs = plan.runs, p.join = plan.join;
   if (plan.bytes) {
     if (!ws) return WZ_ERR_NULL;
     if (!aligned(ws, 256) || ws_bytes < plan.bytes) return WZ_ERR_WORKSPACE;

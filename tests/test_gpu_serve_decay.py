@@ -107,7 +107,7 @@ def test_lengths(new, held, heads, kv, dim):
 @pytest.mark.parametrize("new,held,heads,kv,dim", [
     # runs of chunks that begin and end inside sequences, at their ends, and over several of them
     ([300, 0, 64, 1000, 9, 129, 640], [1, 1, 0, 1, 0, 0, 1], 3, 1, 64), ([128] * 9, [0, 1] * 4 + [1], 2, 2, 128),
-    ([1500], [1], 1, 1, 64), ([64, 1200, 64], [1, 1, 1], 2, 2, 64), ([700, 1] * 3, [0] * 6, 40, 20, 64),
+    ([1500], [1], 1, 1, 64), ([4000], [1], 1, 1, 64), ([3000, 9, 2500], [1, 0, 1], 2, 1, 128), ([64, 1200, 64], [1, 1, 1], 2, 2, 64), ([700, 1] * 3, [0] * 6, 40, 20, 64),
     # the most heads
     ([3, 1], [1, 0], 256, 64, 64), ([70], [1], 256, 256, 64)])
 def test_runs(new, held, heads, kv, dim):
@@ -246,7 +246,7 @@ def test_fewer_tokens_than_rows(new, dim):
         c.check(*c.run(batch=batch, ws=ws), f"{new} of 6000, {most} at most")
 
 
-@pytest.mark.parametrize("new,dim", [([1] * 5, 128), ([900, 40], 64), ([2000], 128)])
+@pytest.mark.parametrize("new,dim", [([1] * 5, 128), ([900, 40], 64), ([2000], 128), ([5000], 64)])
 def test_runs_agree_bit_for_bit(new, dim):
     """The same call again, with whatever lies in its workspace, on a stream of its own, and captured and replayed."""
     c = Layer(new, [1] * len(new), 3, 1, dim, seed=5)
