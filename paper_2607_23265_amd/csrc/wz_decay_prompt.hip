@@ -504,13 +504,21 @@ hipError_t prompt(const DecayArgs& p, hipStream_t s) {
 // and 14.9 us, in a chunk 8.9; of 64 sequences 42 and 70, in chunks 52 and 54.
 //
 // Then a workgroup to a sequence and head, or to a run of chunks of all sequences.
-// What a chunk takes was measured (us): 5.4 where a CU has one workgroup, 8.4 where
-// it has two.  Runs cost two more launches, the states that they begin with (64 KiB
-// a run and head, four times), and the keys' and values' chunks of every sequence that
-// goes on in another run a second time (0.4 of a chunk).  Measured on the side that
-// the rule takes and on the other (28 heads of 128 elements): 200 tokens 22 and 26 us,
-// 8 x 200 27 and 54, 16 x 600 87 and 142, 8 x 6562 506 and 560; in runs, 1286 tokens
-// 43 and 105, 9459 126 and 650, eight sequences of 3531 to 9459 570 and 740.
+// What a chunk takes was measured (us), where a CU has one workgroup, two or three:
+// 5.4 and 8.4 with heads of 128 elements (more do not fit), 3.3, 4.5 and 5.3 with 64.
+// Runs cost another launch, the states that go from run to run (64 or 16 KiB a run
+// and head, three times), and the keys' and values' chunks of every sequence that goes
+// on in another run a second time (0.4 of a chunk).  The states that runs begin with are
+// sums over the runs before: each run adds up its own (64 KiB of every run before it,
+// 0.5 us where a CU has one workgroup, 0.9 with two), or, where those are many, a
+// launch between the two does.  Measured on the side that the rule takes and on the other
+// (28 heads of 128 elements): whole or in runs, 200 tokens 22 and 23 us, 8 x 200 27 and
+// 43, 16 x 600 88 and 127, 8 x 6562 505 and 555; in runs or whole, 1286 tokens 38.5
+// and 96, four of 2000 101 and 148, 9459 125 and 661, eight of 3531 to 9459 556
+// and 678; sums of their own or joined, 1286 tokens 38.5 and 42.6, eight of 3531 to
+// 9459 556 and 565; joined or not, 9459 tokens 125 and 134, 16384 of 2 heads 62 and 127.  With heads
+// of 64 elements, whole or in runs: 64 x 600 154 and 171; in runs or whole: 1286
+// tokens 23.5 and 69, 8 x 3000 113 and 152.
 DecayPlan decay_plan(const wz_states& z, const wz_ragged& r) {
   DecayPlan p{};
   p.token = r.max_tokens <= 8;
@@ -518,15 +526,25 @@ DecayPlan decay_plan(const wz_states& z, const wz_ragged& r) {
   const double most = (r.max_tokens + kChunk - 1) / kChunk;
   // chunks of all sequences at most
   const double all = std::min(r.batch * most, double(r.tokens / kChunk + r.batch));
-  double best = 5 + std::max(most * 4.9, all * z.heads / kCUs * 3.9);
-  int most_runs = std::min(2 * kCUs / z.heads, int(all / 2));
-  for (int i = 0; i < 4 && most_runs > 1; ++i, most_runs /= 2) {
+  struct Times {
+    double alone, full;     // a chunk: of a CU's only workgroup; a CU's time for one, with as many as fit
+    int at_once;            // workgroups of a CU
+    double chunk[4];        // a chunk with 1, 2, ... of them
+    double adds[4];         // what one run before adds, with 1, 2, ...
+    double join, join_run;  // a launch that adds up; for each run
+  };
+  static constexpr Times k128{4.9, 3.9, 2, {0, 5.4, 8.4}, {0, 0.5, 0.9}, 6, 0.2};
+  static constexpr Times k64{3.15, 2.2, 3, {0, 3.3, 4.5, 5.3}, {0, 0.25, 0.35, 0.4}, 6, 0.1};
+  const Times& x = z.head_dim == 128 ? k128 : k64;
+  double best = 5 + std::max(most * x.alone, all * z.heads / kCUs * x.full);
+  for (int n = x.at_once; n >= 0; --n) {  // (0: on half of the CUs)
+    const int most_runs = std::min((n ? n * kCUs : kCUs / 2) / z.heads, int(all / 2));
+    if (most_runs < 2) continue;
     const double each = std::ceil(all / most_runs), again = std::max(0., 1 - each * r.batch / (2 * all));
-    const int runs = int(std::ceil(all / each));
-    const bool two = runs * z.heads > kCUs;
-    const double chunks = each * (two ? 8.4 : 5.4) * (1 + 0.4 * again);
-    const double join = 6 + 0.2 * runs, adds = (two ? 0.9 : 0.5) * std::min(std::ceil(most / each), runs - 1.);
-    const double time = 12.5 + std::min(join, adds) + chunks;
+    const int runs = int(std::ceil(all / each)), there = (runs * z.heads + kCUs - 1) / kCUs;
+    const double join = x.join + x.join_run * runs, adds = x.adds[there] * std::min(std::ceil(most / each), runs - 1.);
+    const double next = 8 * each * r.batch / all;  // from one sequence to the next
+    const double time = 12.5 + std::min(join, adds) + each * x.chunk[there] * (1 + 0.4 * again) + next;
     if (time < best) best = time, p.runs = runs, p.join = join < adds;
   }
   if (p.runs == 0) return p;
