@@ -272,8 +272,8 @@ typedef struct {
 } wz_states;
 
 /* Bytes of workspace wz_decay_attention needs (0 if the arguments are invalid or
- * none is needed), at most 128 MiB: what parts of long sequences add to their
- * states.  Depends on batch, tokens, max_tokens, heads and head_dim alone. */
+ * none is needed), at most 65 MiB: what parts of long sequences add to their
+ * states.  Depends on batch, tokens, max_tokens, heads and head_dim alone.   */
 size_t wz_decay_workspace_bytes(const wz_states* states, const wz_ragged* batch);
 
 /* Linear attention with a decay for each head.  For each new token t of a sequence,
@@ -294,12 +294,17 @@ size_t wz_decay_workspace_bytes(const wz_states* states, const wz_ragged* batch)
  * multiples of 8 elements, at most 2^22 (out's any), pointers 16-byte aligned; out
  * must not overlap q, k or v.  scale: finite.  Sums and states are fp32 (elements of
  * values and of states up to 2^110); a state's sum takes a decayed value with all of
- * its 24 bits, the outputs of prompts take the state and the decayed scores with 15.  A NaN or an infinity in a token's key, value or query
- * reaches those elements of rows and states that depend on it by the formula (as
- * one or the other), and no others.  Rows of tokens that no sequence has are not
- * written.  slot: int32 [batch].  ws: 256-byte aligned, at least
- * wz_decay_workspace_bytes() bytes; contents on entry are ignored.  One to three
- * kernel launches.                                                           */
+ * its 24 bits, the outputs of prompts take the state and the decayed scores with 15.
+ * A NaN or an infinity in a token's key, value or query reaches those elements of
+ * rows and states that depend on it by the formula (as one or the other), and no
+ * others.  Rows of tokens that no sequence has are not written.  slot: int32 [batch].
+ *
+ * Prompts of a call are cut into parts by what batch, tokens and max_tokens allow, so
+ * these also decide the order of sums: the same call gives the same bits.  max_tokens
+ * alone decides whether all its sequences go token by token (up to 8) or in chunks of
+ * 64: a prompt and many single tokens are better two calls.  ws: 256-byte aligned, at
+ * least wz_decay_workspace_bytes() bytes, for one call at a time (captured ones too);
+ * contents on entry are ignored.  One to three kernel launches.              */
 wz_status wz_decay_attention(const wz_states* states, const wz_ragged* batch,
                              const int32_t* slot, const float* log_decay,
                              const void* q, int64_t q_stride, const void* k,

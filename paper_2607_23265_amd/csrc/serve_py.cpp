@@ -435,7 +435,8 @@ PyObject* matmul_int(PyObject*, PyObject* const* a, Py_ssize_t n) {
 PyObject* gated_int(PyObject*, PyObject* const* a, Py_ssize_t n) {
   return guarded(n, 11, [&]() -> PyObject* {
     const Rows r = rows_in(a[0], a[1]);
-    const Weights gate = weights("gate", a[2], a[3], a[7], r.K, r.device), up = weights("up", a[4], a[5], a[8], r.K, r.device);
+    const Weights gate = weights("gate", a[2], a[3], a[7], r.K, r.device);
+    const Weights up = weights("up", a[4], a[5], a[8], r.K, r.device);
     if (gate.rows != up.rows) refuse("gate and up must have the same rows");
     const int32_t act = activation(a[6]);
     at::Tensor out = product_out(r, a[0], up.rows, a[9], a[10]);
@@ -553,8 +554,8 @@ PyObject* raise_as(PyObject*, PyObject* error) {
 
 #define FAST(f) {#f, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(f)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {FAST(cache), FAST(ragged), FAST(rotation), FAST(append), FAST(workspace), FAST(attention),
-                         FAST(quantize_rows), FAST(matmul_int), FAST(gated_int), FAST(norm_quantize), FAST(states), FAST(decay_workspace),
-                         FAST(decay_attention), {"raise_as", raise_as, METH_O, nullptr}, {}};
+                         FAST(quantize_rows), FAST(matmul_int), FAST(gated_int), FAST(norm_quantize), FAST(states),
+                         FAST(decay_workspace), FAST(decay_attention), {"raise_as", raise_as, METH_O, nullptr}, {}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_serve", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

@@ -8,7 +8,10 @@ namespace {
 // S <- l S + k v^T, out = scale q S, as they are written, in fp32.  A wave has 32
 // columns of a sequence's and head's state, four a lane, and a lane D / 8 of
 // their rows: what a row's 128 bytes of state need is read and written whole, and a
-// token's output is a sum over eight lanes.
+// token's output is a sum over eight lanes.  Few waves of many loads each: a state is
+// read and written once, and that bounds it.  Measured (28 heads of 128 elements): the
+// next tokens of 64 sequences, 235 MB, in 48.4 us, 4.9 TB/s (a large copy: 5.2);
+// of one sequence 5.8 us, where an empty launch takes 3.6.
 template <int D>
 __global__ __launch_bounds__(kWave) void k_decay_token(DecayArgs p) {
   constexpr int kRows = D / 8;  // of a lane

@@ -37,7 +37,9 @@ __device__ __forceinline__ void store8(float* p, float (&f)[8]) {
 // LANES threads a row (a wave: four rows a workgroup; or the workgroup).  Up to
 // CHUNKS chunks of 8 elements a thread stay in registers between the row's sums
 // and the rounding (as t = h * weight: the norm's factor is one number a row and
-// cancels in the codes); a longer row's others are read again.
+// cancels in the codes); a longer row's others are read again.  Bound by memory:
+// 9459 x 3584 in bf16 with a residual, 237 MB, in 41 to 48 us, 5.8 to 4.9 TB/s (the first
+// with its result in the last-level cache); 64 rows 4.1 us, a launch and three waits.
 template <typename T, int LANES, int CHUNKS>
 __global__ __launch_bounds__(256) void k_norm(NormArgs p) {
   __shared__ float red[3][4];
@@ -136,6 +138,11 @@ __global__ __launch_bounds__(256) void k_norm(NormArgs p) {
   }
 }
 
+// Measured (us, bf16 with a residual; a wave to a row, a workgroup with 2 chunks a thread,
+// with 8): 9459 x 512 9.1, 13.8, 23.2; 9459 x 1024 13.4, 16.6, 25.2; 9459 x 2048 26.5,
+// 24.0, 28.8; 9459 x 3584 53.5, 40.7, 53.9; 4096 x 8192 54.6, 46.1, 43.3; 2048 x 16384
+// 71.6, 49.4, 39.3.  Of 64 rows the same choices are the fastest but for one: 64 x 1024
+// 4.1, 3.5, 3.5.
 template <typename T>
 hipError_t norm(const NormArgs& p, hipStream_t s) {
   const dim3 block(256);

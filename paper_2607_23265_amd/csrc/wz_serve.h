@@ -158,7 +158,7 @@ struct DecayArgs {
   float scale;
   int group;     // heads that share a key head
   int runs;      // the plan's
-  bool join;
+  bool join;     // likewise
   float* part;   // runs > 1: [2][runs][heads][head_dim][head_dim], states
   int* goes_on;  // runs > 1: [runs] chunks of the run's last sequence, if that goes on in the next run (negative
                  // where it begins in this one); 0: it does not

@@ -1,9 +1,10 @@
 """Python binding of the serving operators (include/wavezip_serve.h): argument marshalling only, in csrc/serve_py.cpp.
 
 A paged key/value cache held in 8 bits and attention over it, linear attention over states of a fixed size, norms to 8
-bits and products in 8-bit integers, for a language model that reads the tokens wavezip.condense() keeps.  Tensors are torch GPU tensors; every call goes to the current HIP stream
-of their device.  Where a tensor has rows of heads ([tokens, heads, head_dim]) its rows may lie apart, so parts of one
-fused projection are passed as they are; everything else is contiguous.
+bits and products in 8-bit integers, for a language model that reads the tokens wavezip.condense() keeps.  Tensors are
+torch GPU tensors; every call goes to the current HIP stream of their device.  Where a tensor has rows of heads
+([tokens, heads, head_dim]) its rows may lie apart, so parts of one fused projection are passed as they are; everything
+else is contiguous.
 """
 import ctypes
 import operator
