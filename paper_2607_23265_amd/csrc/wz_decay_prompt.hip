@@ -16,12 +16,12 @@
 // are rounded to bf16 themselves, take the state and the decayed scores in two.
 // (With one part less each, eight long prompts took 2 to 9 % less.)
 //
-// Measured (28 heads of 128 elements): a prompt of 1286 tokens 38.5 us, eight of 3531 to
-// 9459 556 us, 0.17 PFLOP/s of what the formula asks for.  Their operations and bytes
+// Measured (28 heads of 128 elements): a prompt of 1286 tokens 35 to 38 us, eight of 3531 to
+// 9459 538 to 558 us, 0.18 PFLOP/s of what the formula asks for.  Their operations and bytes
 // would allow 5 and 291 us.  A chunk takes 10600 cycles where a CU has one workgroup,
 // 12200 each where it has two: stores to LDS 1000, scores 1900, q S 1500, scores times
 // values 1200, outputs 1400, the state 2300, and the waits between them.  No pipe is
-// full (vector ALU 39 % of the cycles, MFMA 32 %, LDS 35 %); registers allow two waves
+// full (vector ALU 35 % of the cycles, MFMA 36 %, LDS 28 %); registers allow two waves
 // a SIMD to overlap them.
 #include <cmath>
 

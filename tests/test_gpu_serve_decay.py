@@ -77,7 +77,8 @@ class Layer:
         for z in set(range(len(s))) - touched:
             np.testing.assert_array_equal(s[z], self.state[z])
         worst = []
-        for a, b, m, rel in ((g[:rows], out[:rows], mag[:rows], 2.0 ** -14 + U * (4 * n + 160)), (s, state, size, U * (4 * n + 160))):
+        sums = U * (4 * n + 160)
+        for a, b, m, rel in ((g[:rows], out[:rows], mag[:rows], 2.0 ** -14 + sums), (s, state, size, sums)):
             fine = np.isfinite(b)
             np.testing.assert_array_equal(np.isfinite(a), fine)
             tol = rel * m[fine]
@@ -107,7 +108,8 @@ def test_lengths(new, held, heads, kv, dim):
 @pytest.mark.parametrize("new,held,heads,kv,dim", [
     # runs of chunks that begin and end inside sequences, at their ends, and over several of them
     ([300, 0, 64, 1000, 9, 129, 640], [1, 1, 0, 1, 0, 0, 1], 3, 1, 64), ([128] * 9, [0, 1] * 4 + [1], 2, 2, 128),
-    ([1500], [1], 1, 1, 64), ([4000], [1], 1, 1, 64), ([3000, 9, 2500], [1, 0, 1], 2, 1, 128), ([64, 1200, 64], [1, 1, 1], 2, 2, 64), ([700, 1] * 3, [0] * 6, 40, 20, 64),
+    ([1500], [1], 1, 1, 64), ([4000], [1], 1, 1, 64), ([3000, 9, 2500], [1, 0, 1], 2, 1, 128),
+    ([64, 1200, 64], [1, 1, 1], 2, 2, 64), ([700, 1] * 3, [0] * 6, 40, 20, 64),
     # the most heads
     ([3, 1], [1, 0], 256, 64, 64), ([70], [1], 256, 256, 64)])
 def test_runs(new, held, heads, kv, dim):
@@ -341,8 +343,8 @@ def test_binding():
     three = torch.zeros(c.q.shape[0], 3, 64, dtype=BF, device=DEV)
     with pytest.raises(wz.WZError):
         f(*ok[:4], three, three, ld)
-    for bad in (torch.zeros(2, 3, 64, 32, device=DEV), torch.zeros(3, 64, 64, device=DEV), torch.zeros(2, 3, 64, 64, device=DEV, dtype=BF),
-                torch.zeros(2, 3, 64, 64)):
+    for bad in (torch.zeros(2, 3, 64, 32, device=DEV), torch.zeros(3, 64, 64, device=DEV),
+                torch.zeros(2, 3, 64, 64, device=DEV, dtype=BF), torch.zeros(2, 3, 64, 64)):
         with pytest.raises(ValueError):
             serve.States(bad)
     with pytest.raises(wz.WZError):
