@@ -285,6 +285,25 @@ def test_runs_agree_bit_for_bit(new, dim):
         assert torch.equal(out[:rows], want[:rows]) and torch.equal(z.state, eager.state), i
 
 
+def test_two_calls_at_once():
+    """Two calls on streams of their own, each with a workspace and states of its own."""
+    cs = [Layer([2100, 30], [1, 1], 8, 2, 128, seed=11), Layer([900, 1, 1300], [0, 1, 1], 8, 2, 64, seed=12)]
+    want = [c.run() for c in cs]
+    streams, states = [torch.cuda.Stream() for _ in cs], [serve.States(torch.from_numpy(c.state).to(DEV)) for c in cs]
+    args = [(ints(c.slot), torch.from_numpy(c.log_decay).to(DEV), c.batch(), torch.full(c.q.shape, 9.0, dtype=BF, device=DEV))
+            for c in cs]
+    for _ in range(3):
+        for c, z in zip(cs, states):
+            z.state.copy_(torch.from_numpy(c.state))
+        torch.cuda.synchronize()
+        for c, z, s, (slot, ld, batch, out) in zip(cs, states, streams, args):
+            with torch.cuda.stream(s):
+                serve.decay_attention(z, batch, slot, c.q, c.k, c.v, ld, scale=c.scale, out=out)
+        torch.cuda.synchronize()
+        for (rows, z0), z, (_, _, _, out) in zip(want, states, args):
+            assert torch.equal(out, rows) and torch.equal(z.state, z0.state)
+
+
 def test_nothing_behind_the_workspace_is_written():
     c = Layer([1500, 900], [1, 0], 4, 2, 64, seed=6)
     z, batch = serve.States(torch.from_numpy(c.state).to(DEV)), c.batch()

@@ -294,3 +294,53 @@ def test_refusals():
                dict(residual=torch.zeros(5, 4, device=DEV, dtype=BF)), dict(residual=s)):
         with pytest.raises(ValueError):
             m(q, s, q, s, **kw)
+
+
+def block(s, x, out):
+    """A feed-forward block onto the residual stream, as a layer runs it."""
+    h, hs, total = serve.norm_quantize(x, s["norm"], residual=s["res"])
+    act = serve.gated_int(h, hs, s["w"][:s["n"]], s["ws"][:s["n"]], s["w"][s["n"]:], s["ws"][s["n"]:])
+    a, asc = serve.quantize_rows(act)
+    y = serve.matmul_int(a, asc, s["down"], s["downs"], residual=total)
+    serve.matmul_int(h, hs, s["down2"], s["ws"][:s["down2"].shape[0]], bias=s["norm"][:s["down2"].shape[0]], out=out,
+                     activation="gelu")
+    return y
+
+
+@pytest.mark.parametrize("M", [1, 64, 1300])
+def test_captured_and_beside_another_stream(M):
+    """A block captured and replayed with other rows, and two at once on streams of their own: the eager results."""
+    C, N = 512, 1152
+    r = np.random.default_rng(M)
+    _, _, w, ws = codes(r, 2 * N, C, 0, 0)
+    _, _, down, downs = codes(r, C, N, 0, 0)
+    _, _, down2, _ = codes(r, 300, C, 0, 0)
+    s = dict(norm=1 + 0.1 * torch.randn(C, device=DEV), res=torch.randn(M, C, device=DEV).to(BF), w=w, ws=ws, n=N, down=down,
+             downs=downs, down2=down2)
+    xs = [torch.randn(M, C, device=DEV).to(BF) for _ in range(4)]
+    want = []
+    for x in xs:
+        out = torch.zeros(M, 300, dtype=BF, device=DEV)
+        want.append((block(s, x, out), out))
+    x, out = xs[0].clone(), torch.zeros(M, 300, dtype=BF, device=DEV)
+    block(s, x, out)
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        y = block(s, x, out)
+    for k in (1, 2, 3, 0, 2):
+        x.copy_(xs[k])
+        g.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(y, want[k][0]) and torch.equal(out, want[k][1]), k
+        block(s, xs[k], torch.empty_like(out))  # (work of the program's own between replays)
+    streams, got = [torch.cuda.Stream() for _ in range(2)], [[], []]
+    torch.cuda.synchronize()
+    for k in range(4):
+        with torch.cuda.stream(streams[k % 2]):
+            out = torch.zeros(M, 300, dtype=BF, device=DEV)
+            got[k % 2].append((block(s, xs[k], out), out))
+    torch.cuda.synchronize()
+    for k in range(4):
+        a, b = got[k % 2][k // 2]
+        assert torch.equal(a, want[k][0]) and torch.equal(b, want[k][1]), k
