@@ -533,13 +533,13 @@ hipError_t prompt(const DecayArgs& p, hipStream_t s) {
 // sums over the runs before: each run adds up its own (64 KiB of every run before it,
 // 0.5 us where a CU has one workgroup, 0.9 with two), or, where those are many, a
 // launch between the two does.  Measured on the side that the rule takes and on the other
-// (28 heads of 128 elements): whole or in runs, 200 tokens 22 and 23 us, 8 x 200 27 and
-// 43, 16 x 600 88 and 127, 8 x 6562 505 and 555; in runs or whole, 1286 tokens 38.5
-// and 96, four of 2000 101 and 148, 9459 125 and 661, eight of 3531 to 9459 556
-// and 678; sums of their own or joined, 1286 tokens 38.5 and 42.6, eight of 3531 to
-// 9459 556 and 565; joined or not, 9459 tokens 125 and 134, 16384 of 2 heads 62 and 127.  With heads
-// of 64 elements, whole or in runs: 64 x 600 154 and 171; in runs or whole: 1286
-// tokens 23.5 and 69, 8 x 3000 113 and 152.
+// (28 heads of 128 elements): whole or in runs, 200 tokens 22.1 and 22.8 us, 8 x 200 27 and
+// 42, 3 x 300 28 and 33, 16 x 600 88 and 125, 8 x 6562 503 and 552; in runs or whole, 330
+// tokens 24 and 31, 1286 tokens 38 and 97, four of 2000 101 and 147, 9459 123 and 663,
+// eight of 3531 to 9459 552 and 675; sums of their own or joined, 1286 tokens 38.5 and
+// 42.6, eight of 3531 to 9459 556 and 565; joined or not, 9459 tokens 125 and 134.  With
+// heads of 64 elements, whole or in runs: 64 x 600 155 and 169, 32 x 3000 402 and 413; in
+// runs or whole: 1286 tokens 23 and 69, 8 x 3000 111 and 152.
 DecayPlan decay_plan(const wz_states& z, const wz_ragged& r) {
   DecayPlan p{};
   p.token = r.max_tokens <= 8;
@@ -564,8 +564,9 @@ DecayPlan decay_plan(const wz_states& z, const wz_ragged& r) {
     const double each = std::ceil(all / most_runs), again = std::max(0., 1 - each * r.batch / (2 * all));
     const int runs = int(std::ceil(all / each)), there = (runs * z.heads + kCUs - 1) / kCUs;
     const double join = x.join + x.join_run * runs, adds = x.adds[there] * std::min(std::ceil(most / each), runs - 1.);
-    const double next = 8 * each * r.batch / all;  // from one sequence to the next
-    const double time = 12.5 + std::min(join, adds) + each * x.chunk[there] * (1 + 0.4 * again) + next;
+    const double next = 12 * each * r.batch / all;  // from one sequence to the next
+    const double states = 0.025 * runs * z.heads * z.head_dim * z.head_dim / 16384;  // to memory and from it
+    const double time = 5 + states + std::min(join, adds) + each * x.chunk[there] * (1 + 0.4 * again) + next;
     if (time < best) best = time, p.runs = runs, p.join = join < adds;
   }
   if (p.runs == 0) return p;
