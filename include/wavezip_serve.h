@@ -272,8 +272,9 @@ typedef struct {
 } wz_states;
 
 /* Bytes of workspace wz_decay_attention needs (0 if the arguments are invalid or
- * none is needed), at most 65 MiB: what parts of long sequences add to their
- * states.  Depends on batch, tokens, max_tokens, heads and head_dim alone.   */
+ * none is needed): what parts of long sequences add to their states.  Depends on
+ * batch, tokens, max_tokens, heads and head_dim alone, and fewer tokens can need
+ * more; 65 MiB do for every call.                                            */
 size_t wz_decay_workspace_bytes(const wz_states* states, const wz_ragged* batch);
 
 /* Linear attention with a decay for each head.  For each new token t of a sequence,
