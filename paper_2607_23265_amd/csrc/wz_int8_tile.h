@@ -102,7 +102,7 @@ __device__ __forceinline__ void wait_loads() {
 // The matrix cores are busy for 58 % of the large product's cycles (at 1.9 GHz),
 // LDS for 26 %.
 //
-// Tiles of BM x BN, WM x WN waves, 128 bytes of k at a time through ST stages of
+// Tiles of BM x BN, WM x WN waves, KB bytes of k at a time through ST stages of
 // LDS that the loads write directly, ST - 1 stages ahead of the work.  KS such
 // groups of waves take the steps in turn and add up their integers at the end.
 // Chunks of 16 bytes are exchanged within a row by the row's number, so that
@@ -112,9 +112,10 @@ __device__ __forceinline__ void wait_loads() {
 // kGated: a tile's BN rows of weights are 16 of the gate and 16 of the other
 // projection in turn, so that a lane has both sums of an element, in eight
 // registers of the same fragment, and neither leaves the registers.
-constexpr int KB = 128;  // bytes of a row in a stage
-template <typename Out, int BM, int BN, int WM, int WN, int ST, int KS, int EPI>
-__global__ __launch_bounds__(WM* WN* KS* kWave) void k_matmul_tile(MatmulArgs p, int tiles_m, int tiles_n) {
+//
+// KB = 64: half of the LDS, and registers for three tiles on a CU.
+template <typename Out, int BM, int BN, int WM, int WN, int ST, int KS, int EPI, int KB>
+__global__ __launch_bounds__(WM* WN* KS* kWave, KB == 64 ? 3 : 1) void k_matmul_tile(MatmulArgs p, int tiles_m, int tiles_n) {
   constexpr int kWaves = WM * WN, MT = BM / WM / 32, NT = BN / WN / 32;
   constexpr int kChunks = KB / 16, kLoadRows = kWave / kChunks;  // chunks of a row, rows of one load
   constexpr int kLoadsA = BM / kLoadRows / kWaves, kLoadsB = BN / kLoadRows / kWaves;
@@ -124,7 +125,7 @@ __global__ __launch_bounds__(WM* WN* KS* kWave) void k_matmul_tile(MatmulArgs p,
   __shared__ __align__(16) int8_t lds[ST * KS * kStage];  // [ST][KS][rows of a, then of w][KB]
   const int lane = __lane_id(), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   const int w = wave % kWaves, group = wave / kWaves, c = lane & 31, g = lane >> 5;
-  auto exchange = [](int row) { return row >> 1 & 7; };
+  auto exchange = [](int row) { return KB == 128 ? row >> 1 & 7 : row >> 2 & 3; };
 
   // Workgroups go to the XCDs in turn: each XCD gets a run of tiles that lie
   // together (columns of 8 row tiles), whose rows and weights its L2 holds.
@@ -389,12 +390,12 @@ __global__ __launch_bounds__(WM* WN* KS* kWave) void k_matmul_tile(MatmulArgs p,
 template <int EPI>
 int64_t weight_rows(const MatmulArgs& p) { return EPI == kGated ? 2 * int64_t(p.N) : p.N; }
 
-template <typename Out, int BM, int BN, int WM, int WN, int ST, int KS, int EPI>
+template <typename Out, int BM, int BN, int WM, int WN, int ST, int KS, int EPI, int KB = 128>
 hipError_t tiles(const MatmulArgs& p, hipStream_t s) {
   const int64_t tm = (p.M + BM - 1) / BM, tn = (weight_rows<EPI>(p) + BN - 1) / BN;
   const int64_t groups = (tm * tn + kXcds - 1) / kXcds * kXcds;
   if (groups > 0x7fffffff) return hipErrorInvalidValue;
-  hipLaunchKernelGGL((k_matmul_tile<Out, BM, BN, WM, WN, ST, KS, EPI>), dim3(uint32_t(groups)),
+  hipLaunchKernelGGL((k_matmul_tile<Out, BM, BN, WM, WN, ST, KS, EPI, KB>), dim3(uint32_t(groups)),
                      dim3(WM * WN * KS * kWave), 0, s, p, int(tm), int(tn));
   return hipGetLastError();
 }
@@ -421,8 +422,9 @@ struct Tile {
   // 1152: 92 us in tiles of 256 x 256, 87 in two of 128 x 128 at a time; without one
   // the first are the faster).
   double act(const MatmulArgs& p) const {
-    if (EPI != kRich || p.activation == WZ_ACT_NONE || p.activation == WZ_ACT_RELU) return 0;
-    return (p.activation == WZ_ACT_GELU ? 10. : 5.) * (at_once > 1 ? 0.44 : 1.) * at_once * bm * bn / 65536.;
+    if (EPI == kPlain || p.activation == WZ_ACT_NONE || p.activation == WZ_ACT_RELU) return 0;
+    const double elements = at_once * bm * bn / 65536. * (EPI == kGated ? 0.5 : 1.);
+    return (p.activation == WZ_ACT_GELU ? 10. : 5.) * (at_once > 1 ? 0.44 : 1.) * elements;
   }
   double time(const MatmulArgs& p, double rounds) const {
     return fixed + rounds * (ends + act(p) + steps * (p.K / 3584.));
@@ -451,10 +453,21 @@ hipError_t matmul(const MatmulArgs& p, hipStream_t s) {
       {192, 128, 2.5, 3.8, 19.6, 1, tiles<Out, 192, 128, 2, 4, 3, 1, EPI>},
       {256, 256, 8.0, 5.0, 44.6, 1, tiles<Out, 256, 256, 2, 4, 2, 1, EPI>},
   };
+  // For few steps of K and an activation, whose instructions three tiles on a CU hide
+  // better than two: gelu after 12544 x 3584 x 576 57 us, without this 65, x 1152 79 and
+  // 84, silu 78 and 83; gated 6000 x 4304 x 576 51 and 61.  (x 2304: 144 and 130.)
+  auto each = [](auto f) {
+    for (const Tile<Out, EPI>& t : kTiles) f(t);
+    if constexpr (EPI != kPlain) {
+      static constexpr Tile<Out, EPI> kThree{128, 128, 3.7, 3.5, 43.9, 3, tiles<Out, 128, 128, 2, 2, 3, 1, EPI, 64>};
+      f(kThree);
+    }
+  };
   auto fastest = [&](const MatmulArgs& q) {
     const Tile<Out, EPI>* best = kTiles;
-    for (const Tile<Out, EPI>& t : kTiles)
+    each([&](const Tile<Out, EPI>& t) {
       if (t.time(q) < best->time(q)) best = &t;
+    });
     return best;
   };
   // Rows of tiles that fill whole rounds, and what is left in tiles that fit it
@@ -464,15 +477,15 @@ hipError_t matmul(const MatmulArgs& p, hipStream_t s) {
   double best = whole->time(p);
   const Tile<Out, EPI>* first = nullptr;
   int rows = 0;
-  for (const Tile<Out, EPI>& t : kTiles) {
+  each([&](const Tile<Out, EPI>& t) {
     const int64_t at_once = kCUs * t.at_once, rounds = t.count(p) / at_once;
     const int64_t full = rounds * at_once / t.columns(p) * t.bm;
-    if (full <= 0 || full >= p.M) continue;
+    if (full <= 0 || full >= p.M) return;
     MatmulArgs rest = p;
     rest.M = p.M - int(full);
     const double time = t.time(p, double(rounds)) + fastest(rest)->time(rest);
     if (time < best) best = time, first = &t, rows = int(full);
-  }
+  });
   if (!first) return whole->run(p, s);
   MatmulArgs part = p;
   part.M = rows;

@@ -230,8 +230,8 @@ def gated_int(a, a_scale, gate, gate_scale, up, up_scale, activation="silu", gat
 
 def norm_quantize(x, weight, eps=1e-6, residual=None, total=None, out=None, scale=None):
     """wz_norm_quantize: the root-mean-square norm of x [rows, cols] float32 or bfloat16, times weight [cols] float32 ->
-    (int8 [rows, cols], scale [rows] float32).  With a residual like x the norm is of their sum, which is the third result
-    (total, which may be x or residual itself)."""
+    (int8 [rows, cols], scale [rows] float32).  With a residual like x the norm is of their sum, which is the third
+    result (total, which may be x or residual itself)."""
     return _native.norm_quantize(x, weight, eps, residual, total, out, scale)
 
 
@@ -241,9 +241,9 @@ def decay_workspace_bytes(states, batch, tokens):
 
 
 def decay_attention(states, batch, slot, q, k, v, log_decay, scale=None, out=None, ws=None):
-    """wz_decay_attention: linear attention with a decay for each head, S <- exp(log_decay) S + k v^T and out = scale q S
-    token after token, from and to the states of slot [batch] int32 (which hold what is before the batch's new tokens; the
-    batch's table is not looked at).  q [tokens, heads, head_dim], k and v [tokens, kv_heads, head_dim] bfloat16, log_decay
-    [heads] float32 -> out like q.  scale defaults to head_dim ** -0.5; ws is a uint8 workspace (allocated if not given
-    and needed)."""
+    """wz_decay_attention: linear attention with a decay for each head, S <- exp(log_decay) S + k v^T and out = scale
+    q S token after token, from and to the states of slot [batch] int32 (which hold what is before the batch's new
+    tokens; the batch's table is not looked at).  q [tokens, heads, head_dim], k and v [tokens, kv_heads, head_dim]
+    bfloat16, log_decay [heads] float32 -> out like q.  scale defaults to head_dim ** -0.5; ws is a uint8 workspace
+    (allocated if not given and needed)."""
     return _native.decay_attention(states._c, batch._c, slot, q, k, v, log_decay, scale, out, ws)

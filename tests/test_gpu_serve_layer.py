@@ -62,7 +62,7 @@ def check(got, want, tol, dtype, what):
 # one for each tile that a product is done in, with ragged edges, and the smallest
 SHAPES = [(1, 1, 16), (1, 100, 48), (2, 17, 3584), (31, 33, 80), (64, 4608, 1152), (65, 130, 1040), (130, 257, 3600),
           (300, 640, 16), (1286, 384, 1152), (513, 769, 2064), (33, 9000, 144), (391, 2040, 528), (1286, 4600, 48),
-          (2499, 4601, 144), (100, 15, 8192), (3, 2300, 65536)]
+          (2499, 4601, 144), (100, 15, 8192), (3, 2300, 65536), (4100, 3000, 272)]
 
 
 @pytest.mark.parametrize("M,N,K", SHAPES)
