@@ -92,7 +92,7 @@ def build(verbose=False):
     _link("libwavezip.so", LIB, [hipcc(), "-shared", f"--offload-arch={ARCH}", *[o for o, _ in results]])
     libs = os.path.join(os.path.dirname(torch.__file__), "lib")
     _link("_serve.so", BINDING, ["g++", "-shared", binding[0], "-L", PKG, "-l:libwavezip.so", "-L", libs, "-ltorch_python",
-                                 "-ltorch_cpu", "-ltorch_hip", "-lc10_hip", "-lc10", "-Wl,-rpath,$ORIGIN"])
+                                 "-ltorch_cpu", "-lc10_hip", "-lc10", "-Wl,-rpath,$ORIGIN"])
     return LIB
 
 

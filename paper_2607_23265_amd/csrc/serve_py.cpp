@@ -7,7 +7,7 @@
 #include <torch/csrc/Dtype.h>
 #include <torch/csrc/autograd/python_variable.h>
 
-#include <ATen/hip/EmptyTensor.h>
+#include <ATen/ops/empty.h>
 #include <c10/core/DeviceGuard.h>
 #include <c10/hip/HIPStream.h>
 
@@ -88,9 +88,10 @@ int64_t matrix(const char* name, const at::Tensor& t, bool floats, int device = 
 }
 bool is(const at::Tensor& t, std::initializer_list<int64_t> shape) { return t.sizes() == at::IntArrayRef(shape); }
 
-// An output, of the current stream.  (Through torch's dispatcher, as at::empty, one took 0.2 us more.)
+// An output, of the current stream: through torch's dispatcher, so that it is filled where the program asks torch for
+// that (rows of no sequence are not written), and dispatch modes see it.
 at::Tensor empty_on(const at::Tensor& like, at::IntArrayRef shape, at::ScalarType type) {
-  return at::Tensor(at::detail::empty_cuda(shape, type, like.device(), std::nullopt));
+  return at::empty(shape, like.options().dtype(type).requires_grad(false));
 }
 
 // A struct with its kind (several have the same size) and its device, as bytes.
