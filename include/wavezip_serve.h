@@ -294,9 +294,10 @@ size_t wz_decay_workspace_bytes(const wz_states* states, const wz_ragged* batch)
  * which divide heads: head h reads key head h / (heads / kv_heads).  Strides are
  * multiples of 8 elements, at most 2^22 (out's any), pointers 16-byte aligned; out
  * must not overlap q, k or v.  scale: finite.  Sums and states are fp32 (elements of
- * values and of states up to 2^110); a state's sum takes a decayed value with all of
- * its 24 bits, the outputs of prompts take the state and the decayed scores with 15.
- * A decay (over any number of tokens) below 2^-126 counts as zero.
+ * values and of states up to 2^110; in prompts what lies below 2^-110 in them may count
+ * as zero); a state's sum takes a decayed value with all of its 24 bits, the outputs of
+ * prompts take the state and the decayed scores with 15.  A decay (over any number of
+ * tokens) below 2^-126 counts as zero.
  * A NaN or an infinity in a token's key, value or query reaches those elements of
  * rows and states that depend on it by the formula (as one or the other), and no
  * others.  Rows of tokens that no sequence has are not written.  slot: int32 [batch].

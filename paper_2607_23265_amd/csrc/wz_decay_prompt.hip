@@ -34,6 +34,9 @@ typedef float f32x16 __attribute__((ext_vector_type(16)));
 
 constexpr int kChunk = 64;
 constexpr float kRaised = 16.f;  // log2 of what a state is raised by at most
+// For outputs a state is kept this much lower, so that raised it is what it stands for at most, and q S, which is
+// formed from it, passes fp32 no sooner than the formula's.
+constexpr float kLower = 0x1p-16f, kHigher = 0x1p16f;
 
 __device__ __forceinline__ f32x16 mfma(u32x4 a, u32x4 b, f32x16 c) {
   return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0,
@@ -254,18 +257,19 @@ __global__ __launch_bounds__(2 * D, 2) void k_decay_prompt(DecayArgs p) {
       for (int r = run; r > 0; --r) {
         const int before = first_of(r, all.all, all.runs);
         if (before <= begins) break;
-        from(stored(p, kBegins, r, h), power(float((here - before) * kChunk) * ld));
+        from(stored(p, kBegins, r, h), power(float((here - before) * kChunk) * ld) * kLower);
       }
     } else if (OUT && first > 0) {
-      from(stored(p, kBegins, run, h), 1.f);
+      from(stored(p, kBegins, run, h), kLower);
     } else if (OUT && on) {
-      from(stored(p, kFirst, run, h), 1.f);
+      from(stored(p, kFirst, run, h), kLower);
     } else if (kept && s.place0 > 0 && first == 0) {
 #pragma unroll
       for (int a = 0; a < NA; ++a)
 #pragma unroll
         for (int r = 0; r < 16; ++r)
-          S[a][r] = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(state, in_state, row_of(a, r), 0));
+          S[a][r] = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(state, in_state, row_of(a, r), 0)) *
+                    (OUT ? kLower : 1.f);
     }
     // (the run that stores the sequence's last state may do so before another looks at what the slot holds)
     if (!OUT && first == 0) into(stored(p, kFirst, run, h));
@@ -285,12 +289,12 @@ __global__ __launch_bounds__(2 * D, 2) void k_decay_prompt(DecayArgs p) {
     for (int i = 0; i < chunks; ++i, t0 += OUT ? kChunk : -kChunk) {
       const int len = min(kChunk, last - t0);
       // Outputs: S, whatever the text says of it, is kept as of `age` tokens ago (without their decay), so that it is
-      // not multiplied with every chunk's; what is added to it is raised by as much.
+      // not multiplied with every chunk's; what is added to it is raised by as much.  And times kLower.
       const bool renew = OUT && float(age + len) * ld < -kRaised;
       const int from_age = renew ? -len : age;
       if (threadIdx.x < kChunk)
         weight[threadIdx.x] = power(float(OUT ? -(from_age + 1 + min(int(threadIdx.x), len - 1))
-                                              : last - 1 - t0 - int(threadIdx.x)) * ld);
+                                              : last - 1 - t0 - int(threadIdx.x)) * ld) * (OUT ? kLower : 1.f);
       store_columns(kt, nk);
       store_columns(vt, nv);
       if constexpr (OUT) {
@@ -362,9 +366,9 @@ __global__ __launch_bounds__(2 * D, 2) void k_decay_prompt(DecayArgs p) {
           }
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
-          const float f = power(float(age + 32 * i + row + 1) * ld) * p.scale;
+          const float f = power(float(age + 32 * i + row + 1) * ld) * kHigher;
 #pragma unroll
-          for (int r = 0; r < 16; ++r) O[i][r] *= f;
+          for (int r = 0; r < 16; ++r) O[i][r] = O[i][r] * f * p.scale;
         }
         lds_barrier();
         read_values();
@@ -452,8 +456,8 @@ __global__ __launch_bounds__(2 * D, 2) void k_decay_prompt(DecayArgs p) {
       lds_barrier();
       age = from_age + len;
     }
-    if (OUT && age > 0) {
-      const float fade = power(float(age) * ld);
+    if constexpr (OUT) {
+      const float fade = power(float(age) * ld) * kHigher;
 #pragma unroll
       for (int a = 0; a < NA; ++a)
 #pragma unroll
