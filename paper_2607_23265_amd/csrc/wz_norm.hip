@@ -105,7 +105,8 @@ __global__ __launch_bounds__(256) void k_norm(NormArgs p) {
   }
   const bool fine = amax < 0x7f800000u;
   float unit = 1.f, eps = p.eps;
-  if (fine && !(sum < INFINITY)) {  // (the same for all of a row's threads) squares past fp32: of h / 2^80
+  // (the same for all of a row's threads) squares past fp32, or with eps: of h / 2^80, and eps by as much
+  if (fine && !(sum + eps < INFINITY)) {
     float again = 0.f;
     for (int c = t; c < chunks; c += LANES) {
       float h[8];
@@ -113,7 +114,7 @@ __global__ __launch_bounds__(256) void k_norm(NormArgs p) {
 #pragma unroll
       for (int e = 0; e < 8; ++e) again = fmaf(h[e] * 0x1p-80f, h[e] * 0x1p-80f, again);
     }
-    sum = row_sum(2, wave_sum(again)), unit = 0x1p-80f, eps = 0.f;
+    sum = row_sum(2, wave_sum(again)), unit = 0x1p-80f, eps *= 0x1p-80f, eps *= 0x1p-80f;
   }
   const float top = fmaxf(__uint_as_float(amax), 0x1p-100f), up = 127.f / top;
   if (t == 0)
