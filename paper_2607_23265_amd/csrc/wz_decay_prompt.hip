@@ -16,13 +16,12 @@
 // are rounded to bf16 themselves, take the state and the decayed scores in two.
 // (With one part less each, eight long prompts took 2 to 9 % less.)
 //
-// Measured (28 heads of 128 elements): a prompt of 1286 tokens 35 to 38 us, eight of 3531 to
-// 9459 538 to 558 us, 0.18 PFLOP/s of what the formula asks for.  Their operations and bytes
-// would allow 5 and 291 us.  A chunk takes 10600 cycles where a CU has one workgroup,
-// 12200 each where it has two: stores to LDS 1000, scores 1900, q S 1500, scores times
-// values 1200, outputs 1400, the state 2300, and the waits between them.  No pipe is
-// full (vector ALU 35 % of the cycles, MFMA 36 %, LDS 28 %); registers allow two waves
-// a SIMD to overlap them.
+// Measured (28 heads of 128 elements): a prompt of 1286 tokens 35 to 40 us, eight of 3531 to
+// 9459 552 to 575 us, 0.17 PFLOP/s of what the formula asks for.  Their operations and bytes
+// would allow 5 and 291 us.  A chunk takes 5.4 us where a CU has one workgroup, and 8.4 where
+// it has two: scores, q S, scores times values and the state one after the other, with four
+// barriers.  No pipe is full (vector ALU 36 % of the cycles, MFMA 36 %, LDS 28 %); registers
+// allow two waves a SIMD to overlap them.
 #include <cmath>
 
 #include "wz_decay.h"
@@ -525,8 +524,10 @@ hipError_t prompt(const DecayArgs& p, hipStream_t s) {
 
 }  // namespace
 
-// Token after token up to 8 of a sequence: 5 and 16 tokens (28 heads of 128 elements) 6.5
-// and 14.9 us, in a chunk 8.9; of 64 sequences 42 and 70, in chunks 52 and 54.
+// Token after token up to 8 of a sequence.  With states that come from memory, 28 heads, token
+// after token and in a chunk (us): 5, 8 and 16 tokens of one sequence 7.7 and 10.1, 10.3 and 10.2,
+// 17.2 and 10.2; of 64 sequences 55 and 60, 63 and 61, 87 and 64; with heads of 64 elements
+// 5.0 and 7.1, 6.4 and 7.0, 10.0 and 7.1; 21 and 29, 24 and 29, 34 and 30.
 //
 // Then a workgroup to a sequence and head, or to a run of chunks of all sequences.
 // What a chunk takes was measured (us), where a CU has one workgroup, two or three:
@@ -537,13 +538,14 @@ hipError_t prompt(const DecayArgs& p, hipStream_t s) {
 // sums over the runs before: each run adds up its own (64 KiB of every run before it,
 // 0.5 us where a CU has one workgroup, 0.9 with two), or, where those are many, a
 // launch between the two does.  Measured on the side that the rule takes and on the other
-// (28 heads of 128 elements): whole or in runs, 200 tokens 22.1 and 22.8 us, 8 x 200 27 and
-// 42, 3 x 300 28 and 33, 16 x 600 88 and 125, 8 x 6562 503 and 552; in runs or whole, 330
-// tokens 24 and 31, 1286 tokens 38 and 97, four of 2000 101 and 147, 9459 123 and 663,
-// eight of 3531 to 9459 552 and 675; sums of their own or joined, 1286 tokens 38.5 and
-// 42.6, eight of 3531 to 9459 556 and 565; joined or not, 9459 tokens 125 and 134.  With
-// heads of 64 elements, whole or in runs: 64 x 600 155 and 169, 32 x 3000 402 and 413; in
-// runs or whole: 1286 tokens 23 and 69, 8 x 3000 111 and 152.
+// (28 heads of 128 elements, rows and states from memory): whole or in runs, 200 tokens 23.5
+// and 23.6 us, 8 x 200 31 and 48, 3 x 300 32 and 36, 16 x 600 94 and 131, 8 x 6562 509 and
+// 548; in runs or whole, 330 tokens 25.6 and 33, 1286 tokens 37.5 and 105, four of 2000 109 and
+// 160, 9459 135 and 696, eight of 3531 to 9459 553 and 686; sums of their own or joined,
+// 1286 tokens 37.4 and 40.5, eight of 3531 to 9459 553 and 559; joined or not, 9459 tokens
+// 135 and 142.  With heads of 64 elements, whole or in runs: 64 x 600 161 and 175, 32 x 3000
+// 408 and 427; in runs or whole: 1286 tokens 25.6 and 72, 8 x 3000 124 and 157; joined or
+// not, 9459 tokens 69.1 and 67.2.
 DecayPlan decay_plan(const wz_states& z, const wz_ragged& r) {
   DecayPlan p{};
   p.token = r.max_tokens <= 8;

@@ -426,8 +426,8 @@ struct Tile {
   int64_t count(const MatmulArgs& p) const { return (int64_t(p.M) + bm - 1) / bm * columns(p); }
   // An activation's instructions, in a round's ends: 10 us with the error function for
   // 256 x 256 elements, where a second tile's products hide them 4.4 (12544 x 3584 x
-  // 1152: 92 us in tiles of 256 x 256, 87 in two of 128 x 128 at a time; without one
-  // the first are the faster).
+  // 1152: 92 us in tiles of 256 x 256, 87 in two of 128 x 128 at a time, with an error
+  // function of four instructions less; without one the first are the faster).
   double act(const MatmulArgs& p) const {
     if (EPI == kPlain || p.activation == WZ_ACT_NONE || p.activation == WZ_ACT_RELU) return 0;
     const double elements = at_once * bm * bn / 65536. * (EPI == kGated ? 0.5 : 1.);
@@ -461,8 +461,8 @@ hipError_t matmul(const MatmulArgs& p, hipStream_t s) {
       {256, 256, 8.0, 5.0, 44.6, 1, tiles<Out, 256, 256, 2, 4, 2, 1, EPI>},
   };
   // For few steps of K and an activation, whose instructions three tiles on a CU hide
-  // better than two: gelu after 12544 x 3584 x 576 57 us, without this 65, x 1152 79 and
-  // 84, silu 78 and 83; gated 6000 x 4304 x 576 51 and 61.  (x 2304: 144 and 130.)
+  // better than two: gelu after 12544 x 3584 x 576 63 us, without this 74, x 1152 84 and
+  // 93, silu 79 and 84; gated 6000 x 4304 x 576 52 and 64.  (Gelu, x 2304: 143 and 141.)
   auto each = [](auto f) {
     for (const Tile<Out, EPI>& t : kTiles) f(t);
     if constexpr (EPI != kPlain) {
