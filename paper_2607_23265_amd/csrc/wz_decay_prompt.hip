@@ -17,7 +17,7 @@
 // (With one part less each, eight long prompts took 2 to 9 % less.)
 //
 // Measured (28 heads of 128 elements): a prompt of 1286 tokens 35 to 40 us, eight of 3531 to
-// 9459 552 to 575 us, 0.17 PFLOP/s of what the formula asks for.  Their operations and bytes
+// 9459 541 to 575 us, 0.17 PFLOP/s of what the formula asks for.  Their operations and bytes
 // would allow 5 and 291 us.  A chunk takes 5.4 us where a CU has one workgroup, and 8.4 where
 // it has two: scores, q S, scores times values and the state one after the other, with four
 // barriers.  No pipe is full (vector ALU 36 % of the cycles, MFMA 36 %, LDS 28 %); registers

@@ -12,7 +12,7 @@ namespace {
 // read and written once, and that bounds it.  Measured with states that come from memory
 // (28 heads of 128 elements): the next tokens of 64 sequences, 235 MB, in 48.0 to 48.5 us,
 // 4.9 TB/s (a large copy: 5.1 to 5.2; with the states in the last-level cache 37 us); of one
-// sequence 4.4 to 4.8 us, where an empty launch takes 3.6.  Heads of 64 elements: 16.3 and 3.9.
+// sequence 4.4 to 5.5 us, where an empty launch takes 3.6.  Heads of 64 elements: 16.3 and 3.9.
 template <int D>
 __global__ __launch_bounds__(kWave) void k_decay_token(DecayArgs p) {
   constexpr int kRows = D / 8;  // of a lane

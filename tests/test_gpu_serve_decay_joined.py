@@ -60,7 +60,8 @@ def check(c, got, states, what):
     g, s = got[:rows].double().cpu().numpy(), states.state.double().cpu().numpy()
     chunks, r = sums_of(c.new, runs)
     worst = np.max(np.abs(s - state) / (U * (13 * chunks + 2 * r + 160) * size))
-    norms = off(s[touched], state[touched]) / state_norm_bound(c.new, runs), off(g, out[:rows]) / (2.0 ** -8 / 3 ** 0.5 + 2.0 ** -14)
+    norms = (off(s[touched], state[touched]) / state_norm_bound(c.new, runs),
+             off(g, out[:rows]) / (2.0 ** -8 / 3 ** 0.5 + 2.0 ** -14))
     print(f"[err] {what}: state {worst:.3f} of the bound, as a whole {norms[0]:.3f}, outputs {norms[1]:.3f}", flush=True)
     assert worst <= 1 and norms[0] <= 1 and norms[1] <= 1
 
